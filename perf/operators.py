@@ -147,7 +147,8 @@ def _int32(values):
 def _scale_of(amax):
     """The smallest power of two s with amax <= 448 s."""
     m, e = torch.frexp(amax)
-    return torch.ldexp(torch.ones_like(amax), torch.where(m > 0.875, e - 8, e - 9)).clamp(min=_LOWEST)
+    s = torch.ldexp(torch.ones_like(amax), torch.where(m > 0.875, e - 8, e - 9)).clamp(min=_LOWEST)
+    return torch.where(amax > 0, s, _LOWEST)
 
 
 def _to_pages(x, c, table):
