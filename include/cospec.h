@@ -20,7 +20,9 @@
  *
  * This library computes that step on the GPU from logits, draft tokens,
  * arbitrator hidden states and head weights, and returns accept lengths and the
- * emitted tokens, plus optional per-row and per-decision features.
+ * emitted tokens, plus optional per-row and per-decision features.  The attentions around
+ * it (the arbitrator's, and a token tree's under the target model) and the paged cache
+ * they read follow after it.
  *
  * Conventions shared by every entry point
  *  - Array arguments are DEVICE pointers on the current HIP device, owned by the
@@ -73,7 +75,12 @@ typedef enum {
 /* Bytes of the library's static scratch buffer (per GPU), see cospec_verify_block_static. */
 #define COSPEC_STATIC_SCRATCH_BYTES (64u << 20)
 
-typedef enum { COSPEC_F32 = 0, COSPEC_BF16 = 1 } cospec_dtype;
+typedef enum {
+    COSPEC_F32 = 0,
+    COSPEC_BF16 = 1,
+    COSPEC_F8E4M3 = 2 /* 8 bits: 1 sign, 4 exponent, 3 mantissa bits, no infinity; pages of a
+                         cospec_cache only */
+} cospec_dtype;
 
 /*
  * Arbitration head g_phi (Section 3.3).  The paper gives it no explicit form
@@ -448,6 +455,131 @@ cospec_status cospec_hybrid_attention_ws(const void *q, const void *k, const voi
                                          const int32_t *q_start, int32_t B, int32_t n_q, int32_t L, int32_t Hq,
                                          int32_t Hkv, int32_t D, int32_t K, float scale, void *out,
                                          void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Paged key/value cache of one attention layer, for the arbitrator's attention and for a
+ * target model that verifies token trees.  Positions 0, 1, ... of sequence b are kept in pages of
+ * `page` positions: position p in place p % page of page table[b][p / page], so a sequence
+ * has room for max_pages * page positions.
+ *  dtype      COSPEC_BF16 or COSPEC_F8E4M3.
+ *  page       16, 32, 64 or 128;  d 64 or 128;  heads >= 1 key/value heads.
+ *  k          [n_pages][heads][page][d]: a head's keys, one row per position.
+ *  v          [n_pages][heads][d][page]: a head's values, one row per component (both
+ *             attention products then read a page's memory in the order they need).
+ *             16-byte aligned, as k.
+ *  k_scale,   [n_pages][heads] f32, COSPEC_F8E4M3 only (else ignored): element x of a page
+ *  v_scale    and head stands for x * scale.  Scales are powers of two (the mantissa bits
+ *             are ignored); cospec_cache_append and cospec_cache_keep set them.
+ *  table      [B][max_pages] int32.  An entry outside [0, n_pages) is no page: nothing is
+ *             written there and its positions are not attended.  Entries of pages past a
+ *             sequence's positions are not used.
+ * Sequences may share pages that are only read; a page that a call writes must belong to
+ * one sequence (two sequences writing one page leave unspecified values in it).
+ */
+typedef struct {
+    cospec_dtype dtype;
+    int32_t page;
+    int32_t heads;
+    int32_t d;
+    int64_t n_pages;
+    void *k;
+    void *v;
+    float *k_scale;
+    float *v_scale;
+    const int32_t *table;
+    int32_t max_pages;
+} cospec_cache;
+
+/*
+ * Rotary position embedding: components x1, x2 of a pair become x1 cos a - x2 sin a and
+ * x2 cos a + x1 sin a, a = position * inv_freq[pair].  The first `rot` components are
+ * rotated (a multiple of 16, at most d; 0: none), in pairs (i, i + rot / 2), or (2i, 2i + 1)
+ * when `interleaved` is not 0.  inv_freq [rot / 2] f32 on the device.  The angle is reduced in
+ * double precision, so far positions lose nothing; one rounding, to the stored type.
+ */
+typedef struct {
+    int32_t rot;
+    int32_t interleaved;
+    const float *inv_freq;
+} cospec_rope;
+
+/*
+ * Appends new positions to the cache: token i < count[b] of sequence b goes to position
+ * start[b] + i, its key rotated.  Places it does not write keep what they hold.  Positions
+ * written before are overwritten (a round's rejected tokens need no removal).
+ *  start, count  [B] int32; count NULL: n everywhere (values are clamped to [0, n]).
+ *                Positions outside [0, max_pages * page) or on no page are not written.
+ *  k, v          bf16: token i of sequence b at element (b * n + i) * ld, [heads][d] there
+ *                (so slices of one projection's output are taken as they are); ld_k, ld_v
+ *                multiples of 8, at least heads * d.
+ *  rope          NULL: no rotation.
+ *  positions     [B][n] int32, the position each token is rotated to; NULL: start[b] + i.
+ *                (The nodes of a token tree are kept one after the other and rotated to
+ *                their depth.)
+ *  q, ld_q, Hq   queries of the same tokens to rotate to q_out, or q NULL: bf16, laid out as k
+ *                with Hq heads; q_out [B][n][Hq][d] bf16.  All n tokens, whatever count says.
+ * COSPEC_F8E4M3: the scale of a page and head becomes the smallest power of two s (at least
+ * 2^-100) with |x| <= 448 s for the finite new values x that go there, but not below its
+ * present scale when the page holds earlier positions of the sequence (start[b] is not the
+ * page's first): then it only grows, and the earlier values are rounded anew (exactly, unless
+ * they become subnormal).  Rounding is to nearest even; infinities and NaN become NaN.
+ */
+cospec_status cospec_cache_append(const cospec_cache *cache, const int32_t *start, const int32_t *count,
+                                  const void *k, int64_t ld_k, const void *v, int64_t ld_v,
+                                  const cospec_rope *rope, const int32_t *positions, int32_t B, int32_t n,
+                                  const void *q, int64_t ld_q, int32_t Hq, void *q_out, hipStream_t stream);
+
+/*
+ * Keeps the accepted path of each sequence's token tree, whose N nodes were appended at
+ * positions ctx_len[b] .. ctx_len[b] + N - 1: node path[b][i] moves to position
+ * ctx_len[b] + i.  With path the out_path of cospec_verify_tree, the first accept_len[b]
+ * positions from ctx_len[b] then hold the path (the root first), and ctx_len may be advanced by
+ * accept_len.
+ *  path  [B][N] int32, increasing node ids (so path[i] >= i); the first entry outside
+ *        [0, N) ends it.  1 <= N <= COSPEC_MAX_N.  ctx_len [B] int32 (negative values act as 0).
+ * Positions past the path keep their bytes.  COSPEC_F8E4M3: the scale of a page that a node
+ * moves into becomes the largest scale of the pages its nodes come from, and of its own
+ * when it holds positions before ctx_len[b]; what it holds is rounded anew as by
+ * cospec_cache_append, and what stands past the path there is then unspecified.  Not
+ * increasing paths give unspecified values at the path's positions.
+ */
+cospec_status cospec_cache_keep(const cospec_cache *cache, const int32_t *ctx_len, const int32_t *path, int32_t B,
+                                int32_t N, hipStream_t stream);
+
+/*
+ * cospec_hybrid_attention over the cache: the same mask, for the positions the cache holds
+ * (l = l_c + 2K + 3, at most max_pages * page).  Positions [0, l) that a query may see must hold
+ * finite keys and values; what stands past them is not used.  With n_q = 1, q_start = l_c - 1
+ * this is plain decoding of the last of l_c positions.
+ *  q    [B][n_q][Hq][d] bf16; Hq a multiple of cache->heads; out the same shape.  A query
+ *       outside [0, l), or that sees only positions on no page, gets zeros.
+ * fp32 sums; the attention weights enter the second product rounded to bf16; e4m3 keys and
+ * values times their scale are taken exactly.
+ *  workspace  256-byte aligned, at least cospec_paged_attention_workspace_size(cache, B, n_q,
+ *             Hq) bytes (0: none is needed, and NULL will do): few query groups are
+ *             cut into pieces of their keys, by each sequence's own length, and merged by
+ *             a second kernel.
+ */
+size_t cospec_paged_attention_workspace_size(const cospec_cache *cache, int32_t B, int32_t n_q, int32_t Hq);
+
+cospec_status cospec_hybrid_attention_paged(const void *q, const cospec_cache *cache, const int32_t *ctx_len,
+                                            const int32_t *q_start, int32_t B, int32_t n_q, int32_t Hq, int32_t K,
+                                            float scale, void *out, void *workspace, size_t workspace_bytes,
+                                            hipStream_t stream);
+
+/*
+ * Attention of the nodes of token trees, as a target model needs it to score a tree for
+ * cospec_verify_tree: node n of sequence b, kept at position ctx_len[b] + n, sees positions
+ * [0, ctx_len[b]) and, among the nodes, itself and its ancestors.
+ *  parent   [B][N] int32 as in cospec_verify_tree; a node whose parent breaks
+ *           0 <= parent[n] < n has no ancestors (node 0 always).
+ *  q, out   [B][N][Hq][d] bf16.  1 <= N <= COSPEC_MAX_N.
+ * A node past the cache's room gets zeros.  Otherwise as cospec_hybrid_attention_paged, the
+ * workspace with n_q = N.
+ */
+cospec_status cospec_tree_attention(const void *q, const cospec_cache *cache, const int32_t *ctx_len,
+                                    const int32_t *parent, int32_t B, int32_t N, int32_t Hq, float scale, void *out,
+                                    void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
  * How a whole step of these sizes runs its head's first layer (n: draft tokens K of a chain,

@@ -17,11 +17,13 @@ from . import _build
 
 __all__ = ["lib", "verify_block", "verify_block_static", "verify_tree", "arbitrate", "CospecError", "Prepared",
            "prepare_block", "prepare_tree", "prepare_sps", "SplitBlock", "sps_block", "hybrid_mask",
-           "hybrid_attention", "status_string", "MAX_K",
+           "hybrid_attention", "PagedCache", "CacheCall", "prepare_cache_append", "cache_append",
+           "prepare_cache_keep", "cache_keep", "prepare_hybrid_attention_paged", "hybrid_attention_paged",
+           "prepare_tree_attention", "tree_attention", "status_string", "MAX_K",
            "MAX_N", "MAX_SPLITS"]
 
 MAX_K, MAX_N, MAX_SPLITS = 64, 256, 64
-_F32, _BF16 = 0, 1
+_F32, _BF16, _F8E4M3 = 0, 1, 2
 _lib = None
 
 
@@ -59,6 +61,17 @@ class _Options(ctypes.Structure):
                 ("sample_uniform", ctypes.c_void_p), ("policy_uniform", ctypes.c_void_p),
                 ("rl", ctypes.POINTER(_RL)), ("hidden_row0", ctypes.c_void_p),
                 ("hidden_rows", ctypes.c_int64)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("page", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("n_pages", ctypes.c_int64), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("table", ctypes.c_void_p), ("max_pages", ctypes.c_int32)]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("inv_freq", ctypes.c_void_p)]
 
 
 def _event_handle(ev) -> int:
@@ -134,6 +147,18 @@ def lib():
         L.cospec_head_tile_groups.argtypes = [I32, I32, I32, I32, I32, HP]
         L.cospec_arbitrate.restype = I32
         L.cospec_arbitrate.argtypes = [P, I64, P, I64, HP, ctypes.c_float, P, P, P, SZ, P]
+        CP = ctypes.POINTER(_Cache)
+        L.cospec_cache_append.restype = I32
+        L.cospec_cache_append.argtypes = [CP, P, P, P, I64, P, I64, ctypes.POINTER(_Rope), P, I32, I32, P, I64, I32,
+                                          P, P]
+        L.cospec_cache_keep.restype = I32
+        L.cospec_cache_keep.argtypes = [CP, P, P, I32, I32, P]
+        L.cospec_paged_attention_workspace_size.restype = SZ
+        L.cospec_paged_attention_workspace_size.argtypes = [CP, I32, I32, I32]
+        L.cospec_hybrid_attention_paged.restype = I32
+        L.cospec_hybrid_attention_paged.argtypes = [P, CP, P, P, I32, I32, I32, I32, ctypes.c_float, P, P, SZ, P]
+        L.cospec_tree_attention.restype = I32
+        L.cospec_tree_attention.argtypes = [P, CP, P, P, I32, I32, I32, ctypes.c_float, P, P, SZ, P]
         _lib = L
     return _lib
 
@@ -611,3 +636,217 @@ def hybrid_attention(q, k, v, ctx_len, q_start, K: int, scale: float) -> torch.T
                                          D, int(K), float(scale), _ptr(out), _ptr(ws), ws_bytes, _stream())
     _check(code, "cospec_hybrid_attention")
     return out
+
+
+class PagedCache:
+    """Pages of keys and values of one attention layer (cospec_cache): k [n_pages, heads, page, d]
+    and v [n_pages, heads, d, page], both bf16, or both float8_e4m3fn with f32 scales
+    [n_pages, heads] (powers of two).  page is 16, 32, 64 or 128, d 64 or 128."""
+
+    def __init__(self, k, v, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
+        if k.dim() != 4 or v.dim() != 4:
+            raise ValueError("k must be [n_pages, heads, page, d] and v [n_pages, heads, d, page]")
+        n, heads, page, d = k.shape
+        if tuple(v.shape) != (n, heads, d, page) or v.dtype != k.dtype:
+            raise ValueError("v must be [n_pages, heads, d, page], of k's type")
+        if k.dtype == torch.float8_e4m3fn:
+            self.dtype = _F8E4M3
+            for t in (k_scale, v_scale):
+                if t is None or tuple(t.shape) != (n, heads) or t.dtype != torch.float32:
+                    raise ValueError("float8_e4m3fn pages need float32 scales [n_pages, heads]")
+        elif k.dtype == torch.bfloat16:
+            self.dtype = _BF16
+            if k_scale is not None or v_scale is not None:
+                raise ValueError("bf16 pages have no scales")
+        else:
+            raise TypeError(f"pages are bf16 or float8_e4m3fn, got {k.dtype}")
+        for t in (k, v, k_scale, v_scale):
+            if t is not None and (not t.is_cuda or not t.is_contiguous() or t.device != k.device):
+                raise ValueError("pages and scales must be contiguous tensors of one device")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.heads, self.page, self.d = int(n), int(heads), int(page), int(d)
+
+    @classmethod
+    def empty(cls, n_pages: int, heads: int, d: int, page: int = 64, dtype: torch.dtype = torch.bfloat16,
+              device="cuda") -> "PagedCache":
+        """A cache with nothing in it (its memory is not cleared: every place is written before
+        it is read)."""
+        k = torch.empty((n_pages, heads, page, d), dtype=dtype, device=device)
+        v = torch.empty((n_pages, heads, d, page), dtype=dtype, device=device)
+        scales = [None, None]
+        if dtype == torch.float8_e4m3fn:
+            scales = [torch.empty((n_pages, heads), dtype=torch.float32, device=device) for _ in range(2)]
+        return cls(k, v, *scales)
+
+    def _struct(self, table: torch.Tensor, B: int) -> _Cache:
+        if table.dim() != 2 or table.shape[0] != B or table.dtype != torch.int32 or not table.is_contiguous():
+            raise ValueError("table must be contiguous int32 [B, pages of a sequence]")
+        _same_device(self.k, table)
+        return _Cache(self.dtype, self.page, self.heads, self.d, self.n_pages, _ptr(self.k), _ptr(self.v),
+                      _ptr(self.k_scale), _ptr(self.v_scale), _ptr(table), int(table.shape[1]))
+
+
+def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]):
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("every tensor of a call must be on one device")
+
+
+def _on_current(dev: torch.device):
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+class CacheCall:
+    """Pre-marshalled arguments of one call on a paged cache: `outputs` and the workspace are
+    allocated once, so `launch()` enqueues it, on torch's current stream, with no allocation.  The
+    tensors it was prepared with are kept, and read anew by every launch."""
+
+    def __init__(self, fn, args, outputs, device, keep, workspace=None, ws_bytes=None):
+        self._fn, self._device, self._keep = fn, device, keep
+        self.outputs = outputs
+        self.workspace = workspace
+        self._args = args if ws_bytes is None else args + (_ptr(workspace), ws_bytes)
+        self._index = device.index
+        _on_current(device)
+        self._stream = _stream()                           # where the tensors allocated here are at home
+
+    def launch(self):
+        if torch.cuda.current_device() != self._index:
+            _on_current(self._device)
+        stream = _stream()
+        if stream != self._stream:
+            # used on another stream than their own: the allocator must not hand the memory out early
+            for t in (self.workspace, *self.outputs.values()):
+                if t is not None:
+                    t.record_stream(torch.cuda.current_stream())
+        code = self._fn(*self._args, stream)
+        if code:
+            _check(code, self._fn.__name__)
+
+    def result(self):
+        return self.outputs
+
+
+def _tokens(t: torch.Tensor, B: int, n: int, d: int, what: str) -> int:
+    """Distance in elements between tokens of a [B, n, heads, d] bf16 tensor whose heads lie side
+    by side (a slice of a projection's output will do)."""
+    if t.dim() != 4 or tuple(t.shape[:2]) != (B, n) or t.shape[3] != d or t.dtype != torch.bfloat16 or not t.is_cuda:
+        raise ValueError(f"{what} must be a bf16 device tensor [B, n, heads, {d}]")
+    heads = t.shape[2]
+    if t.stride(3) != 1 or (heads > 1 and t.stride(2) != d):
+        raise ValueError(f"the heads of a token of {what} must lie side by side")
+    if B * n <= 1:
+        return max(heads * d, 8)
+    ld = t.stride(1) if n > 1 else t.stride(0)
+    if B > 1 and n > 1 and t.stride(0) != n * ld:
+        raise ValueError(f"the tokens of {what} must be evenly spaced: stride(0) == n * stride(1)")
+    return int(ld)
+
+
+def prepare_cache_append(cache: PagedCache, table, start, k, v, count: Optional[torch.Tensor] = None,
+                         inv_freq: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                         interleaved: bool = False, q: Optional[torch.Tensor] = None) -> CacheCall:
+    """Pre-marshalled cospec_cache_append: tokens k, v [B, n, heads, d] go to positions start[b] ..
+    start[b] + count[b] - 1 (int32 [B]; count None: n), keys rotated with inv_freq (f32
+    [rot / 2]; None: not rotated) to positions (int32 [B, n]; None: where they go).  q
+    [B, n, Hq, d]: queries to rotate as well, into outputs["q"]."""
+    if k.dim() != 4:
+        raise ValueError("k must be [B, n, heads, d]")
+    B, n = int(k.shape[0]), int(k.shape[1])
+    ld_k, ld_v = _tokens(k, B, n, cache.d, "k"), _tokens(v, B, n, cache.d, "v")
+    if k.shape[2] != cache.heads or v.shape[2] != cache.heads:
+        raise ValueError(f"k and v must have the cache's {cache.heads} heads")
+    cs = cache._struct(table, B)
+    start = _i32(start, B, "start")
+    if count is not None:
+        count = _i32(count, B, "count")
+    if positions is not None and (tuple(positions.shape) != (B, n) or positions.dtype != torch.int32
+                                  or not positions.is_contiguous()):
+        raise ValueError("positions must be contiguous int32 [B, n]")
+    rope = None
+    if inv_freq is not None:
+        if inv_freq.dim() != 1 or inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be contiguous float32 [rot / 2]")
+        rope = _Rope(2 * int(inv_freq.shape[0]), int(bool(interleaved)), _ptr(inv_freq))
+    ld_q, Hq, out = 0, 0, None
+    if q is not None:
+        ld_q, Hq = _tokens(q, B, n, cache.d, "q"), int(q.shape[2])
+        out = torch.empty((B, n, Hq, cache.d), dtype=torch.bfloat16, device=k.device)
+    _same_device(cache.k, k, v, start, count, positions, inv_freq, q)
+    args = (ctypes.byref(cs), _ptr(start), _ptr(count), _ptr(k), ld_k, _ptr(v), ld_v,
+            None if rope is None else ctypes.byref(rope), _ptr(positions), B, n, _ptr(q), ld_q, Hq, _ptr(out))
+    return CacheCall(lib().cospec_cache_append, args, {} if out is None else dict(q=out), cache.k.device,
+                     [cache, table, start, count, k, v, inv_freq, positions, q, cs, rope])
+
+
+def cache_append(cache: PagedCache, table, start, k, v, count: Optional[torch.Tensor] = None,
+                 inv_freq: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                 interleaved: bool = False, q: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """cospec_cache_append (see prepare_cache_append); returns the rotated queries, if any."""
+    p = prepare_cache_append(cache, table, start, k, v, count, inv_freq, positions, interleaved, q)
+    p.launch()
+    return p.outputs.get("q")
+
+
+def prepare_cache_keep(cache: PagedCache, table, ctx_len, path) -> CacheCall:
+    """Pre-marshalled cospec_cache_keep: the nodes path [B, N] (int32, as verify_tree returns
+    it) of each tree at positions ctx_len[b] .. move to its front."""
+    if path.dim() != 2 or path.dtype != torch.int32 or not path.is_contiguous():
+        raise ValueError("path must be contiguous int32 [B, N]")
+    B, N = int(path.shape[0]), int(path.shape[1])
+    cs = cache._struct(table, B)
+    ctx = _i32(ctx_len, B, "ctx_len")
+    _same_device(cache.k, ctx, path)
+    return CacheCall(lib().cospec_cache_keep, (ctypes.byref(cs), _ptr(ctx), _ptr(path), B, N), {}, cache.k.device,
+                     [cache, table, ctx, path, cs])
+
+
+def cache_keep(cache: PagedCache, table, ctx_len, path) -> None:
+    """cospec_cache_keep (see prepare_cache_keep)."""
+    prepare_cache_keep(cache, table, ctx_len, path).launch()
+
+
+def _attention_call(fn, q, cache, table, ctx_len, more, K, scale) -> CacheCall:
+    if q.dim() != 4 or q.shape[3] != cache.d or q.dtype != torch.bfloat16 or not q.is_contiguous():
+        raise ValueError(f"q must be contiguous bf16 [B, n, Hq, {cache.d}]")
+    B, n, Hq = int(q.shape[0]), int(q.shape[1]), int(q.shape[2])
+    cs = cache._struct(table, B)
+    ctx = _i32(ctx_len, B, "ctx_len")
+    _same_device(cache.k, q, ctx, more)
+    out = torch.empty_like(q)
+    ws_bytes = lib().cospec_paged_attention_workspace_size(ctypes.byref(cs), B, n, Hq)
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device) if ws_bytes else None
+    args = (_ptr(q), ctypes.byref(cs), _ptr(ctx), _ptr(more), B, n, Hq) + K + (float(scale), _ptr(out))
+    return CacheCall(fn, args, dict(out=out), q.device, [q, cache, table, ctx, more, cs], ws, ws_bytes)
+
+
+def prepare_hybrid_attention_paged(q, cache: PagedCache, table, ctx_len, q_start, K: int, scale: float) -> CacheCall:
+    """Pre-marshalled cospec_hybrid_attention_paged: q [B, n_q, Hq, d] (bf16, contiguous) at positions
+    q_start[b] .. q_start[b] + n_q - 1 against the cache, under the arbitrator's hybrid mask;
+    outputs["out"] has q's shape."""
+    return _attention_call(lib().cospec_hybrid_attention_paged, q, cache, table, ctx_len,
+                           _i32(q_start, int(q.shape[0]), "q_start"), (int(K),), scale)
+
+
+def hybrid_attention_paged(q, cache: PagedCache, table, ctx_len, q_start, K: int, scale: float) -> torch.Tensor:
+    """cospec_hybrid_attention_paged (see prepare_hybrid_attention_paged) -> [B, n_q, Hq, d] bf16."""
+    p = prepare_hybrid_attention_paged(q, cache, table, ctx_len, q_start, K, scale)
+    p.launch()
+    return p.outputs["out"]
+
+
+def prepare_tree_attention(q, cache: PagedCache, table, ctx_len, parent, scale: float) -> CacheCall:
+    """Pre-marshalled cospec_tree_attention: q [B, N, Hq, d] (bf16, contiguous) of the nodes kept at
+    positions ctx_len[b] .. ctx_len[b] + N - 1, parent [B, N] as verify_tree takes it;
+    outputs["out"] has q's shape."""
+    if tuple(parent.shape) != tuple(q.shape[:2]) or parent.dtype != torch.int32 or not parent.is_contiguous():
+        raise ValueError("parent must be contiguous int32 [B, N]")
+    return _attention_call(lib().cospec_tree_attention, q, cache, table, ctx_len, parent, (), scale)
+
+
+def tree_attention(q, cache: PagedCache, table, ctx_len, parent, scale: float) -> torch.Tensor:
+    """cospec_tree_attention (see prepare_tree_attention) -> [B, N, Hq, d] bf16."""
+    p = prepare_tree_attention(q, cache, table, ctx_len, parent, scale)
+    p.launch()
+    return p.outputs["out"]

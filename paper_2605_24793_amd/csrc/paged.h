@@ -1,0 +1,74 @@
+// The paged key/value cache (cospec_cache): arguments of its kernels and what they share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "launch.h"
+
+namespace cospec {
+
+// Keys [n_pages][H][P][D], values [n_pages][H][D][P], P = 1 << log_page.
+struct PageArgs {
+    char *k, *v;
+    float *k_scale, *v_scale;  // [n_pages][H], 8-bit pages only
+    const int32_t *table;      // [B][max_pages]
+    int64_t n_pages;
+    int32_t max_pages, log_page, H, D, f8;
+};
+
+struct AppendArgs {
+    PageArgs c;
+    const int32_t *start, *count, *positions;
+    const char *k, *v, *q;     // bf16
+    int64_t ld_k, ld_v, ld_q;  // elements
+    const float *inv_freq;
+    int32_t rot, interleaved, B, n, Hq;
+    char *q_out;
+    // set by the launch: page workgroups ahead of the query ones, and their divisions
+    uint32_t page_wgs;
+    FastDiv by_pages, by_heads, by_n;
+};
+
+struct KeepArgs {
+    PageArgs c;
+    const int32_t *ctx_len, *path;
+    int32_t B, N;
+    FastDiv by_heads;
+};
+
+// Queries of a hybrid call (q_start, K) or of tree nodes (parent, n_q = N).
+struct PagedArgs {
+    PageArgs c;
+    const void *q;
+    const int32_t *ctx_len, *q_start, *parent;
+    int32_t B, n_q, Hq, K;
+    float scale;
+    void *out;
+    // keys cut into at most `splits` pieces: unnormalised sums [splits][rows][D] and {running
+    // max, weight sum} [splits][rows], rows = B * n_q * Hq
+    int32_t splits;
+    float *part_o;
+    float2 *part_ml;
+    // set by the launch
+    int32_t row_tiles;         // 16-row tiles of a workgroup
+    FastDiv by_grp, by_blocks, by_heads, by_splits, by_seq_rows, by_hq;
+};
+
+struct PagedPlan {
+    int32_t row_tiles, blocks, splits;   // blocks: workgroups that share a group's rows
+    int64_t rows;                        // B * n_q * Hq
+};
+
+PagedPlan paged_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq);
+hipError_t launch_cache_append(AppendArgs a, hipStream_t s);
+hipError_t launch_cache_keep(KeepArgs a, hipStream_t s);
+hipError_t launch_paged_attention(PagedArgs a, const PagedPlan &p, hipStream_t s);
+
+// The page a table entry names, or -1.
+__device__ inline int64_t page_or_none(const PageArgs &c, int32_t id) {
+    return id >= 0 && id < c.n_pages ? id : -1;
+}
+
+}  // namespace cospec

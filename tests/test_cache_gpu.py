@@ -1,0 +1,572 @@
+"""The paged key/value cache and its attentions on the GPU against plain 64-bit
+implementations (tests/cache_reference.py)."""
+import math
+
+import pytest
+import torch
+
+import cache_reference as ref
+import paper_2605_24793_amd as cs
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+F8, BF16 = torch.float8_e4m3fn, torch.bfloat16
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def _filled(table, n_pages, H, D, P, dtype, lengths, seed, junk=True):
+    """A cache whose sequences hold `lengths[b]` random positions; every other place, and the
+    scales of unused pages, hold NaN (`junk`) or zeros."""
+    g = _gen(seed)
+    k = torch.randn(n_pages, H, P, D, generator=g)
+    v = torch.randn(n_pages, H, P, D, generator=g)
+    live = torch.zeros(n_pages, P, dtype=torch.bool)
+    for b, length in enumerate(lengths):
+        for p in range(length):
+            pid = int(table[b, p // P])
+            if 0 <= pid < n_pages:
+                live[pid, p % P] = True
+    scales = [None, None]
+    if dtype == F8:
+        # |x| < 6 here: 448 * 2^-6 holds it
+        scales = [2.0 ** torch.randint(-6, -2, (n_pages, H), generator=g).float() for _ in range(2)]
+        k, v = k / scales[0][:, :, None, None], v / scales[1][:, :, None, None]
+        scales = [torch.where(live.any(1)[:, None], s, math.nan if junk else 1.0) for s in scales]
+    dead = ~live[:, None, :, None]
+    k, v = (x.masked_fill(dead, math.nan if junk else 0.0).to(dtype) for x in (k, v))
+    dev = [k.to(DEV), v.transpose(2, 3).contiguous().to(DEV)] + [None if s is None else s.to(DEV) for s in scales]
+    return cs.PagedCache(*dev)
+
+
+def _host(cache):
+    return ref.Pages(cache.k, cache.v, cache.k_scale, cache.v_scale)
+
+
+def _bits(x):
+    return x.contiguous().view(torch.uint8)
+
+
+def _same(a, b):
+    """The same bits, but that e4m3 has two codes for NaN, which differ in the sign."""
+    x, y = _bits(a), _bits(b)
+    if a.dtype == F8:
+        x, y = (torch.where((t & 127) == 127, 127, t) for t in (x, y))
+    return bool((x == y).all())
+
+
+# ------------------------------------------------------------------------------- append
+
+def _check_append(dtype, D, P, H, n, start, count=None, rot=None, interleaved=False, Hq=0, positions=None, seed=0,
+                  T=None, strided=False, size=1.0, table=None, special=None):
+    B = len(start)
+    g = _gen(seed)
+    T = T or (max(max(start), 0) + n + P - 1) // P
+    if table is None:
+        table, n_pages = ref.make_table(B, T, seed)
+    else:
+        n_pages = int(table.max()) + 3
+    cache = _filled(table, n_pages, H, D, P, dtype, [min(max(s, 0), T * P) for s in start], seed, junk=False)
+    heads = Hq + 2 * H
+    wide = torch.randn(B, n, heads * D + (24 if strided else 0), generator=g) * size
+    wide = wide.to(BF16)
+    if special:
+        special(wide)
+    dev = wide.to(DEV)
+    at = [0, Hq * D, (Hq + H) * D, heads * D]
+    parts = [wide[:, :, at[i]:at[i + 1]].reshape(B, n, -1, D) for i in range(3)]
+    views = [dev[:, :, at[i]:at[i + 1]].unflatten(2, ((at[i + 1] - at[i]) // D, D)) if at[i + 1] > at[i] else None
+             for i in range(3)]
+    rot = D if rot is None else rot
+    inv_freq = (10000.0 ** (-torch.arange(0, rot, 2).double() / rot)).float() if rot else None
+    i32 = lambda x: None if x is None else torch.tensor(x, dtype=torch.int32)  # noqa: E731
+    pos, cnt = i32(positions), i32(count)
+    host = _host(cache)
+    before = _host(cache)
+    news = ref.append(host, table, start, parts[1], parts[2], count, inv_freq, pos, interleaved)
+    on = lambda t: None if t is None else t.to(DEV)  # noqa: E731
+    got_q = cs.cache_append(cache, on(table), on(i32(start)), views[1], views[2], count=on(cnt), inv_freq=on(inv_freq),
+                            positions=on(pos), interleaved=interleaved, q=views[0])
+    torch.cuda.synchronize()
+    got = _host(cache)
+    for side in ("k", "v"):
+        if dtype == F8:
+            assert torch.equal(got.scale[side], host.scale[side]), side
+        want = host.raw[side].clone()
+        for pid, place, x in news[side]:
+            # the largest pair bounds the rotation's fp32 error (three roundings and the angle's)
+            fp32 = 2.0 ** -21 * float(x[torch.isfinite(x)].abs().max()) if torch.isfinite(x).any() else 0.0
+            y = got.raw[side][pid, :, place].double()
+            s = host.scale[side][pid].double()[:, None] if dtype == F8 else torch.ones(H, 1, dtype=torch.float64)
+            real = torch.isfinite(x)
+            if dtype == F8:
+                assert torch.isnan(y[~real]).all()
+                # half a step of e4m3: relative 2^-4, or 2^-10 among the subnormals
+                tol = torch.maximum(2.0 ** -4 * x.abs(), 2.0 ** -10 * s) + fp32
+            else:
+                tol = 2.0 ** -8 * x.abs() + fp32
+                assert torch.equal(torch.isnan(y[~real]), torch.isnan(x[~real]))
+            assert ((y * s - x).abs() <= tol)[real].all(), (side, pid, place)
+            want[pid, :, place] = got.raw[side][pid, :, place]
+        # nothing else has changed, but for the earlier values of pages whose scale grew
+        assert _same(got.raw[side], want), side
+    if Hq:
+        p0 = torch.tensor(start)[:, None] + torch.arange(n) if pos is None else pos
+        for b in range(B):
+            for i in range(n):
+                x = ref.rotate(parts[0][b, i], int(p0[b, i]), inv_freq, interleaved) if rot else parts[0][b, i].double()
+                tol = 2.0 ** -8 * x.abs() + 2.0 ** -21 * float(x.abs().max())
+                assert ((got_q[b, i].cpu().double() - x).abs() <= tol).all()
+    return before, got
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("D,P,H,n,start", [
+    (128, 64, 2, 1, [0]), (128, 64, 2, 1, [63, 64, 65]), (64, 16, 3, 5, [14, 0, 16]), (128, 128, 1, 130, [126, 7]),
+    (64, 32, 2, 37, [31, 95]), (128, 16, 2, 70, [3, 33]),
+])
+def test_append(dtype, D, P, H, n, start):
+    _check_append(dtype, D, P, H, n, start, Hq=2 * H, seed=n)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("rot,interleaved", [(0, False), (16, False), (32, True), (64, True), (48, False)])
+def test_append_rotations(dtype, rot, interleaved):
+    _check_append(dtype, 64, 32, 2, 9, [29, 4], rot=rot, interleaved=interleaved, Hq=3, strided=True, seed=rot)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+def test_append_positions_and_counts(dtype):
+    # tree nodes rotated to their depth, far positions, counts of nothing, too many, too few
+    n, start = 6, [10, 61, 0, 5, 40]
+    positions = [[s + 1000003 + (i + 1) // 2 for i in range(n)] for s in start]
+    _check_append(dtype, 128, 64, 2, n, start, count=[0, 6, 99, -4, 3], positions=positions, Hq=2, T=2)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+def test_append_outside_the_room(dtype):
+    # before position 0, past the table, on entries that name no page
+    table = torch.tensor([[4, 1], [-1, 6], [2, 9], [7, 3]], dtype=torch.int32)
+    table[2, 1] = 10 ** 9
+    n_pages_table = table.clone()
+    cache_pages = 12
+    B, H, D, P, n = 4, 2, 64, 16, 20
+    start = [-7, 10, 10, 30]
+    safe = torch.where((table < 0) | (table >= cache_pages), torch.full_like(table, -1), table)
+    cache = _filled(safe, cache_pages, H, D, P, dtype, [0, 10, 10, 30], 3, junk=False)
+    g = _gen(5)
+    k, v = (torch.randn(B, n, H, D, generator=g).to(BF16) for _ in range(2))
+    host = _host(cache)
+    news = ref.append(host, n_pages_table, start, k, v, None, None, None, False)
+    cs.cache_append(cache, table.to(DEV), torch.tensor(start, dtype=torch.int32, device=DEV), k.to(DEV), v.to(DEV))
+    torch.cuda.synchronize()
+    got = _host(cache)
+    # 13 of the first (seven lie before position 0), 14 on the second's real page, 6 on the third's, 2 of the last
+    assert len(news["k"]) == 13 + 14 + 6 + 2
+    for side in ("k", "v"):
+        want = host.raw[side].clone()
+        for pid, place, x in news[side]:
+            want[pid, :, place] = got.raw[side][pid, :, place]
+            s = host.scale[side][pid].double()[:, None] if dtype == F8 else 1.0
+            assert ((got.raw[side][pid, :, place].double() * s - x).abs() <= 2.0 ** -4 * x.abs() + 2.0 ** -10).all()
+        assert _same(got.raw[side], want)
+
+
+@pytest.mark.parametrize("size", [300.0, 1e-3, 3e38, 1e-36])
+def test_append_scales_grow_and_keep(size):
+    # far larger values: earlier ones are rounded anew; far smaller ones: the scale stays
+    _check_append(F8, 128, 64, 2, 3, [40, 62, 0], rot=0, size=size, seed=7)
+
+
+def test_append_values_without_a_number():
+    def special(x):
+        x[0, 0, 3], x[0, 1, 200], x[1, 2, 70] = math.inf, math.nan, -math.inf
+        x[1, 0] = 0.0
+    for dtype in (F8, BF16):
+        _check_append(dtype, 64, 32, 2, 3, [5, 31], rot=0, special=special)
+
+
+def test_append_after_values_without_a_number():
+    """Earlier values of a page whose scale grows: NaN stays NaN, the others are rounded anew."""
+    table, n_pages = ref.make_table(1, 1, 1)
+    cache = _filled(table, n_pages, 2, 64, 32, F8, [20], 1, junk=False)
+    for x in (cache.k, cache.v):
+        _bits(x)[:, :, 3:9] |= 127
+    k, v = (torch.randn(1, 2, 2, 64, generator=_gen(i)).mul(1000).to(BF16) for i in range(2))
+    host = _host(cache)
+    news = ref.append(host, table, [20], k, v, None, None, None, False)
+    cs.cache_append(cache, table.to(DEV), torch.tensor([20], dtype=torch.int32, device=DEV), k.to(DEV), v.to(DEV))
+    torch.cuda.synchronize()
+    got = _host(cache)
+    pid = int(table[0, 0])
+    for side in ("k", "v"):
+        assert len(news[side]) == 2 and bool(torch.isnan(host.raw[side][pid, :, :20].float()).any())
+        assert _same(got.raw[side][pid, :, :20], host.raw[side][pid, :, :20])
+
+
+def test_append_again_changes_nothing_more():
+    table, n_pages = ref.make_table(2, 2, 1)
+    cache = _filled(table, n_pages, 2, 128, 64, F8, [50, 3], 1, junk=False)
+    g = _gen(2)
+    k, v = (torch.randn(2, 20, 2, 128, generator=g).to(BF16).to(DEV) for _ in range(2))
+    call = cs.prepare_cache_append(cache, table.to(DEV), torch.tensor([50, 3], dtype=torch.int32, device=DEV), k, v)
+    call.launch()
+    once = [t.clone() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale)]
+    call.launch()
+    for a, b in zip(once, (cache.k, cache.v, cache.k_scale, cache.v_scale)):
+        assert _same(a, b)
+
+
+# ----------------------------------------------------------------------------- attention
+
+def _tolerance(out, size):
+    # a weight enters the second product off by at most half a bf16 step (2^-8 of it), the
+    # result is stored off by at most 2^-8 of it; scores in fp32: D + 4 roundings of at most
+    # sum |q k| scale < 20, twice (numerator and denominator), below 4e-4
+    return (2.0 ** -8 + 4e-4) * size + 2.0 ** -8 * out.abs() + 1e-30
+
+
+def _check_rows(got, out, size):
+    err = (got.double().cpu() - out).abs()
+    worst = float((err / _tolerance(out, size)).max()) if err.numel() else 0.0
+    print(f"worst error {worst:.3f} of the tolerance", flush=True)
+    assert not torch.isnan(got.float()).any()
+    assert (err <= _tolerance(out, size)).all()
+
+
+def _check_hybrid(dtype, D, P, Hq, H, ctx, q_start, n_q, K, T=None, scale=None, seed=0, spoil=None):
+    B = len(ctx)
+    need = max(max(c, 0) for c in ctx) + 2 * K + 3
+    T = T or (need + P - 1) // P
+    table, n_pages = ref.make_table(B, T, seed)
+    room = T * P
+    lengths = [min(max(c, 0) + 2 * K + 3, room) for c in ctx]
+    if spoil:
+        spoil(table)
+    cache = _filled(table, n_pages, H, D, P, dtype, lengths, seed)
+    g = _gen(seed + 1)
+    q = torch.randn(B, n_q, Hq, D, generator=g).to(BF16)
+    scale = D ** -0.5 if scale is None else scale
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    got = cs.hybrid_attention_paged(q.to(DEV), cache, table.to(DEV), i32(ctx), i32(q_start), K, scale)
+    torch.cuda.synchronize()
+    host = _host(cache)
+    for b in range(B):
+        sees = torch.tensor(ref.hybrid_sees(ctx[b], q_start[b], n_q, K, room))
+        mask = torch.arange(lengths[b]) < sees[:, None]
+        out, size = ref.attention(q[b], host.of("k", table[b], lengths[b]), host.of("v", table[b], lengths[b]), mask,
+                                  scale)
+        _check_rows(got[b], out, size)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("D,P,Hq,H,ctx,n_q,K", [
+    (128, 64, 8, 2, [100, 61, 0], 9, 3),          # the region's queries
+    (64, 16, 6, 2, [1, 15, 33], 3, 0),            # groups of three heads
+    (128, 16, 4, 4, [250, 777], 17, 7),           # one head a group
+    (128, 128, 14, 2, [130, 5], 5, 1),            # groups of seven
+    (64, 32, 16, 2, [64, 200], 13, 5),            # 104 rows a group
+    (128, 32, 8, 1, [40, 321], 23, 10),           # 184 rows
+])
+def test_hybrid_region(dtype, D, P, Hq, H, ctx, n_q, K):
+    _check_hybrid(dtype, D, P, Hq, H, ctx, ctx, n_q, K, seed=n_q)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("D,ctx", [(128, [1, 2, 64, 65, 255, 256, 257, 1030]), (64, [63, 500, 3, 129])])
+def test_hybrid_single_token(dtype, D, ctx):
+    _check_hybrid(dtype, D, 64, 8, 2, ctx, [c - 1 for c in ctx], 1, 0, seed=ctx[0])
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("D,P", [(128, 32), (64, 128)])
+def test_hybrid_whole_input(dtype, D, P):
+    # every position, and padding rows behind the shorter sequence
+    _check_hybrid(dtype, D, P, 4, 2, [70, 23], [0, 0], 79, 3, seed=3)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+def test_hybrid_queries_outside(dtype):
+    # before position 0, across its border, past the end, a negative context, nothing at all
+    _check_hybrid(dtype, 128, 16, 4, 2, [40, 40, 40, -5, 12], [-9, -3, 45, 0, 1000], 8, 2, seed=4)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("D", [64, 128])
+def test_hybrid_padding_beside_long_rows(dtype, D):
+    # padding rows in workgroups whose other rows see whole turns of keys, cut and uncut
+    _check_hybrid(dtype, D, 32, 2, 2, [300, 150], [270, 120], 80, 4, seed=12)
+    _check_hybrid(dtype, D, 32, 1, 1, [900], [880], 90, 4, seed=13)
+
+
+def test_hybrid_room_cuts_the_input():
+    _check_hybrid(F8, 64, 16, 4, 2, [60, 64, 90], [58, 60, 55], 12, 5, T=4, seed=5)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+def test_hybrid_long_in_pieces(dtype):
+    # cut over the keys, lengths that end inside a piece, one far shorter sequence
+    _check_hybrid(dtype, 128, 64, 8, 2, [3001, 40, 2047], [3001, 40, 2047], 9, 3, seed=6)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("scale", [-0.1, 0.0, 0.9])
+def test_hybrid_scales(dtype, scale):
+    _check_hybrid(dtype, 64, 32, 4, 2, [90, 33], [90, 33], 5, 1, scale=scale, seed=7)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+def test_hybrid_entries_that_name_no_page(dtype):
+    def spoil(table):
+        table[0, 1], table[1, 0], table[2, :] = -1, 2 ** 30, -7
+    _check_hybrid(dtype, 128, 16, 4, 2, [60, 10, 30, 50], [60, 0, 30, 50], 13, 5, seed=8, spoil=spoil)
+
+
+def _check_tree(dtype, D, P, Hq, H, ctx, parent, T=None, seed=0):
+    B, N = len(ctx), len(parent[0])
+    T = T or (max(max(c, 0) for c in ctx) + N + P - 1) // P
+    table, n_pages = ref.make_table(B, T, seed)
+    room = T * P
+    lengths = [min(max(c, 0) + N, room) for c in ctx]
+    cache = _filled(table, n_pages, H, D, P, dtype, lengths, seed)
+    q = torch.randn(B, N, Hq, D, generator=_gen(seed + 1)).to(BF16)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    got = cs.tree_attention(q.to(DEV), cache, table.to(DEV), i32(ctx), i32(parent), D ** -0.5)
+    torch.cuda.synchronize()
+    host = _host(cache)
+    for b in range(B):
+        lc = max(ctx[b], 0)
+        mask = torch.zeros(N, lengths[b], dtype=torch.bool)
+        mask[:, :min(lc, room)] = True
+        inside = max(lengths[b] - lc, 0)
+        mask[:, lc:] = ref.ancestors(parent[b])[:, :inside]
+        mask[inside:] = False
+        out, size = ref.attention(q[b], host.of("k", table[b], lengths[b]), host.of("v", table[b], lengths[b]), mask,
+                                  D ** -0.5)
+        _check_rows(got[b], out, size)
+
+
+def _random_tree(N, seed, near=None):
+    g = _gen(seed)
+    return [-1] + [int(torch.randint(max(0, n - (near or n)), n, (1,), generator=g)) for n in range(1, N)]
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("D,P,Hq,H,ctx,N", [(128, 64, 8, 2, [50, 0, 333], 33), (64, 16, 3, 3, [7, 16], 60),
+                                            (128, 128, 4, 1, [700], 256), (64, 32, 8, 2, [5], 1)])
+def test_tree(dtype, D, P, Hq, H, ctx, N):
+    _check_tree(dtype, D, P, Hq, H, ctx, [_random_tree(N, b, near=6) for b in range(len(ctx))], seed=N)
+
+
+@pytest.mark.parametrize("N", [2, 65, 256])
+def test_tree_shapes(N):
+    # a path, a star, and parents that break the rule (the node itself, later ones, none)
+    bad = [n - 1 if n % 5 else (n, n + 3, -4, 10 ** 6)[n % 4] for n in range(N)]
+    _check_tree(F8, 64, 32, 4, 2, [20, 61, 90], [list(range(-1, N - 1)), [-1] + [0] * (N - 1), bad], seed=N)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+def test_tree_room_cuts_the_nodes(dtype):
+    _check_tree(dtype, 128, 16, 4, 2, [40, 48, 70], [_random_tree(20, b) for b in range(3)], T=3, seed=9)
+
+
+# ---------------------------------------------------------------------------------- keep
+
+def _check_keep(dtype, D, P, H, ctx, path, N, T=None, seed=0):
+    B = len(ctx)
+    T = T or (max(max(c, 0) for c in ctx) + N + P - 1) // P
+    table, n_pages = ref.make_table(B, T, seed)
+    cache = _filled(table, n_pages, H, D, P, dtype, [min(max(c, 0) + N, T * P) for c in ctx], seed, junk=False)
+    full = torch.tensor([p + [-1] * (N - len(p)) for p in path], dtype=torch.int32)
+    host = _host(cache)
+    ref.keep(host, table, ctx, full)
+    cs.cache_keep(cache, table.to(DEV), torch.tensor(ctx, dtype=torch.int32, device=DEV), full.to(DEV))
+    torch.cuda.synchronize()
+    got = _host(cache)
+    for side in ("k", "v"):
+        if dtype == F8:
+            assert torch.equal(got.scale[side], host.scale[side])
+        assert _same(got.raw[side], host.raw[side])
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("D,P,H,ctx,N,seed", [(128, 64, 2, [60, 0, 130], 60, 1), (64, 16, 3, [15, 16, 1], 33, 2),
+                                              (128, 32, 1, [5, 31], 256, 3), (64, 128, 2, [127], 7, 4)])
+def test_keep(dtype, D, P, H, ctx, N, seed):
+    g = _gen(seed)
+    paths = []
+    for _ in ctx:
+        s = int(torch.randint(1, N + 1, (1,), generator=g))
+        paths.append([0] + sorted((torch.randperm(N - 1, generator=g)[:s - 1] + 1).tolist()))
+    _check_keep(dtype, D, P, H, ctx, paths, N, seed=seed)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+def test_keep_nothing_everything_and_beyond(dtype):
+    # an empty path, one that stays, ends at an id too large, runs out of the room, a negative context
+    _check_keep(dtype, 64, 16, 2, [20, 20, 20, 40, -3], [[], [0, 1, 2], [0, 2, 30, 4], [0, 3, 8, 9, 19], [0, 2, 5]], 20,
+                T=3, seed=6)
+
+
+# ------------------------------------------------------------------------------ together
+
+def _round_trip(dtype, seed):
+    """A token tree under the target's attention, its accepted path kept, and the arbitrator's
+    region over the result, with the cache's contents checked against values that never were in one."""
+    B, H, Hq, D, P, N, V = 3, 2, 8, 64, 16, 13, 211
+    g = _gen(seed)
+    T = 8
+    table, n_pages = ref.make_table(B, T, seed)
+    cache = cs.PagedCache.empty(n_pages, H, D, P, dtype, DEV)
+    tab = table.to(DEV)
+    inv = (10000.0 ** (-torch.arange(0, D, 2).double() / D)).float().to(DEV)
+    draw = lambda n, h: torch.randn(B, n, h, D, generator=g).to(BF16).to(DEV)  # noqa: E731
+    ctx = torch.tensor([30, 17, 5], dtype=torch.int32, device=DEV)
+    zero = torch.zeros_like(ctx)
+    pk, pv = draw(30, H), draw(30, H)
+    cs.cache_append(cache, tab, zero, pk, pv, count=ctx, inv_freq=inv)
+    parent = torch.tensor([_random_tree(N, b, near=4) for b in range(B)], dtype=torch.int32)
+    depth = torch.zeros(B, N, dtype=torch.int32)
+    for n in range(1, N):
+        depth[:, n] = depth.gather(1, parent[:, n:n + 1].long())[:, 0] + 1
+    tk, tv, tq = draw(N, H), draw(N, H), draw(N, Hq)
+    positions = ctx[:, None] + depth.to(DEV)
+    q = cs.cache_append(cache, tab, ctx, tk, tv, inv_freq=inv, positions=positions, q=tq)
+    att = cs.tree_attention(q, cache, tab, ctx, parent.to(DEV), D ** -0.5)
+    # logits of a made-up head over the attention's result
+    w = torch.randn(Hq * D, V, generator=g).to(DEV) / 8
+    logits = torch.nn.functional.pad((att.float().reshape(B, N, -1) @ w).to(BF16), (0, 5))[:, :, :V]
+    tokens = logits.float().argmax(-1).int().gather(1, parent.clamp(min=0).long().to(DEV)).contiguous()
+    tokens[:, 5::3] = (tokens[:, 5::3] + 1) % V
+    from paper_2605_24793_amd.workloads import Head
+    head = Head((torch.randn(64, 64, generator=g) / 8).to(BF16).to(DEV), None,
+                (torch.randn(64, generator=g) / 8).to(BF16).to(DEV), 0.0)
+    hidden = torch.randn(B, N, 64, generator=g).to(BF16).to(DEV)
+    step = cs.verify_tree(logits, logits, parent.to(DEV), tokens, hidden, head, 2.0)
+    cs.cache_keep(cache, tab, ctx, step["path"])
+    new_ctx = ctx + step["accept_len"]
+    K = 2
+    rk, rv, rq = draw(2 * K + 3, H), draw(2 * K + 3, H), draw(2 * K + 3, Hq)
+    rq2 = cs.cache_append(cache, tab, new_ctx, rk, rv, inv_freq=inv, q=rq)
+    out = cs.hybrid_attention_paged(rq2, cache, tab, new_ctx, new_ctx, K, D ** -0.5)
+    torch.cuda.synchronize()
+    assert int(step["accept_len"].max()) > 1
+    for b in range(B):
+        c, s = int(ctx[b]), int(step["accept_len"][b])
+        path = step["path"][b, :s].tolist()
+        rows = [(pk[b, i], pv[b, i], i) for i in range(c)]
+        rows += [(tk[b, n], tv[b, n], c + int(depth[b, n])) for n in path]
+        rows += [(rk[b, i], rv[b, i], c + s + i) for i in range(2 * K + 3)]
+        assert [r[2] for r in rows] == list(range(len(rows)))
+        keys = torch.stack([ref.rotate(k.cpu(), p, inv.cpu(), False) for k, _, p in rows], 1)
+        values = torch.stack([v.cpu().double() for _, v, _ in rows], 1)
+        host = _host(cache)
+        held = {"k": host.of("k", table[b], len(rows)), "v": host.of("v", table[b], len(rows))}
+        half = 2.0 ** -4 if dtype == F8 else 2.0 ** -8
+        for side, x in (("k", keys), ("v", values)):
+            # one rounding to the stored type, and in 8 bits one more where a scale grew later;
+            # among the subnormals 2^-10 of a scale, no more than 2^-6 here (|x| < 7)
+            tol = half * x.abs() + (2 * 2.0 ** -16 if dtype == F8 else 2.0 ** -20)
+            assert ((held[side] - x).abs() <= tol).all(), side
+        m = torch.ones(2 * K + 3, len(rows), dtype=torch.bool)
+        want, size = ref.attention(rq2[b].cpu(), held["k"], held["v"], m, D ** -0.5)
+        _check_rows(out[b], want, size)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+def test_a_round_on_the_cache(dtype):
+    _round_trip(dtype, 11)
+
+
+def test_calls_replay_from_a_hip_graph():
+    """Append and attention captured once; every replay sees the inputs of its moment."""
+    B, H, Hq, D, P, n = 2, 2, 8, 128, 64, 7
+    table, n_pages = ref.make_table(B, 6, 3)
+    cache = _filled(table, n_pages, H, D, P, F8, [300, 70], 3, junk=False)
+    tab = table.to(DEV)
+    g = _gen(4)
+    start = torch.tensor([300, 70], dtype=torch.int32, device=DEV)
+    k, v, q = (torch.randn(B, n, h, D, generator=g).to(BF16).to(DEV) for h in (H, H, Hq))
+    inv = (10000.0 ** (-torch.arange(0, D, 2).double() / D)).float().to(DEV)
+    app = cs.prepare_cache_append(cache, tab, start, k, v, inv_freq=inv, q=q)
+    att = cs.prepare_hybrid_attention_paged(app.outputs["q"], cache, tab, start, start, 2, D ** -0.5)
+    assert att.workspace is not None                        # cut: both kernels are in the graph
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        app.launch()
+        att.launch()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        app.launch()
+        att.launch()
+    for i in range(4):
+        k.copy_(torch.randn(B, n, H, D, generator=g).to(BF16))
+        q.copy_(torch.randn(B, n, Hq, D, generator=g).to(BF16))
+        start.copy_(torch.tensor([300 - i, 70 + i], dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        first = att.outputs["out"].clone()
+        app.launch()
+        att.launch()
+        torch.cuda.synchronize()
+        assert _same(first, att.outputs["out"])
+
+
+def test_two_calls_on_two_streams():
+    B, H, Hq, D, P = 2, 2, 8, 128, 32
+    calls, wants = [], []
+    for i in range(2):
+        table, n_pages = ref.make_table(B, 80, i)
+        cache = _filled(table, n_pages, H, D, P, F8, [2500, 900], i, junk=False)
+        q = torch.randn(B, 9, Hq, D, generator=_gen(i)).to(BF16).to(DEV)
+        ctx = torch.tensor([2400, 800], dtype=torch.int32, device=DEV)
+        calls.append(cs.prepare_hybrid_attention_paged(q, cache, table.to(DEV), ctx, ctx, 3, D ** -0.5))
+        wants.append(cs.hybrid_attention_paged(q, cache, table.to(DEV), ctx, ctx, 3, D ** -0.5).clone())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(5):
+        for c, s in zip(calls, streams):
+            with torch.cuda.stream(s):
+                c.launch()
+    torch.cuda.synchronize()
+    for c, w in zip(calls, wants):
+        assert _same(c.outputs["out"], w)
+
+
+def test_pages_past_four_gigabytes():
+    """Pages whose memory lies past 2^32 bytes of the array."""
+    H, D, P = 8, 128, 128
+    n_pages = (1 << 32) // (H * D * P * 2) + 40
+    cache = cs.PagedCache.empty(n_pages, H, D, P, BF16, DEV)
+    table = torch.tensor([[n_pages - 1, n_pages - 17], [n_pages - 30, 0]], dtype=torch.int32)
+    g = _gen(1)
+    k, v = (torch.randn(2, 150, H, D, generator=g).to(BF16) for _ in range(2))
+    zero = torch.zeros(2, dtype=torch.int32, device=DEV)
+    cs.cache_append(cache, table.to(DEV), zero, k.to(DEV), v.to(DEV))
+    q = torch.randn(2, 2, H, D, generator=g).to(BF16)
+    ctx = torch.full((2,), 150, dtype=torch.int32, device=DEV)
+    got = cs.hybrid_attention_paged(q.to(DEV), cache, table.to(DEV), ctx, ctx - 2, 0, D ** -0.5)
+    torch.cuda.synchronize()
+    for b in range(2):
+        mask = torch.arange(150) < torch.tensor([149, 150])[:, None]
+        out, size = ref.attention(q[b], k[b].double().transpose(0, 1), v[b].double().transpose(0, 1), mask, D ** -0.5)
+        _check_rows(got[b], out, size)
+
+
+def test_nothing_to_do():
+    table, n_pages = ref.make_table(2, 2, 0)
+    cache = _filled(table, n_pages, 2, 64, 16, BF16, [4, 4], 0, junk=False)
+    before = _host(cache)
+    tab, z = table.to(DEV), torch.zeros(2, dtype=torch.int32, device=DEV)
+    empty = torch.empty(2, 0, 2, 64, dtype=BF16, device=DEV)
+    cs.cache_append(cache, tab, z, empty, empty)
+    assert cs.hybrid_attention_paged(torch.empty(2, 0, 4, 64, dtype=BF16, device=DEV), cache, tab, z, z, 1, 0.1).numel() == 0
+    none = torch.empty(0, 3, 4, 64, dtype=BF16, device=DEV)
+    assert cs.hybrid_attention_paged(none, cache, tab[:0], z[:0], z[:0], 1, 0.1).shape == (0, 3, 4, 64)
+    cs.cache_keep(cache, tab[:0], z[:0], torch.empty(0, 3, dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    after = _host(cache)
+    assert torch.equal(before.raw["k"], after.raw["k"]) and torch.equal(before.raw["v"], after.raw["v"])
