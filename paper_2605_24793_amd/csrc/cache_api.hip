@@ -25,8 +25,8 @@ cospec_status check_cache_sizes(const cospec_cache *c) {
     if (c->dtype != COSPEC_BF16 && c->dtype != COSPEC_F8E4M3) return COSPEC_ERR_UNSUPPORTED;
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return COSPEC_ERR_UNSUPPORTED;
     if (c->d != 64 && c->d != 128) return COSPEC_ERR_UNSUPPORTED;
-    // table entries are int32, and a sequence's positions stay below 2^31
-    if (c->n_pages > INT32_MAX || c->max_pages > INT32_MAX / c->page) return COSPEC_ERR_UNSUPPORTED;
+    // pages times heads and a sequence's positions are counted in 32 bits, with room to spare
+    if (c->n_pages > INT32_MAX / 4 / c->heads || c->max_pages > (INT32_MAX - 65536) / c->page) return COSPEC_ERR_UNSUPPORTED;
     return COSPEC_OK;
 }
 

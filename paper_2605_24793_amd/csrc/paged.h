@@ -52,12 +52,13 @@ struct PagedArgs {
     float *part_o;
     float2 *part_ml;
     // set by the launch
-    int32_t row_tiles;         // 16-row tiles of a workgroup
+    int32_t row_tiles, row_waves;   // 16-row tiles of a wave, waves with rows of their own
+    int32_t min_piece;         // keys of a piece, at least
     FastDiv by_grp, by_blocks, by_heads, by_splits, by_seq_rows, by_hq;
 };
 
 struct PagedPlan {
-    int32_t row_tiles, blocks, splits;   // blocks: workgroups that share a group's rows
+    int32_t row_tiles, row_waves, blocks, splits, min_piece;   // blocks: workgroups that share a group's rows
     int64_t rows;                        // B * n_q * Hq
 };
 

@@ -7,10 +7,13 @@
 // joined the same way.
 //
 // Work split: the query rows (position x head) that share a key/value head of a sequence form
-// a group.  A workgroup takes up to 16 * RT rows of a group, and its waves take turns at the
-// group's keys, 64 at a time, all rows each: a wave reads its keys and values straight from the
-// pages into the registers that the matrix instructions take them from, once, with no LDS
-// and no barrier on the way, and the waves' sums are joined through LDS at the end.
+// a group.  A workgroup takes rows of a group; with up to 48 of them (96 in many groups) its waves
+// take turns at the group's keys (k_paged_attention): a wave's keys and values of a turn go from the
+// pages into LDS of its own with loads that pass no register, each lane's operands where the
+// lane reads them back, so that the wave has its next turn under way without a barrier, and the
+// waves' sums are joined at the end.  With more rows the waves take rows of their own and share
+// the keys (k_paged_attention_wide).  Few groups are cut over their keys into pieces,
+// by each sequence's own length, which a second kernel joins.
 //
 // S^T = K Q^T (v_mfma_f32_16x16x32_bf16): lane l holds query column l % 16, so the softmax of a
 // query stays in four lanes.  Which key stands in which row of a product is free: row i of
@@ -21,6 +24,8 @@
 //
 // e4m3: v_cvt_scalef32_pk_bf16_fp8 widens two elements and applies the page's power of two;
 // e4m3 has fewer bits than bf16, so nothing is rounded, and one conversion serves all rows.
+#include <algorithm>
+
 #include "paged.h"
 
 namespace cospec {
@@ -33,11 +38,14 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;             // of a workgroup
-constexpr int kStep = 64;             // keys of a wave's turn
+constexpr int kThreads = 64 * kWaves;
+constexpr int kSegment = 252;         // pages looked up at a time: with one more, at most one a thread; whole turns
+constexpr int kStep = 64;             // keys of a wave's turn, at most
 // 16-row tiles of a workgroup, at most: what the registers hold of queries, scores and sums
 constexpr int kMaxRowTiles = 3;
-constexpr int kMinPiece = 256;        // keys of a piece, at least: a turn per wave
-constexpr int kMaxPieces = 64;        // of a group's keys (the merge weighs them in one wave)
+constexpr int kMinPiece = 512;        // keys of a piece, at least
+constexpr int kMinPieceWide = 256;
+constexpr int64_t kMaxPieces = 64;        // of a group's keys (the merge weighs them in one wave)
 constexpr float kLog2eP = 1.4426950408889634f;
 constexpr float kLazyRescale = 8.0f;  // log2 units a block's max may exceed the running max by
 
@@ -50,19 +58,12 @@ __device__ inline floatx4 mfma(u32x4 a, u32x4 b, floatx4 c) {
                                                    0, 0);
 }
 
-// max and sum over the four lanes that share a query column (l % 16)
+// max over the four lanes that share a query column (l % 16)
 __device__ inline float max_rows(float x) {
     const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     x = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
     const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
-}
-
-__device__ inline float sum_rows(float x) {
-    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 
 // Eight e4m3 bytes (two words) times a power of two, as four words of two bf16.
@@ -73,350 +74,781 @@ __device__ inline u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
 }
 
+// A value that is the same in every lane, for the scalar registers.
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Loads through the scalar cache, of what no kernel writes while this one runs.
+typedef __attribute__((address_space(4))) const int const_int;
+typedef __attribute__((address_space(4))) const float const_float;
+__device__ inline int scalar_load(const int32_t *p) { return *(const_int *)reinterpret_cast<uintptr_t>(p); }
+__device__ inline float scalar_load(const float *p) { return *(const_float *)reinterpret_cast<uintptr_t>(p); }
+
 // What the queries of sequence b see.  Hybrid: position p < lc sees [0, p], lc <= p < end sees
 // [0, end).  Tree: node r sees [0, lc) and its ancestors among lc .. end - 1.
 struct Seq {
-    int64_t lc, end, qs;
+    int lc, end;
+    int64_t qs;
 };
 
 __device__ inline Seq sequence_of(const PagedArgs &a, int b) {
     const int64_t room = static_cast<int64_t>(a.c.max_pages) << a.c.log_page;
-    const int64_t lc = max(a.ctx_len[b], 0);
+    const int64_t lc = max(scalar_load(a.ctx_len + b), 0);
     const int64_t more = a.parent ? a.n_q : 2 * static_cast<int64_t>(a.K) + 3;
-    const int64_t end = min(lc + more, room);
-    return Seq{min(lc, end), end, a.parent ? lc : static_cast<int64_t>(a.q_start[b])};
+    const int end = static_cast<int>(min(lc + more, room));
+    return Seq{static_cast<int>(min(lc, static_cast<int64_t>(end))), end, a.parent ? lc : static_cast<int64_t>(scalar_load(a.q_start + b))};
 }
 
 // Keys [0, kend) that the rows [q0, q1) of a group see, and how they are cut.
 struct Cut {
-    int64_t kend, chunk;
+    int kend, chunk;
     int pieces;                // at least 1
 };
 
 __device__ inline Cut cut_of(const PagedArgs &a, const Seq &s, int q0, int q1) {
     const int64_t p_lo = s.qs + quot(a.by_grp, q0), p_hi = s.qs + quot(a.by_grp, q1 - 1);
-    int64_t kend = s.end;
+    int kend = s.end;
     if (p_lo >= s.end) kend = 0;                            // all padding: no key
-    else if (!a.parent && p_hi < s.lc) kend = max(p_hi + 1, static_cast<int64_t>(0));
-    const int64_t part = (kend + a.splits - 1) / a.splits;
-    const int64_t chunk = max((part + kStep - 1) / kStep * kStep, static_cast<int64_t>(kMinPiece));
-    return Cut{kend, chunk, max(static_cast<int>((kend + chunk - 1) / chunk), 1)};
+    else if (!a.parent && p_hi < s.lc) kend = max(static_cast<int>(p_hi) + 1, 0);
+    const int part = quot(a.by_splits, kend + a.splits - 1);
+    const int chunk = max((part + kStep - 1) / kStep * kStep, a.min_piece);
+    return Cut{kend, chunk, max((kend + chunk - 1) / chunk, 1)};
 }
 
 // The sixteen bits from bit `at` (may be negative) of a set of 256.
-__device__ inline uint32_t window16(const uint32_t *set, int64_t at) {
+__device__ inline uint32_t window16(const uint32_t *set, int at) {
     if (at <= -16 || at >= 256) return 0;
     if (at < 0) return (set[0] << -at) & 0xffffu;
-    const int w = static_cast<int>(at) >> 5;
+    const int w = at >> 5;
     const uint64_t two = set[w] | static_cast<uint64_t>(w < 7 ? set[w + 1] : 0u) << 32;
     return static_cast<uint32_t>(two >> (at & 31)) & 0xffffu;
 }
 
-template <int D, bool F8, int RT>
-__global__ __launch_bounds__(64 * kWaves, RT == 1 || (F8 && RT == 2) ? 2 : 1) void k_paged_attention(PagedArgs a) {
+// 16 bytes per lane from global memory into LDS at byte lds + 16 * lane, lds the same in every
+// lane.  Written as assembly, so that the compiler, which knows nothing of these loads, places no
+// wait for them before LDS reads; the kernel's own waits order them.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ inline void load_lds16(const char *src, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(src) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// Waits until at most N vector-memory operations of this wave are outstanding.
+template <int N> __device__ inline void wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// Waits for this wave's LDS reads.
+__device__ inline void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+typedef __attribute__((address_space(3))) const char lds_cchar;
+
+// Workgroup barrier that does not wait for the loads still in flight (as the fence of
+// __syncthreads would); the compiler may not move memory accesses across it.
+__device__ inline void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Ancestors of every node, as sets of 256 bits in LDS, by all threads: each round joins the set
+// of the node `up`, twice as far up as the round before.
+__device__ inline void find_ancestors(const PagedArgs &a, int b, uint32_t (*s_anc)[8], int *s_up) {
+    const int tid = threadIdx.x;
+    const int n = a.n_q;
+    int up = -1;
+    if (tid < n) {
+        const int p = a.parent[static_cast<int64_t>(b) * n + tid];
+        up = p >= 0 && p < tid ? p : -1;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) s_anc[tid][w] = w == tid >> 5 ? 1u << (tid & 31) : 0u;
+        s_up[tid] = up;
+    }
+    for (int far = 1; far < n; far *= 2) {
+        __syncthreads();
+        uint32_t set[8];
+        int next_up = -1;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) set[w] = up >= 0 ? s_anc[up][w] : 0u;
+        if (up >= 0) next_up = s_up[up];
+        __syncthreads();
+        if (tid < n) {
+#pragma unroll
+            for (int w = 0; w < 8; ++w) s_anc[tid][w] |= set[w];
+            s_up[tid] = up = next_up;
+        }
+    }
+    __syncthreads();
+}
+
+// Which rows, keys and group a workgroup takes.  Workgroups are dealt to the XCDs round-robin: those
+// that read the same keys (the row blocks of a piece of a group) follow each other on one XCD,
+// whose L2 then serves all but the first; the last rows, which see the most keys, come first.
+struct Place {
+    int b, h, block, piece;
+};
+
+__device__ inline Place place_of(const PagedArgs &a) {
+    const uint32_t slot = blockIdx.x / kXcds;
+    const uint32_t round = quot(a.by_blocks, slot);
+    const int block = a.by_blocks.d - 1 - (slot - round * a.by_blocks.d);
+    const uint32_t unit = round * kXcds + blockIdx.x % kXcds;
+    const uint32_t bh = quot(a.by_splits, unit);
+    const int b = quot(a.by_heads, bh);
+    return Place{b, static_cast<int>(bh - b * a.by_heads.d), block, static_cast<int>(unit - bh * a.by_splits.d)};
+}
+
+// What a workgroup keeps in LDS of each page of its keys, up to kThreads of them at a time, one looked
+// up by each thread: {page * heads + head, with kNone for a page that is none (it is read as page
+// 0, and not used); the upper halves of the scales of keys and of values (e4m3)}.
+typedef uint2 PageEntry;
+constexpr uint32_t kNone = 0x80000000u;
+
+__device__ inline uint32_t pack_scales(float k, float v) {
+    return (__float_as_uint(k) & 0x7f800000u) | (__float_as_uint(v) & 0x7f800000u) >> 16;
+}
+__device__ inline float key_scale(PageEntry e) { return __uint_as_float(e.y & 0xffff0000u); }
+__device__ inline float value_scale(PageEntry e) { return __uint_as_float(e.y << 16); }
+
+// This thread's entry of sequence b's table, from entry `first` on (clamped to the table).
+__device__ inline uint32_t table_entry(const PagedArgs &a, int b, int first) {
+    const int at = min(first + static_cast<int>(threadIdx.x), a.c.max_pages - 1);
+    return a.c.table[static_cast<int64_t>(b) * a.c.max_pages + at];
+}
+
+// RW waves of the four share the keys, each with RT row tiles of its own; the 4 / RW sets of them
+// take turns at the keys.
+template <int D, bool F8, int RT, int RW>
+__global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
     constexpr int DS = D / 32;                              // k-steps of the first product
     constexpr int DT = D / 16;                              // d tiles of the second
     constexpr int EB = F8 ? 1 : 2;
-    constexpr int KC = D * EB / 64;                         // 16-byte loads of a lane's key
+    constexpr int KS = D * EB > 128 ? 32 : 64;              // keys of a turn: 16 KB with their values
+    constexpr int NT = KS / 16, NU = KS / 32;               // key tiles, and k-steps of the second product
+    constexpr int HT = RT > 2 ? 1 : NT / 2, HD = RT > 2 ? 1 : DT / 2;   // key and component tiles whose operands are held at a time
+    constexpr int GK = KS / 4;                              // keys of a lane group
+    constexpr int KC = D * EB / 64;                         // 16-byte pieces of a lane's key
+    constexpr int VC = GK * EB / 16;                        // ... and of its values of a component
+    constexpr int NK = NT * KC, NV = DT * VC;               // loads of a turn's keys, and values
+    constexpr int KW = kWaves / RW;                         // sets of waves
+    constexpr int NS = RW;                                  // turns of a set that are in LDS at a time
+    constexpr int kValuesAt = NK * 1024, kStage = (NK + NV) * 1024;
     constexpr int OS = D + 4;                               // floats of a staged row of sums
-    __shared__ __attribute__((aligned(16))) float s_o[kWaves][16 * OS];
+    constexpr int kLds = kWaves * (kStage > 16 * OS * 4 ? kStage : 16 * OS * 4);
+    static_assert(NK % RW == 0 && NV % RW == 0 && KW * NS == kWaves, "turns");
+    __shared__ __attribute__((aligned(16))) char s_ring[kLds];
     __shared__ float2 s_ml[kWaves][16 * RT];
+    __shared__ PageEntry s_page[kThreads];
     __shared__ uint32_t s_anc[kMaxSeqRows][8];
     __shared__ int s_up[kMaxSeqRows];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int g = lane >> 4, l16 = lane & 15;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int rw = wave % RW, kw = wave / RW;
+    const int g = lane >> 4, l16 = lane & 15, kg = l16 >> 2;
     const int grp = a.by_grp.d, rows = a.n_q * grp;
-    const uint32_t unit = quot(a.by_splits, blockIdx.x);
-    const int piece = blockIdx.x - unit * a.by_splits.d;
-    const uint32_t bh = quot(a.by_blocks, unit);
-    const int blk = unit - bh * a.by_blocks.d;
-    const int b = quot(a.by_heads, bh), h = bh - b * a.by_heads.d;
-    const int q0 = blk * (16 * RT), q1 = min(q0 + 16 * RT, rows);
-    const Seq s = sequence_of(a, b);
-    const Cut cut = cut_of(a, s, q0, q1);
-    if (piece >= cut.pieces) return;
-    const int64_t kbeg = piece * cut.chunk, kend = min(kbeg + cut.chunk, cut.kend);
-
-    if (a.parent) {
-        // ancestors of every node, as sets: each round joins the set of the node `up`, twice as
-        // far up as the round before
-        const int n = a.n_q;
-        int up = -1;
-        if (tid < n) {
-            const int p = a.parent[static_cast<int64_t>(b) * n + tid];
-            up = p >= 0 && p < tid ? p : -1;
-#pragma unroll
-            for (int w = 0; w < 8; ++w) s_anc[tid][w] = w == tid >> 5 ? 1u << (tid & 31) : 0u;
-            s_up[tid] = up;
-        }
-        for (int far = 1; far < n; far *= 2) {
-            __syncthreads();
-            uint32_t set[8];
-            int next = -1;
-#pragma unroll
-            for (int w = 0; w < 8; ++w) set[w] = up >= 0 ? s_anc[up][w] : 0u;
-            if (up >= 0) next = s_up[up];
-            __syncthreads();
-            if (tid < n) {
-#pragma unroll
-                for (int w = 0; w < 8; ++w) s_anc[tid][w] |= set[w];
-                s_up[tid] = up = next;
-            }
-        }
-        __syncthreads();
-    }
-
-    // this lane's query of every row tile.  Keys are taken by a k-step as they lie in memory:
+    const Place w_ = place_of(a);
+    const int b = w_.b, h = w_.h, piece = w_.piece;
+    if (b >= a.B) return;
+    const int q0 = w_.block * (16 * RT * RW), q1 = min(q0 + 16 * RT * RW, rows);
+    // what the loads below need is known: they go out before the sequence's length is
+    uint32_t id = a.splits == 1 ? table_entry(a, b, 0) : 0u;
+    // This lane's query of every row tile.  Keys are taken by a k-step as they lie in memory:
     // bf16 key bytes 64 c + 16 g .. + 15, k-step c; e4m3 the same bytes, k-steps 2c and 2c + 1.
     u32x4 qf[RT][DS];
-    int64_t vis[RT];                                        // keys [0, vis) are seen
     int node[RT];
-    int64_t vis_min = INT64_MAX;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const int qi = q0 + rt * 16 + l16;
-        const bool valid = qi < q1;
-        const int r = valid ? quot(a.by_grp, qi) : 0;
-        const int hq = h * grp + (valid ? qi - r * grp : 0);
-        const int64_t p = s.qs + r;
-        const bool live = valid && p >= 0 && p < s.end;
-        node[rt] = r;
-        vis[rt] = !live ? 0 : a.parent || p >= s.lc ? (a.parent ? s.lc : s.end) : p + 1;
-        if (live) vis_min = min(vis_min, vis[rt]);
-        const char *qrow = static_cast<const char *>(a.q) + ((static_cast<int64_t>(b) * a.n_q + r) * a.Hq + hq) * D * 2;
+        const int qi = min(q0 + (rw * RT + rt) * 16 + l16, q1 - 1);
+        node[rt] = quot(a.by_grp, qi);
+        const int hq = h * grp + (qi - node[rt] * grp);
+        const char *qrow = static_cast<const char *>(a.q) + ((static_cast<int64_t>(b) * a.n_q + node[rt]) * a.Hq + hq) * D * 2;
 #pragma unroll
         for (int c = 0; c < DS; ++c) {
             const int d = F8 ? (c / 2) * 64 + g * 16 + (c % 2) * 8 : c * 32 + g * 8;
-            qf[rt][c] = live ? *reinterpret_cast<const u32x4 *>(qrow + d * 2) : u32x4{0, 0, 0, 0};
+            qf[rt][c] = *reinterpret_cast<const u32x4 *>(qrow + d * 2);
         }
-        if (!live) node[rt] = -1;
+    }
+    const Seq s = sequence_of(a, b);
+    const Cut cut = cut_of(a, s, q0, q1);
+    if (piece >= cut.pieces) return;
+    const int kbeg = piece * cut.chunk, kend = min(kbeg + cut.chunk, cut.kend);
+
+    // The pages of up to kSegment pages' keys are looked up at a time, by all threads, into LDS.
+    const int P1 = (1 << a.c.log_page) - 1;
+    const char *const set_lds = s_ring + kw * NS * kStage;
+    const uint32_t ring = uniform(static_cast<int>(reinterpret_cast<uintptr_t>((lds_cchar *)set_lds)));
+    int first_page = 0, last_page = 0;                      // of those in LDS
+    uint32_t scales = 0;
+    auto look_up = [&](int from, int to, uint32_t entry) {  // of keys [from, to), this thread's table entry given
+        first_page = from >> a.c.log_page;
+        last_page = (to - 1) >> a.c.log_page;
+        const bool in = tid <= last_page - first_page, none = entry >= static_cast<uint32_t>(a.c.n_pages);
+        const uint32_t at = (none ? 0 : entry) * a.c.H + h;
+        if (in) s_page[tid].x = at | (none ? kNone : 0u);
+        if (F8 && in) scales = pack_scales(a.c.k_scale[at], a.c.v_scale[at]);
+    };
+    // This lane's key rows of a turn are among the keys GK kg .. GK kg + GK - 1, its values those of
+    // the keys GK g ..: each within one page.
+    // (keys past the last one are looked for in the last page, and not used)
+    auto page_of = [&](int key) { return s_page[min(key >> a.c.log_page, last_page) - first_page]; };
+    // this wave's share of a turn's keys and values, into LDS at `at`
+    auto load_keys = [&](int k0, uint32_t at) {
+        const int key = k0 + kg * GK;
+        const PageEntry page = page_of(key);
+        const char *base = a.c.k + ((static_cast<int64_t>(page.x & ~kNone) << a.c.log_page) + (key & P1) + (l16 & 3)) * (D * EB) + g * 16;
+#pragma unroll
+        for (int i = 0; i < NK / RW; ++i) {
+            const int e = rw * (NK / RW) + i;
+            load_lds16(base + (e / KC) * 4 * (D * EB) + (e % KC) * 64, at + e * 1024);
+        }
+    };
+    const int64_t v_tile = (static_cast<int64_t>(16) << a.c.log_page) * EB;
+    auto load_values = [&](int k0, uint32_t at) {
+        const int key = k0 + g * GK;
+        const PageEntry page = page_of(key);
+        const char *base = a.c.v + (((static_cast<int64_t>(page.x & ~kNone) * D + l16) << a.c.log_page) + (key & P1)) * EB;
+#pragma unroll
+        for (int i = 0; i < NV / RW; ++i) {
+            const int e = rw * (NV / RW) + i;
+            load_lds16(base + (e / VC) * v_tile + (e % VC) * 16, at + kValuesAt + e * 1024);
+        }
+    };
+    constexpr int kTurn = KW * KS;                          // keys of all sets' turns
+    const int segment = kSegment << a.c.log_page;
+    if (a.parent) find_ancestors(a, b, s_anc, s_up);
+
+    // Scores are taken as |scale| (+-q) . k, so that the largest product is the largest score.
+    int vis[RT];                                            // keys [0, vis) are seen
+    int vis_min = INT32_MAX;
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int64_t p = s.qs + node[rt];
+        const bool live = q0 + (rw * RT + rt) * 16 + l16 < q1 && p >= 0 && p < s.end;
+        vis[rt] = !live ? 0 : a.parent ? s.lc : p >= s.lc ? s.end : static_cast<int>(p) + 1;
+        if (live) vis_min = min(vis_min, vis[rt]);
+        else node[rt] = -1;
+#pragma unroll
+        for (int c = 0; c < DS; ++c)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) qf[rt][c][w] = live ? qf[rt][c][w] ^ flip : 0u;
     }
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) vis_min = min(vis_min, __shfl_xor(vis_min, off));
+    const int clear = uniform(min(vis_min, kend));          // turns that end here or before mask nothing
 
     floatx4 o[RT][DT];
-    float m[RT], l[RT];
+    float m[RT];
+    floatx4 ol[RT];                                         // sums of the weights alone, rows all alike
+    const u32x4 ones{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
+        ol[rt] = floatx4{0.f, 0.f, 0.f, 0.f};
         m[rt] = -INFINITY;
-        l[rt] = 0.f;
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[rt][t] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
-    const float sc = a.scale * kLog2eP;
-
-    // A turn's keys lie in up to four pages: of key group l16 / 4 for this lane's key rows, of
-    // group g for its values.
-    const int32_t *table = a.c.table + static_cast<int64_t>(b) * a.c.max_pages;
-    const int P1 = (1 << a.c.log_page) - 1;
-    const int kg = l16 >> 2;
-    auto ids = [&](int64_t k0, int &idk, int &idv) {
-        const int64_t last = a.c.max_pages - 1;
-        idk = table[min((k0 + kg * 16) >> a.c.log_page, last)];
-        idv = table[min((k0 + g * 16) >> a.c.log_page, last)];
-    };
-    u32x4 kr[4][KC], vr[DT][EB];
-    float ksc = 1.f, vsc = 1.f;
-    auto load_keys = [&](int64_t k0, int id) {
-        const int64_t pid = max(page_or_none(a.c, id), static_cast<int64_t>(0)), blk_ = pid * a.c.H + h;
-        const int place = static_cast<int>(k0 + kg * 16) & P1;
-        const char *base = a.c.k + ((blk_ << a.c.log_page) + place + (l16 & 3)) * (D * EB) + g * 16;
+    const float sc = fmaxf(fabsf(a.scale) * kLog2eP, 1.17549435e-38f);
+    for (int seg = kbeg; seg < kend; seg += segment) {
+        const int seg_end = min(seg + segment, kend);
+        if (seg > kbeg || a.splits > 1) id = table_entry(a, b, seg >> a.c.log_page);
+        if (seg > kbeg) __syncthreads();                    // the pages of the segment before are used up
+        look_up(seg, seg_end, id);
+        lds_barrier();
+        const int k_first = seg + kw * KS;
+        const int turns = k_first < seg_end ? (seg_end - k_first + kTurn - 1) / kTurn : 0;
+        const int all_turns = (seg_end - seg + kTurn - 1) / kTurn;   // of the set that has most
+        if (turns > 0) {                                    // a set is one turn ahead in its loads
+            load_keys(k_first, ring);
+            load_values(k_first, ring);
+        }
+        if (F8 && tid <= last_page - first_page) s_page[tid].y = scales;
+        lds_barrier();
+        for (int j = 0; j < (RW > 1 ? all_turns : turns); ++j) {
+            const int k0 = k_first + j * kTurn;
+            const bool more = j + 1 < turns;
+            const uint32_t at = RW > 1 ? (j % NS) * kStage : 0;
+            const u32x4 *keys = reinterpret_cast<const u32x4 *>(set_lds + at) + lane;
+            u32x4 *values = reinterpret_cast<u32x4 *>(s_ring + kw * NS * kStage + at + kValuesAt) + lane;
+            if constexpr (RW > 1) {
+                wait_vm<0>();                               // this wave's loads of the turn
+                lds_barrier();                              // ... and the others'; the turn before is used up
+                if (more) {
+                    const uint32_t to = ring + ((j + 1) % NS) * kStage;
+                    load_keys(k0 + kTurn, to);
+                    load_values(k0 + kTurn, to);
+                }
+                if (j >= turns) continue;                   // wave-uniform; another set has one more
+            }
+            const float ksc = key_scale(page_of(k0 + kg * GK));
+            const PageEntry page_v = page_of(k0 + g * GK);
+            float vsc = value_scale(page_v);
+            const bool none = page_v.x >= kNone;
+            // wave-uniform: a key that some query does not see, or that does not exist
+            const bool masked = k0 + KS > clear || __ballot(none) != 0;
+            // S^T of the turn
+            floatx4 st[RT][NT];
+            if (RW == 1) wait_vm<NV>();                         // its keys have landed
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+            for (int th = 0; th < NT; th += HT) {
+                u32x4 kf[HT][DS];
 #pragma unroll
-            for (int c = 0; c < KC; ++c) kr[t][c] = *reinterpret_cast<const u32x4 *>(base + t * 4 * (D * EB) + c * 64);
-        if (F8) ksc = a.c.k_scale[blk_];
-    };
-    auto load_values = [&](int64_t k0, int id) {
-        const int64_t pid = max(page_or_none(a.c, id), static_cast<int64_t>(0)), blk_ = pid * a.c.H + h;
-        const int place = static_cast<int>(k0 + g * 16) & P1;
-        const char *base = a.c.v + ((((blk_ * D) + l16) << a.c.log_page) + place) * EB;
+                for (int t = 0; t < HT; ++t) {
+                    u32x4 raw[KC];
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
+                    for (int c = 0; c < KC; ++c) raw[c] = keys[((th + t) * KC + c) * 64];
 #pragma unroll
-            for (int c = 0; c < EB; ++c)
-                vr[t][c] = *reinterpret_cast<const u32x4 *>(base + ((static_cast<int64_t>(t) * 16) << a.c.log_page) * EB + c * 16);
-        if (F8) vsc = a.c.v_scale[blk_];
-    };
-
-    constexpr int kTurn = kWaves * kStep;
-    int64_t k0 = kbeg + wave * kStep;
-    int idk, idv, idk1 = 0, idv1 = 0;
-    if (k0 < kend) {
-        ids(k0, idk, idv);
-        ids(k0 + kTurn, idk1, idv1);
-        load_keys(k0, idk);
-        load_values(k0, idv);
-    }
-    for (; k0 < kend; k0 += kTurn) {
-        const bool more = k0 + kTurn < kend;
-        // S^T of the turn
-        floatx4 st[RT][4];
+                    for (int c = 0; c < DS; ++c) {
+                        if constexpr (F8) kf[t][c] = widen(raw[c / 2][2 * (c % 2)], raw[c / 2][2 * (c % 2) + 1], ksc);
+                        else kf[t][c] = raw[c];
+                    }
+                }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            u32x4 kf[DS];
+                for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-            for (int c = 0; c < DS; ++c)
-                kf[c] = F8 ? widen(kr[t][c / 2][2 * (c % 2)], kr[t][c / 2][2 * (c % 2) + 1], ksc) : kr[t][F8 ? 0 : c];
+                    for (int t = 0; t < HT; ++t) st[rt][th + t] = floatx4{0.f, 0.f, 0.f, 0.f};
+                // products that follow each other are of different sums
+#pragma unroll
+                for (int i = 0; i < DS * RT; ++i) {
+                    const int c = RT > 2 ? i / RT : i % DS, rt = RT > 2 ? i % RT : i / DS;
+#pragma unroll
+                    for (int t = 0; t < HT; ++t) st[rt][th + t] = mfma(kf[t][c], qf[rt][c], st[rt][th + t]);
+                }
+            }
+            __builtin_amdgcn_s_setprio(0);
+            if constexpr (RW == 1) {
+                wait_lds();
+                if (more) load_keys(k0 + kTurn, ring);
+            }
+            if (masked) {
+                const int kb = k0 + g * GK;                     // this lane's first key
+                const int real = none ? 0 : min(max(kend - kb, 0), GK);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const int top = min(max(vis[rt] - kb, 0), real);
+                    uint32_t see = (1u << top) - 1u;
+                    if (a.parent && node[rt] >= 0) see |= window16(s_anc[node[rt]], kb - s.lc) & ((1u << real) - 1u);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (!(see >> (4 * t + r) & 1)) st[rt][t][r] = -INFINITY;
+                }
+            }
+            float bm[RT];
+            bool raise = false;
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                st[rt][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+                bm[rt] = -INFINITY;
 #pragma unroll
-                for (int c = 0; c < DS; ++c) st[rt][t] = mfma(kf[c], qf[rt][c], st[rt][t]);
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) bm[rt] = fmaxf(bm[rt], st[rt][t][r]);
+                bm[rt] = max_rows(bm[rt]) * sc;
+                raise |= bm[rt] > m[rt] + kLazyRescale;         // always when m is still -inf
             }
-        }
-        const int id_now = idv;
-        if (more) {
-            load_keys(k0 + kTurn, idk1);
-            idv = idv1;
-        }
-        const int64_t kb = k0 + g * 16;                     // this lane's first key
-        const bool none = page_or_none(a.c, id_now) < 0;
-        // wave-uniform: a key that some query does not see, or that does not exist
-        const bool masked = k0 + kStep > min(vis_min, kend) || __ballot(none) != 0;
-        u32x4 pb[RT][2];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            float bm = -INFINITY;
-            if (!masked) {
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        st[rt][t][r] *= sc;
-                        bm = fmaxf(bm, st[rt][t][r]);
-                    }
-            } else {
-                const int64_t top = min(vis[rt], kend) - kb;
-                uint32_t see = top >= 16 ? 0xffffu : top > 0 ? (1u << top) - 1u : 0u;
-                if (a.parent && node[rt] >= 0) {
-                    const int64_t real = kend - kb;
-                    see |= window16(s_anc[node[rt]], kb - s.lc) & (real >= 16 ? 0xffffu : real > 0 ? (1u << real) - 1u : 0u);
-                }
-                if (none) see = 0;
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        st[rt][t][r] = see >> (4 * t + r) & 1 ? st[rt][t][r] * sc : -INFINITY;
-                        bm = fmaxf(bm, st[rt][t][r]);
-                    }
-            }
-            bm = max_rows(bm);
-            const bool raise = bm > m[rt] + kLazyRescale;   // always when m is still -inf
             if (__builtin_expect(__ballot(raise) != 0, 0)) {
-                const float alpha = raise ? __builtin_amdgcn_exp2f(m[rt] - bm) : 1.f;   // 0 from -inf
-                if (raise) m[rt] = bm;
-                l[rt] *= alpha;
 #pragma unroll
-                for (int t = 0; t < DT; ++t) o[rt][t] *= alpha;
-            }
-            // a query that has seen nothing yet keeps m = -inf and adds nothing
-            const float mm = m[rt] == -INFINITY ? INFINITY : m[rt];
+                for (int rt = 0; rt < RT; ++rt) {
+                    const bool up = bm[rt] > m[rt] + kLazyRescale;
+                    const float alpha = up ? __builtin_amdgcn_exp2f(m[rt] - bm[rt]) : 1.f;   // 0 from -inf
+                    if (up) m[rt] = bm[rt];
+                    ol[rt] *= alpha;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float p[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    p[i] = __builtin_amdgcn_exp2f(st[rt][2 * u + i / 4][i % 4] - mm);
-                    l[rt] += p[i];
+                    for (int t = 0; t < DT; ++t) o[rt][t] *= alpha;
                 }
-                pb[rt][u] = u32x4{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3]), bf16_pair(p[4], p[5]), bf16_pair(p[6], p[7])};
             }
-        }
-        if (masked) {
-            // places that hold no key of the sequence may hold anything, as may the scale of a
-            // page without one: a weight of zero does not make a NaN harmless
-            const int64_t left = none ? 0 : kend - kb;
-            const int real = left >= 16 ? 16 : left > 0 ? static_cast<int>(left) : 0;
-            if (real == 0) vsc = 1.f;
+            // O^T += V^T P^T
+            if constexpr (RW == 1) {
+                if (more) wait_vm<NK>();
+                else wait_vm<0>();
+            }
+            if (masked) {
+                // places that hold no key of the sequence may hold anything, as may the scale of a
+                // page without one: a weight of zero does not make a NaN harmless
+                const int real = none ? 0 : min(max(kend - (k0 + g * GK), 0), GK);
+                if (real == 0) vsc = 1.f;
 #pragma unroll
-            for (int c = 0; c < EB; ++c)
+                for (int c = 0; c < VC; ++c)
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    constexpr int PER = 4 / EB;             // elements of a word
-                    const int in = real - (c * 4 + w) * PER;
-                    const uint32_t keep = in >= PER ? 0xffffffffu : in > 0 ? (1u << (in * 8 * EB)) - 1u : 0u;
+                    for (int w = 0; w < 4; ++w) {
+                        constexpr int EW = 4 / EB;              // elements of a word
+                        const int in = real - (c * 4 + w) * EW;
+                        const uint32_t keep = in >= EW ? 0xffffffffu : in > 0 ? (1u << (in * 8 * EB)) - 1u : 0u;
 #pragma unroll
-                    for (int t = 0; t < DT; ++t) vr[t][c][w] &= keep;
+                        for (int t = 0; t < DT; ++t) {          // waves that share the turn store the same
+                            uint32_t *word = reinterpret_cast<uint32_t *>(values + (t * VC + c) * 64) + w;
+                            *word &= keep;
+                        }
+                    }
+            }
+            u32x4 pb[RT][NU];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                // a query that has seen nothing yet keeps m = -inf and adds nothing
+                const float mm = m[rt] == -INFINITY ? INFINITY : m[rt];
+#pragma unroll
+                for (int u = 0; u < NU; ++u) {
+                    float p[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(st[rt][2 * u + i / 4][i % 4], sc, -mm));
+                    pb[rt][u] = u32x4{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3]), bf16_pair(p[4], p[5]), bf16_pair(p[6], p[7])};
                 }
-        }
-        // O^T += V^T P^T
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const u32x4 vf = F8 ? widen(vr[t][0][2 * u], vr[t][0][2 * u + 1], vsc) : vr[t][F8 ? 0 : u];
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) o[rt][t] = mfma(vf, pb[rt][u], o[rt][t]);
             }
-        if (more) {
-            load_values(k0 + kTurn, idv);
-            ids(k0 + 2 * kTurn, idk1, idv1);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) ol[rt] = mfma(ones, pb[rt][u], ol[rt]);
+#pragma unroll
+            for (int th = 0; th < DT; th += HD) {
+                u32x4 vf[HD][NU];
+#pragma unroll
+                for (int t = 0; t < HD; ++t) {
+                    u32x4 raw[VC];
+#pragma unroll
+                    for (int c = 0; c < VC; ++c) raw[c] = values[((th + t) * VC + c) * 64];
+#pragma unroll
+                    for (int u = 0; u < NU; ++u) {
+                        if constexpr (F8) vf[t][u] = widen(raw[0][2 * u], raw[0][2 * u + 1], vsc);
+                        else vf[t][u] = raw[u];
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < NU; ++u)
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int t = 0; t < HD; ++t) o[rt][th + t] = mfma(vf[t][u], pb[rt][u], o[rt][th + t]);
+            }
+            __builtin_amdgcn_s_setprio(0);
+            if constexpr (RW == 1) {
+                wait_lds();
+                if (more) load_values(k0 + kTurn, ring);
+            }
         }
     }
 
-    // join the waves
+    // join the sets
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        l[rt] = sum_rows(l[rt]);
-        if (node[rt] < 0) {                                 // no query: unmasked turns weighed its zeros evenly
-            m[rt] = -INFINITY;
-            l[rt] = 0.f;
-        }
-        if (g == 0) s_ml[wave][rt * 16 + l16] = make_float2(m[rt], l[rt]);
+        const bool live = node[rt] >= 0;                    // else unmasked turns weighed its zeros evenly
+        if (!live) m[rt] = -INFINITY;
+        if (g == 0) s_ml[wave][rt * 16 + l16] = make_float2(m[rt], live ? ol[rt][0] : 0.f);
     }
-    __syncthreads();
     const bool whole = cut.pieces == 1;
     const int64_t rows_all = static_cast<int64_t>(a.B) * a.n_q * a.Hq;
+    constexpr int TPR = kThreads / (16 * RW);               // threads of a row, four components each at a time
+    float *s_o = reinterpret_cast<float *>(s_ring);         // [kWaves][16][OS]
+    __syncthreads();                                    // every wave is done with its turns
+    const int row = tid / TPR % 16, rw_ = tid / TPR / 16, d0 = tid % TPR * 4;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         float M = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_ml[w][rt * 16 + l16].x);
+        for (int w = 0; w < KW; ++w) M = fmaxf(M, s_ml[w * RW + rw][rt * 16 + l16].x);
         const float f = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[rt] - M);
 #pragma unroll
         for (int t = 0; t < DT; ++t)
-            *reinterpret_cast<floatx4 *>(&s_o[wave][l16 * OS + t * 16 + g * 4]) = o[rt][t] * f;
+            *reinterpret_cast<floatx4 *>(s_o + (wave * 16 + l16) * OS + t * 16 + g * 4) = o[rt][t] * f;
         __syncthreads();
-        // thread: DT components of row tid / 16
-        const int row = tid >> 4, d0 = (tid & 15) * DT, qi = q0 + rt * 16 + row;
-        float x[DT];
-#pragma unroll
-        for (int i = 0; i < DT; ++i) x[i] = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w)
-#pragma unroll
-            for (int i = 0; i < DT; ++i) x[i] += s_o[w][row * OS + d0 + i];
+        const int qi = q0 + (rw_ * RT + rt) * 16 + row;
         float RM = -INFINITY, L = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) RM = fmaxf(RM, s_ml[w][rt * 16 + row].x);
+        for (int w = 0; w < KW; ++w) RM = fmaxf(RM, s_ml[w * RW + rw_][rt * 16 + row].x);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float2 ml = s_ml[w][rt * 16 + row];
+        for (int w = 0; w < KW; ++w) {
+            const float2 ml = s_ml[w * RW + rw_][rt * 16 + row];
             L += ml.x == -INFINITY ? 0.f : ml.y * __builtin_amdgcn_exp2f(ml.x - RM);
         }
-        if (qi < q1) {
-            const int r = quot(a.by_grp, qi);
-            const int64_t R = (static_cast<int64_t>(b) * a.n_q + r) * a.Hq + h * grp + (qi - r * grp);
-            if (whole) {
-                const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;    // NaN stays
-                uint32_t w[DT / 2];
+        const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;       // NaN stays
+        const int r = quot(a.by_grp, min(qi, q1 - 1));
+        const int64_t R = (static_cast<int64_t>(b) * a.n_q + r) * a.Hq + h * grp + (min(qi, q1 - 1) - r * grp);
 #pragma unroll
-                for (int i = 0; i < DT / 2; ++i) w[i] = bf16_pair(x[2 * i] * inv, x[2 * i + 1] * inv);
-                char *dst = static_cast<char *>(a.out) + (R * D + d0) * 2;
-                if constexpr (DT == 8) *reinterpret_cast<u32x4 *>(dst) = u32x4{w[0], w[1], w[2], w[3]};
-                else *reinterpret_cast<u32x2 *>(dst) = u32x2{w[0], w[1]};
-            } else {
-                float *po = a.part_o + (piece * rows_all + R) * D + d0;
+        for (int i = 0; i < D; i += 4 * TPR) {
+            floatx4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < DT; i += 4)
-                    __builtin_nontemporal_store(floatx4{x[i], x[i + 1], x[i + 2], x[i + 3]}, reinterpret_cast<floatx4 *>(po + i));
-                if ((tid & 15) == 0) a.part_ml[piece * rows_all + R] = make_float2(RM, L);
+            for (int w = 0; w < KW; ++w)
+                x += *reinterpret_cast<const floatx4 *>(s_o + ((w * RW + rw_) * 16 + row) * OS + d0 + i);
+            if (qi < q1) {
+                if (whole)
+                    *reinterpret_cast<u32x2 *>(static_cast<char *>(a.out) + (R * D + d0 + i) * 2) =
+                        u32x2{bf16_pair(x[0] * inv, x[1] * inv), bf16_pair(x[2] * inv, x[3] * inv)};
+                else
+                    *reinterpret_cast<floatx4 *>(a.part_o + (piece * rows_all + R) * D + d0 + i) = x;
             }
         }
-        __syncthreads();                                    // the staged sums are read
+        if (!whole && qi < q1 && d0 == 0) a.part_ml[piece * rows_all + R] = make_float2(RM, L);
+        __syncthreads();                                // the staged sums are read
+    }
+}
+
+// ---------------------------------------------------------------- many query rows
+
+typedef __attribute__((ext_vector_type(16))) float floatx16;
+
+constexpr int kWideRows = 32 * kWaves;
+
+__device__ inline floatx16 mfma32(u32x4 a, u32x4 b, floatx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                   0, 0);
+}
+
+// The same attention where a group has many query rows.  There the vector unit bounds it: every
+// instruction, a matrix one too, takes it for 4 to 5 cycles.  So each wave takes 32 rows with 32 x 32
+// products (half as many instructions), and the workgroup widens a turn's 64 keys and values once,
+// for its four waves: each takes a quarter through its registers into LDS, in the order of the
+// products' operands, while the turn before is worked on.
+//
+// S^T = K Q^T: row p of key tile kt is its key 16 (p / 4 % 2) + 4 (p / 8) + p % 4, so that lane half
+// gh's sixteen scores are those of the keys 16 gh + 0 .. 15 in order, P^T's operand as they stand.
+template <int D, bool F8>
+__global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs a) {
+    constexpr int KS = 64, KT = KS / 32;                    // keys of a turn, and tiles of them
+    constexpr int DS = D / 16, DT = D / 32;                 // k-steps of the first product, component tiles
+    constexpr int EB = F8 ? 1 : 2;
+    constexpr int CPR = D * EB / 16;                        // 16-byte pieces of a key row
+    constexpr int LK = KS * CPR / kThreads;                 // of a turn's keys, of one thread
+    constexpr int CPD = KS * EB / 16, LV = D * CPD / kThreads;  // of a component's values, and of one thread
+    constexpr int kValuesAt = KS * D * 2, kStage = 2 * kValuesAt;
+    __shared__ __attribute__((aligned(16))) char s_stage[2][kStage];
+    __shared__ PageEntry s_page[kThreads];
+    __shared__ uint32_t s_anc[kMaxSeqRows][8];
+    __shared__ int s_up[kMaxSeqRows];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int gh = lane >> 5, l32 = lane & 31;
+    const int grp = a.by_grp.d, rows = a.n_q * grp;
+    const Place w = place_of(a);
+    if (w.b >= a.B) return;
+    const int b = w.b, h = w.h;
+    const int q0 = w.block * kWideRows, q1 = min(q0 + kWideRows, rows);
+    // what the loads below need is known: they go out before the sequence's length is
+    uint32_t id = a.splits == 1 ? table_entry(a, b, 0) : 0u;
+    const int qi = q0 + wave * 32 + l32;                    // this lane's query
+    const bool valid = qi < q1;
+    const int r = quot(a.by_grp, min(qi, q1 - 1));
+    const int64_t R = (static_cast<int64_t>(b) * a.n_q + r) * a.Hq + h * grp + (min(qi, q1 - 1) - r * grp);
+    u32x4 qf[DS];
+#pragma unroll
+    for (int c = 0; c < DS; ++c)
+        qf[c] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.q) + (R * D + c * 16 + gh * 8) * 2);
+    const Seq s = sequence_of(a, b);
+    const Cut cut = cut_of(a, s, q0, q1);
+    if (w.piece >= cut.pieces) return;
+    const int kbeg = w.piece * cut.chunk, kend = min(kbeg + cut.chunk, cut.kend);
+
+    const int P1 = (1 << a.c.log_page) - 1;
+    int first_page = 0, last_page = 0;                      // of those in LDS
+    bool any_none = false;                                  // among them
+    auto page_of = [&](int key) { return s_page[min(key >> a.c.log_page, last_page) - first_page]; };
+    // piece i of this thread: of key row key_at(i) the bytes 16 key_piece(i) .. + 15, and of component
+    // comp_at(i) the keys 16 / EB * comp_piece(i) ..; sixteen lanes side by side take sixteen rows
+    auto key_at = [&](int i) { return ((wave * LK + i) / (CPR / 4)) * 16 + (lane & 15); };
+    auto key_piece = [&](int i) { return (wave * LK + i) % (CPR / 4) * 4 + (lane >> 4); };
+    auto comp_at = [&](int i) { return ((wave * LV + i) / (CPD / 4)) * 16 + (lane & 15); };
+    auto comp_piece = [&](int i) { return (wave * LV + i) % (CPD / 4) * 4 + (lane >> 4); };
+    u32x4 kr[LK], vr[LV];
+    auto load = [&](int k0) {
+#pragma unroll
+        for (int i = 0; i < LK; ++i) {
+            const int key = k0 + key_at(i);
+            const int64_t at = page_of(key).x & ~kNone;
+            kr[i] = *reinterpret_cast<const u32x4 *>(
+                a.c.k + ((at << a.c.log_page) + (key & P1)) * (D * EB) + key_piece(i) * 16);
+        }
+#pragma unroll
+        for (int i = 0; i < LV; ++i) {
+            const int key = k0 + comp_piece(i) * (16 / EB);
+            const int64_t at = page_of(key).x & ~kNone;
+            vr[i] = *reinterpret_cast<const u32x4 *>(
+                a.c.v + (((at * D + comp_at(i)) << a.c.log_page) + (key & P1)) * EB);
+        }
+    };
+    // widened into LDS; values of places that hold no key of the sequence become zeros (such places
+    // may hold anything, as may the scale of a page without one, and a weight of zero does
+    // not make a NaN harmless)
+    auto stage = [&](int k0, char *to) {
+#pragma unroll
+        for (int i = 0; i < LK; ++i) {
+            const int key = key_at(i), k32 = key & 31;
+            const int p = ((k32 >> 2) & 3) * 8 + (k32 >> 4) * 4 + (k32 & 3);
+            char *tile = to + (key >> 5) * (DS * 1024) + p * 16;
+            if constexpr (F8) {
+                const float scale = key_scale(page_of(k0 + key));
+                *reinterpret_cast<u32x4 *>(tile + key_piece(i) * 1024) = widen(kr[i][0], kr[i][1], scale);
+                *reinterpret_cast<u32x4 *>(tile + key_piece(i) * 1024 + 512) = widen(kr[i][2], kr[i][3], scale);
+            } else {
+                *reinterpret_cast<u32x4 *>(tile + (key_piece(i) >> 1) * 1024 + (key_piece(i) & 1) * 512) = kr[i];
+            }
+        }
+        const bool tail = k0 + KS > kend || any_none;
+#pragma unroll
+        for (int i = 0; i < LV; ++i) {
+            const int at = comp_piece(i) * (16 / EB);        // first of the piece's keys
+            const PageEntry page = page_of(k0 + at);
+            float scale = value_scale(page);
+            if (tail) {
+                const int real = page.x >= kNone ? 0 : min(max(kend - (k0 + at), 0), 16 / EB);
+                if (real == 0) scale = 1.f;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    constexpr int EW = 4 / EB;
+                    const int in = real - x * EW;
+                    vr[i][x] &= in >= EW ? 0xffffffffu : in > 0 ? (1u << (in * 8 * EB)) - 1u : 0u;
+                }
+            }
+            const int d = comp_at(i);
+            // operand of component tile d / 32, key tile at / 32, k-step v: keys 16 gh + 8 v ..
+            char *tile = to + kValuesAt + (((d >> 5) * KT + (at >> 5)) * 2) * 1024 + ((d & 31) + 32 * ((at >> 4) & 1)) * 16;
+            if constexpr (F8) {
+                *reinterpret_cast<u32x4 *>(tile) = widen(vr[i][0], vr[i][1], scale);
+                *reinterpret_cast<u32x4 *>(tile + 1024) = widen(vr[i][2], vr[i][3], scale);
+            } else {
+                *reinterpret_cast<u32x4 *>(tile + ((at >> 3) & 1) * 1024) = vr[i];
+            }
+        }
+    };
+    const int segment = kSegment << a.c.log_page;
+    auto look_up = [&](int from, int to, uint32_t entry) {  // of keys [from, to), this thread's table entry given
+        first_page = from >> a.c.log_page;
+        last_page = (to - 1) >> a.c.log_page;
+        const bool in = tid <= last_page - first_page, none = entry >= static_cast<uint32_t>(a.c.n_pages);
+        const uint32_t at = (none ? 0 : entry) * a.c.H + h;
+        if (in) s_page[tid].x = at | (none ? kNone : 0u);
+        uint32_t scales = 0;
+        if (F8 && in) scales = pack_scales(a.c.k_scale[at], a.c.v_scale[at]);
+        any_none = __syncthreads_or(in && none);
+        load(from);
+        if (F8 && in) s_page[tid].y = scales;
+        __syncthreads();
+    };
+    if (a.parent) find_ancestors(a, b, s_anc, s_up);
+
+    // scores are taken as |scale| (+-q) . k, so that the largest product is the largest score
+    const int64_t p_q = s.qs + r;
+    const bool live = valid && p_q >= 0 && p_q < s.end;
+    const int vis = !live ? 0 : a.parent ? s.lc : p_q >= s.lc ? s.end : static_cast<int>(p_q) + 1;   // keys [0, vis) are seen
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int c = 0; c < DS; ++c)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) qf[c][x] = live ? qf[c][x] ^ flip : 0u;
+    int vis_min = live ? vis : INT32_MAX;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) vis_min = min(vis_min, __shfl_xor(vis_min, off));
+    const int clear = uniform(min(vis_min, kend));          // turns that end here or before mask nothing
+    const float sc = fmaxf(fabsf(a.scale) * kLog2eP, 1.17549435e-38f);
+
+    floatx16 o[DT], ol;                                     // sums, and of the weights alone (rows all alike)
+    const u32x4 ones{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        ol[i] = 0.f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[t][i] = 0.f;
+    }
+    float m = -INFINITY;
+
+    for (int seg = kbeg; seg < kend; seg += segment) {
+        const int seg_end = min(seg + segment, kend);
+        if (seg > kbeg || a.splits > 1) id = table_entry(a, b, seg >> a.c.log_page);
+        if (seg > kbeg) __syncthreads();                    // the pages of the segment before are used up
+        look_up(seg, seg_end, id);
+        stage(seg, s_stage[0]);
+        for (int k0 = seg, buf = 0; k0 < seg_end; k0 += KS, buf ^= 1) {
+            const bool more = k0 + KS < seg_end;
+            lds_barrier();                                  // the turn is staged; the one before is used up
+            if (more) load(k0 + KS);
+            const u32x4 *keys = reinterpret_cast<const u32x4 *>(s_stage[buf]) + lane;
+            const u32x4 *values = reinterpret_cast<const u32x4 *>(s_stage[buf] + kValuesAt) + lane;
+            floatx16 st[KT];
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) st[t][i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < DS; ++c)
+#pragma unroll
+                for (int t = 0; t < KT; ++t) st[t] = mfma32(keys[(t * DS + c) * 64], qf[c], st[t]);
+            if (k0 + KS > clear || any_none) {
+#pragma unroll
+                for (int t = 0; t < KT; ++t) {
+                    const int kb = k0 + 32 * t + 16 * gh;   // this lane's first key of the tile
+                    const int real = page_of(kb).x >= kNone ? 0 : min(max(kend - kb, 0), 16);
+                    const int top = min(max(vis - kb, 0), real);
+                    uint32_t see = (1u << top) - 1u;
+                    if (a.parent && live) see |= window16(s_anc[r], kb - s.lc) & ((1u << real) - 1u);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (!(see >> i & 1)) st[t][i] = -INFINITY;
+                }
+            }
+            float bm = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) bm = fmaxf(bm, st[t][i]);
+            {
+                const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
+                bm = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * sc;
+            }
+            const bool raise = bm > m + kLazyRescale;       // always when m is still -inf
+            if (__builtin_expect(__ballot(raise) != 0, 0)) {
+                const float alpha = raise ? __builtin_amdgcn_exp2f(m - bm) : 1.f;   // 0 from -inf
+                if (raise) m = bm;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    ol[i] *= alpha;
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) o[t][i] *= alpha;
+                }
+            }
+            // a query that has seen nothing yet keeps m = -inf and adds nothing
+            const float mm = m == -INFINITY ? INFINITY : m;
+            u32x4 pb[KT][2];
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int v = 0; v < 2; ++v)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        pb[t][v][i] = bf16_pair(__builtin_amdgcn_exp2f(fmaf(st[t][8 * v + 2 * i], sc, -mm)),
+                                                __builtin_amdgcn_exp2f(fmaf(st[t][8 * v + 2 * i + 1], sc, -mm)));
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    ol = mfma32(ones, pb[t][v], ol);
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32(values[((dt * KT + t) * 2 + v) * 64], pb[t][v], o[dt]);
+                }
+            if (more) stage(k0 + KS, s_stage[buf ^ 1]);
+        }
+    }
+
+    if (!valid) return;
+    // O^T tile t, elements 4e .. 4e + 3: d = 32 t + 8 e + 4 gh + 0..3 of this lane's query
+    const float l = live ? ol[0] : 0.f;                     // no query: unmasked turns weighed its zeros evenly
+    if (cut.pieces == 1) {
+        const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;   // NaN stays
+        char *dst = static_cast<char *>(a.out) + (R * D + 4 * gh) * 2;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *reinterpret_cast<u32x2 *>(dst + (32 * t + 8 * e) * 2) =
+                    u32x2{bf16_pair(o[t][4 * e] * inv, o[t][4 * e + 1] * inv), bf16_pair(o[t][4 * e + 2] * inv, o[t][4 * e + 3] * inv)};
+    } else {
+        const int64_t at = w.piece * (static_cast<int64_t>(a.B) * a.n_q * a.Hq) + R;
+        float *po = a.part_o + at * D + 4 * gh;
+        const float f = live ? 1.f : 0.f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *reinterpret_cast<floatx4 *>(po + 32 * t + 8 * e) =
+                    floatx4{o[t][4 * e], o[t][4 * e + 1], o[t][4 * e + 2], o[t][4 * e + 3]} * f;
+        if (gh == 0) a.part_ml[at] = make_float2(live ? m : -INFINITY, l);
     }
 }
 
@@ -432,13 +864,20 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
     const int b = quot(a.by_seq_rows, static_cast<uint32_t>(R));
     const uint32_t pos = quot(a.by_hq, static_cast<uint32_t>(R));
     const int r = pos - static_cast<uint32_t>(b) * a.n_q, hq = static_cast<uint32_t>(R) - pos * a.Hq;
-    const int grp = a.by_grp.d, tile = 16 * a.row_tiles;
+    const int c = lane % LP, sp = lane / LP;
+    // the first pieces' sums are asked for before the sequence's length says how many there are
+    // (what no piece has written is not used)
+    float2 ml = a.part_ml[min(lane, a.splits - 1) * rows_all + R];
+    floatx4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        v[u] = *(reinterpret_cast<const floatx4 *>(a.part_o + (min(u * SP + sp, a.splits - 1) * rows_all + R) * D) + c);
+    const int grp = a.by_grp.d, tile = 16 * a.row_tiles * a.row_waves;
     const int qi = r * grp + hq % grp, q0 = qi / tile * tile;
     const Cut cut = cut_of(a, sequence_of(a, b), q0, min(q0 + tile, a.n_q * grp));
     if (cut.pieces == 1) return;                            // written whole
     const int n = cut.pieces;
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < n) ml = a.part_ml[lane * rows_all + R];
+    if (lane >= n) ml = make_float2(-INFINITY, 0.f);
     float M = ml.x;
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
@@ -446,22 +885,20 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
     float l = w * ml.y;
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off);
-    const int c = lane % LP, sp = lane / LP;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = 0; s0 < n; s0 += SP * U) {
-        floatx4 v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int s = min(s0 + u * SP + sp, n - 1);
-            v[u] = __builtin_nontemporal_load(reinterpret_cast<const floatx4 *>(a.part_o + (s * rows_all + R) * D) + c);
-        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int s = s0 + u * SP + sp;
             const float ws = __shfl(w, s & 63);
-            const bool in = s < n;                          // a clamped piece adds nothing
+            const bool in = s < n;
 #pragma unroll
             for (int k = 0; k < 4; ++k) acc[k] = in ? fmaf(ws, v[u][k], acc[k]) : acc[k];
+        }
+        if (s0 + SP * U < n) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                v[u] = *(reinterpret_cast<const floatx4 *>(a.part_o + (min(s0 + (U + u) * SP + sp, n - 1) * rows_all + R) * D) + c);
         }
     }
 #pragma unroll
@@ -477,12 +914,13 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
 
 template <int D, bool F8>
 void run_attention(const PagedArgs &a, unsigned grid, hipStream_t s) {
-    const dim3 g(grid), t(64 * kWaves);
-    switch (a.row_tiles) {
-    case 1: hipLaunchKernelGGL((k_paged_attention<D, F8, 1>), g, t, 0, s, a); break;
-    case 2: hipLaunchKernelGGL((k_paged_attention<D, F8, 2>), g, t, 0, s, a); break;
-    default: hipLaunchKernelGGL((k_paged_attention<D, F8, 3>), g, t, 0, s, a); break;
-    }
+    const dim3 g(grid), t(kThreads);
+    if (a.row_waves == 4) hipLaunchKernelGGL((k_paged_attention_wide<D, F8>), g, t, 0, s, a);
+    else if (a.row_waves == 2 && a.row_tiles == 3) hipLaunchKernelGGL((k_paged_attention<D, F8, 3, 2>), g, t, 0, s, a);
+    else if (a.row_waves == 2) hipLaunchKernelGGL((k_paged_attention<D, F8, 2, 2>), g, t, 0, s, a);
+    else if (a.row_tiles == 3) hipLaunchKernelGGL((k_paged_attention<D, F8, 3, 1>), g, t, 0, s, a);
+    else if (a.row_tiles == 2) hipLaunchKernelGGL((k_paged_attention<D, F8, 2, 1>), g, t, 0, s, a);
+    else hipLaunchKernelGGL((k_paged_attention<D, F8, 1, 1>), g, t, 0, s, a);
 }
 
 constexpr int64_t kCus = 256;         // compute units of an MI355X
@@ -490,33 +928,38 @@ constexpr int64_t kCus = 256;         // compute units of an MI355X
 }  // namespace
 
 PagedPlan paged_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq) {
-    PagedPlan p{1, 0, 1, static_cast<int64_t>(B) * n_q * Hq};
+    PagedPlan p{1, 1, 0, 1, kMinPiece, static_cast<int64_t>(B) * n_q * Hq};
     const int64_t tiles = (static_cast<int64_t>(n_q) * (Hq / c.H) + 15) / 16;
     if (B <= 0 || tiles == 0) return p;
+    const int64_t groups = static_cast<int64_t>(B) * c.H;
+    if (tiles > 2 * kMaxRowTiles) p.row_waves = 4;
+    else if (tiles > kMaxRowTiles && groups >= kCus) p.row_waves = 2;
     // rows shared out evenly over the fewest workgroups
-    const int64_t blocks = (tiles + kMaxRowTiles - 1) / kMaxRowTiles;
-    p.row_tiles = static_cast<int32_t>((tiles + blocks - 1) / blocks);
-    p.blocks = static_cast<int32_t>((tiles + p.row_tiles - 1) / p.row_tiles);
-    const int64_t units = static_cast<int64_t>(B) * c.H * p.blocks;
-    const int64_t slots = kCus * (p.row_tiles <= 2 ? 2 : 1);
+    const int64_t most = p.row_waves == 4 ? kWideRows / 16 : kMaxRowTiles * p.row_waves, blocks = (tiles + most - 1) / most;
+    p.row_tiles = p.row_waves == 4 ? kWideRows / 64 : static_cast<int32_t>((tiles + blocks * p.row_waves - 1) / (blocks * p.row_waves));
+    p.blocks = static_cast<int32_t>((tiles + p.row_tiles * p.row_waves - 1) / (p.row_tiles * p.row_waves));
+    const int64_t units = groups * p.blocks;
+    p.min_piece = p.row_waves == 4 ? kMinPieceWide : kMinPiece;
+    if (units > kCus / 2) return p;
     const int64_t room = static_cast<int64_t>(c.max_pages) << c.log_page;
-    int64_t splits = slots / units;
-    splits = splits < (room + kMinPiece - 1) / kMinPiece ? splits : (room + kMinPiece - 1) / kMinPiece;
-    p.splits = static_cast<int32_t>(splits < 1 ? 1 : splits > kMaxPieces ? kMaxPieces : splits);
+    p.splits = static_cast<int32_t>(std::min({2 * kCus / units, (room + p.min_piece - 1) / p.min_piece, kMaxPieces}));
+    if (p.splits < 1) p.splits = 1;
     return p;
 }
 
 hipError_t launch_paged_attention(PagedArgs a, const PagedPlan &p, hipStream_t s) {
-    const int64_t units = static_cast<int64_t>(a.B) * a.c.H * p.blocks;
     a.row_tiles = p.row_tiles;
+    a.row_waves = p.row_waves;
     a.splits = p.splits;
+    a.min_piece = p.min_piece;
     a.by_grp = fast_div(a.Hq / a.c.H);
     a.by_blocks = fast_div(p.blocks);
     a.by_heads = fast_div(a.c.H);
     a.by_splits = fast_div(p.splits);
     a.by_seq_rows = fast_div(static_cast<uint32_t>(a.n_q) * static_cast<uint32_t>(a.Hq));
     a.by_hq = fast_div(a.Hq);
-    const unsigned grid = static_cast<unsigned>(units * p.splits);
+    const int64_t turns = (static_cast<int64_t>(a.B) * a.c.H * p.splits + kXcds - 1) / kXcds;
+    const unsigned grid = static_cast<unsigned>(turns * kXcds * p.blocks);
     if (a.c.D == 128) a.c.f8 ? run_attention<128, true>(a, grid, s) : run_attention<128, false>(a, grid, s);
     else a.c.f8 ? run_attention<64, true>(a, grid, s) : run_attention<64, false>(a, grid, s);
     if (p.splits > 1) {

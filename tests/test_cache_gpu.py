@@ -236,7 +236,8 @@ def _check_rows(got, out, size):
     assert (err <= _tolerance(out, size)).all()
 
 
-def _check_hybrid(dtype, D, P, Hq, H, ctx, q_start, n_q, K, T=None, scale=None, seed=0, spoil=None):
+def _check_hybrid(dtype, D, P, Hq, H, ctx, q_start, n_q, K, T=None, scale=None, seed=0, spoil=None,
+                  only=None):
     B = len(ctx)
     need = max(max(c, 0) for c in ctx) + 2 * K + 3
     T = T or (need + P - 1) // P
@@ -253,7 +254,7 @@ def _check_hybrid(dtype, D, P, Hq, H, ctx, q_start, n_q, K, T=None, scale=None, 
     got = cs.hybrid_attention_paged(q.to(DEV), cache, table.to(DEV), i32(ctx), i32(q_start), K, scale)
     torch.cuda.synchronize()
     host = _host(cache)
-    for b in range(B):
+    for b in only or range(B):
         sees = torch.tensor(ref.hybrid_sees(ctx[b], q_start[b], n_q, K, room))
         mask = torch.arange(lengths[b]) < sees[:, None]
         out, size = ref.attention(q[b], host.of("k", table[b], lengths[b]), host.of("v", table[b], lengths[b]), mask,
@@ -309,6 +310,21 @@ def test_hybrid_room_cuts_the_input():
 def test_hybrid_long_in_pieces(dtype):
     # cut over the keys, lengths that end inside a piece, one far shorter sequence
     _check_hybrid(dtype, 128, 64, 8, 2, [3001, 40, 2047], [3001, 40, 2047], 9, 3, seed=6)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("B,n_q,Hq", [(17, 1, 8), (32, 13, 32), (17, 25, 32)])
+def test_hybrid_more_pages_than_are_looked_up_at_once(dtype, B, n_q, Hq):
+    # groups enough that nothing is cut, more than 252 pages each: few rows, 52 and 100 of a group
+    ctx = [4100 - 31 * (b % 5) for b in range(B)]
+    _check_hybrid(dtype, 64, 16, Hq, 8, ctx, ctx, n_q, 3, seed=B, only=[0, B - 1])
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("n_q,Hq", [(3, 2), (40, 8), (140, 2)])
+def test_hybrid_pieces_of_many_rows(dtype, n_q, Hq):
+    # cut over the keys with few rows, 160 of a group, and context queries that see some pieces only
+    _check_hybrid(dtype, 128, 32, Hq, 2, [1900, 700], [1850, 640], n_q, 7, seed=n_q)
 
 
 @pytest.mark.parametrize("dtype", [F8, BF16])
@@ -483,11 +499,11 @@ def test_a_round_on_the_cache(dtype):
 def test_calls_replay_from_a_hip_graph():
     """Append and attention captured once; every replay sees the inputs of its moment."""
     B, H, Hq, D, P, n = 2, 2, 8, 128, 64, 7
-    table, n_pages = ref.make_table(B, 6, 3)
-    cache = _filled(table, n_pages, H, D, P, F8, [300, 70], 3, junk=False)
+    table, n_pages = ref.make_table(B, 30, 3)
+    cache = _filled(table, n_pages, H, D, P, F8, [1700, 70], 3, junk=False)
     tab = table.to(DEV)
     g = _gen(4)
-    start = torch.tensor([300, 70], dtype=torch.int32, device=DEV)
+    start = torch.tensor([1700, 70], dtype=torch.int32, device=DEV)
     k, v, q = (torch.randn(B, n, h, D, generator=g).to(BF16).to(DEV) for h in (H, H, Hq))
     inv = (10000.0 ** (-torch.arange(0, D, 2).double() / D)).float().to(DEV)
     app = cs.prepare_cache_append(cache, tab, start, k, v, inv_freq=inv, q=q)
@@ -505,7 +521,7 @@ def test_calls_replay_from_a_hip_graph():
     for i in range(4):
         k.copy_(torch.randn(B, n, H, D, generator=g).to(BF16))
         q.copy_(torch.randn(B, n, Hq, D, generator=g).to(BF16))
-        start.copy_(torch.tensor([300 - i, 70 + i], dtype=torch.int32))
+        start.copy_(torch.tensor([1700 - i, 70 + i], dtype=torch.int32))
         graph.replay()
         torch.cuda.synchronize()
         first = att.outputs["out"].clone()
