@@ -28,7 +28,7 @@ struct AppendArgs {
     char *q_out;
     // set by the launch: page workgroups ahead of the query ones, and their divisions
     uint32_t page_wgs;
-    FastDiv by_pages, by_heads, by_n;
+    FastDiv by_pages, by_heads, by_n, by_chunks[9];   // by_chunks: by 1 .. 8, sixteen-place chunks of a page
 };
 
 struct KeepArgs {
