@@ -473,8 +473,8 @@ cospec_status cospec_hybrid_attention_ws(const void *q, const void *k, const voi
  *  table      [B][max_pages] int32.  An entry outside [0, n_pages) is no page: nothing is
  *             written there and its positions are not attended.  Entries of pages past a
  *             sequence's positions are not used.
- * Sequences may share pages that are only read; a page that a call writes must belong to
- * one sequence (two sequences writing one page leave unspecified values in it).
+ * Sequences may share pages that are only read; a page that a call writes must stand once in the
+ * tables (written through two entries it is left with unspecified values).
  */
 typedef struct {
     cospec_dtype dtype;
@@ -553,8 +553,8 @@ cospec_status cospec_cache_keep(const cospec_cache *cache, const int32_t *ctx_le
  * this is plain decoding of the last of l_c positions.
  *  q    [B][n_q][Hq][d] bf16; Hq a multiple of cache->heads; out the same shape.  A query
  *       outside [0, l), or that sees only positions on no page, gets zeros.
- * fp32 sums; the attention weights enter the second product rounded to bf16; e4m3 keys and
- * values times their scale are taken exactly.
+ * fp32 sums; the attention weights enter the second product, and their sum, rounded to bf16;
+ * e4m3 keys and values times their scale are taken exactly.
  *  workspace  256-byte aligned, at least cospec_paged_attention_workspace_size(cache, B, n_q,
  *             Hq) bytes (0: none is needed, and NULL will do): few query groups are
  *             cut into pieces of their keys, by each sequence's own length, and merged by

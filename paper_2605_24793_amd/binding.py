@@ -744,6 +744,13 @@ def _tokens(t: torch.Tensor, B: int, n: int, d: int, what: str) -> int:
     return int(ld)
 
 
+def _i32_kept(t: torch.Tensor, n: int, what: str) -> torch.Tensor:
+    """_i32, for a call that reads the tensor anew at every launch: no copy of it will do."""
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return _i32(t, n, what)
+
+
 def prepare_cache_append(cache: PagedCache, table, start, k, v, count: Optional[torch.Tensor] = None,
                          inv_freq: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
                          interleaved: bool = False, q: Optional[torch.Tensor] = None) -> CacheCall:
@@ -758,9 +765,9 @@ def prepare_cache_append(cache: PagedCache, table, start, k, v, count: Optional[
     if k.shape[2] != cache.heads or v.shape[2] != cache.heads:
         raise ValueError(f"k and v must have the cache's {cache.heads} heads")
     cs = cache._struct(table, B)
-    start = _i32(start, B, "start")
+    start = _i32_kept(start, B, "start")
     if count is not None:
-        count = _i32(count, B, "count")
+        count = _i32_kept(count, B, "count")
     if positions is not None and (tuple(positions.shape) != (B, n) or positions.dtype != torch.int32
                                   or not positions.is_contiguous()):
         raise ValueError("positions must be contiguous int32 [B, n]")
@@ -796,7 +803,7 @@ def prepare_cache_keep(cache: PagedCache, table, ctx_len, path) -> CacheCall:
         raise ValueError("path must be contiguous int32 [B, N]")
     B, N = int(path.shape[0]), int(path.shape[1])
     cs = cache._struct(table, B)
-    ctx = _i32(ctx_len, B, "ctx_len")
+    ctx = _i32_kept(ctx_len, B, "ctx_len")
     _same_device(cache.k, ctx, path)
     return CacheCall(lib().cospec_cache_keep, (ctypes.byref(cs), _ptr(ctx), _ptr(path), B, N), {}, cache.k.device,
                      [cache, table, ctx, path, cs])
@@ -812,7 +819,7 @@ def _attention_call(fn, q, cache, table, ctx_len, more, K, scale) -> CacheCall:
         raise ValueError(f"q must be contiguous bf16 [B, n, Hq, {cache.d}]")
     B, n, Hq = int(q.shape[0]), int(q.shape[1]), int(q.shape[2])
     cs = cache._struct(table, B)
-    ctx = _i32(ctx_len, B, "ctx_len")
+    ctx = _i32_kept(ctx_len, B, "ctx_len")
     _same_device(cache.k, q, ctx, more)
     out = torch.empty_like(q)
     ws_bytes = lib().cospec_paged_attention_workspace_size(ctypes.byref(cs), B, n, Hq)
@@ -826,7 +833,7 @@ def prepare_hybrid_attention_paged(q, cache: PagedCache, table, ctx_len, q_start
     q_start[b] .. q_start[b] + n_q - 1 against the cache, under the arbitrator's hybrid mask;
     outputs["out"] has q's shape."""
     return _attention_call(lib().cospec_hybrid_attention_paged, q, cache, table, ctx_len,
-                           _i32(q_start, int(q.shape[0]), "q_start"), (int(K),), scale)
+                           _i32_kept(q_start, int(q.shape[0]), "q_start"), (int(K),), scale)
 
 
 def hybrid_attention_paged(q, cache: PagedCache, table, ctx_len, q_start, K: int, scale: float) -> torch.Tensor:

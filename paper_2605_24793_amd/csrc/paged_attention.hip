@@ -43,9 +43,11 @@ constexpr int kSegment = 252;         // pages looked up at a time: with one mor
 constexpr int kStep = 64;             // keys of a wave's turn, at most
 // 16-row tiles of a workgroup, at most: what the registers hold of queries, scores and sums
 constexpr int kMaxRowTiles = 3;
-constexpr int kMinPiece = 512;        // keys of a piece, at least
+// Keys of a piece, at least.  One token at 15000 positions: pieces of 256 17.6 us, 512 15.0, 1024 17.0; with many rows
+// (196 of a group at 4687) 25.7, 24.3 and 33.5.
+constexpr int kMinPiece = 512;
 constexpr int kMinPieceWide = 256;
-constexpr int64_t kMaxPieces = 64;        // of a group's keys (the merge weighs them in one wave)
+constexpr int64_t kMaxPieces = 64;    // of a group's keys (the join weighs them in one wave)
 constexpr float kLog2eP = 1.4426950408889634f;
 constexpr float kLazyRescale = 8.0f;  // log2 units a block's max may exceed the running max by
 
@@ -216,6 +218,15 @@ __device__ inline uint32_t table_entry(const PagedArgs &a, int b, int first) {
 
 // RW waves of the four share the keys, each with RT row tiles of its own; the 4 / RW sets of them
 // take turns at the keys.
+//
+// A round of 64 sequences at 1536 to 2065 positions, 32/8 heads, D = 128, e4m3 (68 rows a group, 255 MB, 32 GFLOP):
+// 64.5 us, 3.9 TB/s.  Its vector and matrix instructions share one issue port and fill 70% of the
+// time a wave is there; a workgroup starts to work some 8 us after its launch, and
+// sequences of different lengths leave 1.4 waves per SIMD on average.  Measured on the way: keys and values in
+// registers with no LDS 114, through LDS (a wave's next turn in flight without a register) 87, 48 rows a wave
+// and no branch to choose a page 77, two waves sharing keys 69, the weights' sum by the matrix
+// cores and raised priority there 65.  64 single tokens at about 3600 positions (471 MB): 86 us, 5.5 TB/s.
+// A fifth row tile per wave spills (190 us); a wave alone on its SIMD, whatever its rows, is slower than two.
 template <int D, bool F8, int RT, int RW>
 __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
     constexpr int DS = D / 32;                              // k-steps of the first product
@@ -599,6 +610,13 @@ __device__ inline floatx16 mfma32(u32x4 a, u32x4 b, floatx16 c) {
 // for its four waves: each takes a quarter through its registers into LDS, in the order of the
 // products' operands, while the turn before is worked on.
 //
+// Whole inputs of 4 x 1820 to 2063 positions, 32/8 heads, D = 128, e4m3 (121 GFLOP): 160 us, 757 TFLOP/s; trees of
+// 60 nodes after 64 contexts of 1536 to 2048 (113 GFLOP) 161 us.  The LDS reads of the operands bound it, 1 KB a product
+// of 32 cycles, 128 bytes a cycle for the four SIMDs at full rate: without them the same code takes 116 to 125 us, without
+// staging 124 to 132, without the products 139 to 145, without the exponentials 150.  Measured and not
+// taken: 16 x 16 products 163 to 175, each wave widening for itself 170, products and weights interleaved by
+// scheduling groups 157 to 168, 32-key turns with three workgroups a CU 165 to 178, 64 rows a wave spills.
+//
 // S^T = K Q^T: row p of key tile kt is its key 16 (p / 4 % 2) + 4 (p / 8) + p % 4, so that lane half
 // gh's sixteen scores are those of the keys 16 gh + 0 .. 15 in order, P^T's operand as they stand.
 template <int D, bool F8>
@@ -933,6 +951,7 @@ PagedPlan paged_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq) {
     if (B <= 0 || tiles == 0) return p;
     const int64_t groups = static_cast<int64_t>(B) * c.H;
     if (tiles > 2 * kMaxRowTiles) p.row_waves = 4;
+    // 68 rows in 512 groups: two waves sharing keys 64.5 us, two workgroups 77; in 16 groups 45 and 29.8
     else if (tiles > kMaxRowTiles && groups >= kCus) p.row_waves = 2;
     // rows shared out evenly over the fewest workgroups
     const int64_t most = p.row_waves == 4 ? kWideRows / 16 : kMaxRowTiles * p.row_waves, blocks = (tiles + most - 1) / most;
@@ -940,6 +959,9 @@ PagedPlan paged_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq) {
     p.blocks = static_cast<int32_t>((tiles + p.row_tiles * p.row_waves - 1) / (p.row_tiles * p.row_waves));
     const int64_t units = groups * p.blocks;
     p.min_piece = p.row_waves == 4 ? kMinPieceWide : kMinPiece;
+    // Cut only while that fills CUs: each has two workgroups then.  16 x 8 groups in two blocks, 1037
+    // positions: uncut 17.3 us, in two pieces 24.6; 8 x 17 blocks, 515 positions 19.1 and 27.6; 16 groups in two
+    // blocks, 16401 positions: 8 pieces 35.0, 16 pieces 29.8.
     if (units > kCus / 2) return p;
     const int64_t room = static_cast<int64_t>(c.max_pages) << c.log_page;
     p.splits = static_cast<int32_t>(std::min({2 * kCus / units, (room + p.min_piece - 1) / p.min_piece, kMaxPieces}));

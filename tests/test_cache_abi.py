@@ -180,6 +180,7 @@ def test_binding_checks_shapes_before_the_library():
         lambda: cs.cache_append(cache, table, z, k, k[:, :3]),
         lambda: cs.cache_append(cache, table, z, k.transpose(1, 2).contiguous().transpose(1, 2), k),
         lambda: cs.cache_append(cache, table, z, k, k, count=z[:2]),
+        lambda: cs.cache_append(cache, table, fake(6, dtype=torch.int32)[::2], k, k),  # every launch reads it anew
         lambda: cs.cache_append(cache, table, z, k, k, positions=z),
         lambda: cs.cache_append(cache, table, z, k, k, inv_freq=fake(32)),
         lambda: cs.cache_append(cache, table, z, k, k, q=q[..., :32]),

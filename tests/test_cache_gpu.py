@@ -222,10 +222,11 @@ def test_append_again_changes_nothing_more():
 # ----------------------------------------------------------------------------- attention
 
 def _tolerance(out, size):
-    # a weight enters the second product off by at most half a bf16 step (2^-8 of it), the
-    # result is stored off by at most 2^-8 of it; scores in fp32: D + 4 roundings of at most
-    # sum |q k| scale < 20, twice (numerator and denominator), below 4e-4
-    return (2.0 ** -8 + 4e-4) * size + 2.0 ** -8 * out.abs() + 1e-30
+    # with weights off by e_j, |e_j| <= 2^-8 (half a bf16 step), in the product and in their sum alike,
+    # out is off by sum(w_j e_j (v_j - out)) / (1 + sum(w_j e_j)) <= 2^-8 (size + |out|) to first order,
+    # size = sum(w |v|); the result is stored off by at most 2^-8 of it.  Scores in fp32: D + 4
+    # roundings of at most sum |q k| scale < 20, on both sides of the quotient, below 4e-4.
+    return (2.0 ** -8 + 4e-4) * (size + out.abs()) + 2.0 ** -8 * out.abs() + 1e-30
 
 
 def _check_rows(got, out, size):
@@ -338,6 +339,17 @@ def test_hybrid_entries_that_name_no_page(dtype):
     def spoil(table):
         table[0, 1], table[1, 0], table[2, :] = -1, 2 ** 30, -7
     _check_hybrid(dtype, 128, 16, 4, 2, [60, 10, 30, 50], [60, 0, 30, 50], 13, 5, seed=8, spoil=spoil)
+
+
+def test_scales_count_by_their_power_of_two():
+    table, n_pages = ref.make_table(2, 3, 4)
+    cache = _filled(table, n_pages, 2, 64, 32, F8, [90, 40], 4)
+    q = torch.randn(2, 5, 4, 64, generator=_gen(5)).to(BF16).to(DEV)
+    ctx = torch.tensor([85, 35], dtype=torch.int32, device=DEV)
+    want = cs.hybrid_attention_paged(q, cache, table.to(DEV), ctx, ctx, 1, 0.125)
+    cache.k_scale.mul_(1.75)
+    cache.v_scale.mul_(1.25)
+    assert _same(cs.hybrid_attention_paged(q, cache, table.to(DEV), ctx, ctx, 1, 0.125), want)
 
 
 def _check_tree(dtype, D, P, Hq, H, ctx, parent, T=None, seed=0):
