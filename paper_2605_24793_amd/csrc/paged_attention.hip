@@ -127,11 +127,15 @@ __device__ inline uint32_t window16(const uint32_t *set, int at) {
 
 // 16 bytes per lane from global memory into LDS at byte lds + 16 * lane, lds the same in every
 // lane.  Written as assembly, so that the compiler, which knows nothing of these loads, places no
-// wait for them before LDS reads; the kernel's own waits order them.
+// wait for them before LDS reads; the kernel's own waits order them.  ONCE: read once, not to be kept in
+// the caches.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-__device__ inline void load_lds16(const char *src, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(src) : "memory", "m0");
+template <bool ONCE> __device__ inline void load_lds16(const char *src, uint32_t lds) {
+    if constexpr (ONCE)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" : : "s"(lds), "v"(src) : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(src) : "memory", "m0");
 }
 #pragma clang diagnostic pop
 
@@ -225,9 +229,9 @@ __device__ inline uint32_t table_entry(const PagedArgs &a, int b, int first) {
 // sequences of different lengths leave 1.4 waves per SIMD on average.  Measured on the way: keys and values in
 // registers with no LDS 114, through LDS (a wave's next turn in flight without a register) 87, 48 rows a wave
 // and no branch to choose a page 77, two waves sharing keys 69, the weights' sum by the matrix
-// cores and raised priority there 65.  64 single tokens at about 3600 positions (471 MB): 86 us, 5.5 TB/s.
+// cores and raised priority there 65.  64 single tokens at about 3600 positions (471 MB): 80 us, 5.9 TB/s.
 // A fifth row tile per wave spills (190 us); a wave alone on its SIMD, whatever its rows, is slower than two.
-template <int D, bool F8, int RT, int RW>
+template <int D, bool F8, int RT, int RW, bool ONCE = false>
 __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
     constexpr int DS = D / 32;                              // k-steps of the first product
     constexpr int DT = D / 16;                              // d tiles of the second
@@ -308,7 +312,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
 #pragma unroll
         for (int i = 0; i < NK / RW; ++i) {
             const int e = rw * (NK / RW) + i;
-            load_lds16(base + (e / KC) * 4 * (D * EB) + (e % KC) * 64, at + e * 1024);
+            load_lds16<ONCE>(base + (e / KC) * 4 * (D * EB) + (e % KC) * 64, at + e * 1024);
         }
     };
     const int64_t v_tile = (static_cast<int64_t>(16) << a.c.log_page) * EB;
@@ -319,7 +323,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
 #pragma unroll
         for (int i = 0; i < NV / RW; ++i) {
             const int e = rw * (NV / RW) + i;
-            load_lds16(base + (e / VC) * v_tile + (e % VC) * 16, at + kValuesAt + e * 1024);
+            load_lds16<ONCE>(base + (e / VC) * v_tile + (e % VC) * 16, at + kValuesAt + e * 1024);
         }
     };
     constexpr int kTurn = KW * KS;                          // keys of all sets' turns
@@ -930,6 +934,12 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
     }
 }
 
+// Up to 16 rows of a group, whose keys are read by one workgroup only: not kept in the caches where every
+// load takes whole 64-byte runs of keys and of values, as with e4m3 pages of 64 places.  64 single tokens
+// at about 3600 positions: kept 86.4 us, not kept 80.1; pages of 128, 128 tokens 168.6 and 191.7 (the
+// other half of a run is fetched again); of 16, 48 tokens 76.5 and 77.3; bf16 178 and 202.
+constexpr int kNontemporalPage = 6;   // log2 of its places
+
 template <int D, bool F8>
 void run_attention(const PagedArgs &a, unsigned grid, hipStream_t s) {
     const dim3 g(grid), t(kThreads);
@@ -938,6 +948,7 @@ void run_attention(const PagedArgs &a, unsigned grid, hipStream_t s) {
     else if (a.row_waves == 2) hipLaunchKernelGGL((k_paged_attention<D, F8, 2, 2>), g, t, 0, s, a);
     else if (a.row_tiles == 3) hipLaunchKernelGGL((k_paged_attention<D, F8, 3, 1>), g, t, 0, s, a);
     else if (a.row_tiles == 2) hipLaunchKernelGGL((k_paged_attention<D, F8, 2, 1>), g, t, 0, s, a);
+    else if (F8 && a.c.log_page == kNontemporalPage) hipLaunchKernelGGL((k_paged_attention<D, F8, 1, 1, F8>), g, t, 0, s, a);
     else hipLaunchKernelGGL((k_paged_attention<D, F8, 1, 1>), g, t, 0, s, a);
 }
 
