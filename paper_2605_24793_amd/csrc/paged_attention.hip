@@ -79,11 +79,9 @@ __device__ inline u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
 // A value that is the same in every lane, for the scalar registers.
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// Loads through the scalar cache, of what no kernel writes while this one runs.
+// A load through the scalar cache, of what no kernel writes while this one runs.
 typedef __attribute__((address_space(4))) const int const_int;
-typedef __attribute__((address_space(4))) const float const_float;
 __device__ inline int scalar_load(const int32_t *p) { return *(const_int *)reinterpret_cast<uintptr_t>(p); }
-__device__ inline float scalar_load(const float *p) { return *(const_float *)reinterpret_cast<uintptr_t>(p); }
 
 // What the queries of sequence b see.  Hybrid: position p < lc sees [0, p], lc <= p < end sees
 // [0, end).  Tree: node r sees [0, lc) and its ancestors among lc .. end - 1.
@@ -960,21 +958,30 @@ PagedPlan paged_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq) {
     PagedPlan p{1, 1, 0, 1, kMinPiece, static_cast<int64_t>(B) * n_q * Hq};
     const int64_t tiles = (static_cast<int64_t>(n_q) * (Hq / c.H) + 15) / 16;
     if (B <= 0 || tiles == 0) return p;
-    const int64_t groups = static_cast<int64_t>(B) * c.H;
-    if (tiles > 2 * kMaxRowTiles) p.row_waves = 4;
-    // 68 rows in 512 groups: two waves sharing keys 64.5 us, two workgroups 77; in 16 groups 45 and 29.8
-    else if (tiles > kMaxRowTiles && groups >= kCus) p.row_waves = 2;
-    // rows shared out evenly over the fewest workgroups
-    const int64_t most = p.row_waves == 4 ? kWideRows / 16 : kMaxRowTiles * p.row_waves, blocks = (tiles + most - 1) / most;
-    p.row_tiles = p.row_waves == 4 ? kWideRows / 64 : static_cast<int32_t>((tiles + blocks * p.row_waves - 1) / (blocks * p.row_waves));
-    p.blocks = static_cast<int32_t>((tiles + p.row_tiles * p.row_waves - 1) / (p.row_tiles * p.row_waves));
+    const int64_t groups = static_cast<int64_t>(B) * c.H, room = static_cast<int64_t>(c.max_pages) << c.log_page;
+    const int64_t pieces = (room + kMinPiece - 1) / kMinPiece;
+    int64_t per_block = 0;                                  // row tiles of a workgroup
+    // Small calls: as few rows a workgroup as give every CU at most one, cut over the keys too.  One
+    // sequence of 317 positions, 68 rows a group: 16 rows 8.0 us, 32 10.2, 48 13.1; a tree of 38 nodes after 1000
+    // positions 12.5, 13.8 and 15.6; two sequences of 2017 positions 16.8, 15.2 and 17.7.
+    for (int rt = 1; rt <= kMaxRowTiles && !per_block; ++rt)
+        if (groups * ((tiles + rt - 1) / rt) * pieces <= kCus) per_block = p.row_tiles = rt;
+    if (!per_block) {
+        if (tiles > 2 * kMaxRowTiles) p.row_waves = 4;
+        // 68 rows in 512 groups: two waves sharing keys 64.5 us, two workgroups 77; in 16 groups 45 and 29.8
+        else if (tiles > kMaxRowTiles && groups >= kCus) p.row_waves = 2;
+        // rows shared out evenly over the fewest workgroups
+        const int64_t most = p.row_waves == 4 ? kWideRows / 16 : kMaxRowTiles * p.row_waves, blocks = (tiles + most - 1) / most;
+        p.row_tiles = p.row_waves == 4 ? kWideRows / 64 : static_cast<int32_t>((tiles + blocks * p.row_waves - 1) / (blocks * p.row_waves));
+        per_block = p.row_tiles * p.row_waves;
+    }
+    p.blocks = static_cast<int32_t>((tiles + per_block - 1) / per_block);
     const int64_t units = groups * p.blocks;
     p.min_piece = p.row_waves == 4 ? kMinPieceWide : kMinPiece;
     // Cut only while that fills CUs: each has two workgroups then.  16 x 8 groups in two blocks, 1037
     // positions: uncut 17.3 us, in two pieces 24.6; 8 x 17 blocks, 515 positions 19.1 and 27.6; 16 groups in two
     // blocks, 16401 positions: 8 pieces 35.0, 16 pieces 29.8.
     if (units > kCus / 2) return p;
-    const int64_t room = static_cast<int64_t>(c.max_pages) << c.log_page;
     p.splits = static_cast<int32_t>(std::min({2 * kCus / units, (room + p.min_piece - 1) / p.min_piece, kMaxPieces}));
     if (p.splits < 1) p.splits = 1;
     return p;

@@ -237,16 +237,23 @@ def _check_rows(got, out, size):
     assert (err <= _tolerance(out, size)).all()
 
 
+def _longer(table, columns):
+    """The table with more entries behind, which name no page: room for long sequences, which the
+    kernels' work split goes by as long as it does not know better."""
+    return torch.cat([table, torch.full((table.shape[0], columns), -1, dtype=torch.int32)], 1)
+
+
 def _check_hybrid(dtype, D, P, Hq, H, ctx, q_start, n_q, K, T=None, scale=None, seed=0, spoil=None,
-                  only=None):
+                  only=None, more=0):
     B = len(ctx)
     need = max(max(c, 0) for c in ctx) + 2 * K + 3
     T = T or (need + P - 1) // P
     table, n_pages = ref.make_table(B, T, seed)
-    room = T * P
-    lengths = [min(max(c, 0) + 2 * K + 3, room) for c in ctx]
+    lengths = [min(max(c, 0) + 2 * K + 3, T * P) for c in ctx]
     if spoil:
         spoil(table)
+    table = _longer(table, more)
+    room = table.shape[1] * P
     cache = _filled(table, n_pages, H, D, P, dtype, lengths, seed)
     g = _gen(seed + 1)
     q = torch.randn(B, n_q, Hq, D, generator=g).to(BF16)
@@ -272,8 +279,9 @@ def _check_hybrid(dtype, D, P, Hq, H, ctx, q_start, n_q, K, T=None, scale=None, 
     (64, 32, 16, 2, [64, 200], 13, 5),            # 104 rows a group
     (128, 32, 8, 1, [40, 321], 23, 10),           # 184 rows
 ])
-def test_hybrid_region(dtype, D, P, Hq, H, ctx, n_q, K):
-    _check_hybrid(dtype, D, P, Hq, H, ctx, ctx, n_q, K, seed=n_q)
+@pytest.mark.parametrize("more", [0, 3000])
+def test_hybrid_region(dtype, D, P, Hq, H, ctx, n_q, K, more):
+    _check_hybrid(dtype, D, P, Hq, H, ctx, ctx, n_q, K, seed=n_q, more=more)
 
 
 @pytest.mark.parametrize("dtype", [F8, BF16])
@@ -283,24 +291,30 @@ def test_hybrid_single_token(dtype, D, ctx):
 
 
 @pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("more", [0, 3000])
 @pytest.mark.parametrize("D,P", [(128, 32), (64, 128)])
-def test_hybrid_whole_input(dtype, D, P):
+def test_hybrid_whole_input(dtype, D, P, more):
     # every position, and padding rows behind the shorter sequence
-    _check_hybrid(dtype, D, P, 4, 2, [70, 23], [0, 0], 79, 3, seed=3)
+    _check_hybrid(dtype, D, P, 4, 2, [70, 23], [0, 0], 79, 3, seed=3, more=more)
+    _check_hybrid(dtype, D, P, 4, 2, [330, 140], [0, 0], 345, 6, seed=4, more=more)
 
 
 @pytest.mark.parametrize("dtype", [F8, BF16])
-def test_hybrid_queries_outside(dtype):
-    # before position 0, across its border, past the end, a negative context, nothing at all
-    _check_hybrid(dtype, 128, 16, 4, 2, [40, 40, 40, -5, 12], [-9, -3, 45, 0, 1000], 8, 2, seed=4)
+@pytest.mark.parametrize("n_q,Hq,more", [(8, 4, 0), (8, 24, 3000), (60, 8, 3000)])
+def test_hybrid_queries_outside(dtype, n_q, Hq, more):
+    # before position 0, across its border, past the end, a negative context, nothing at all; few rows a
+    # group, 96 and 240
+    _check_hybrid(dtype, 128, 16, Hq, 2, [40, 40, 40, -5, 12], [-9, -3, 45, 0, 1000], n_q, 2, seed=4, more=more)
 
 
 @pytest.mark.parametrize("dtype", [F8, BF16])
 @pytest.mark.parametrize("D", [64, 128])
 def test_hybrid_padding_beside_long_rows(dtype, D):
     # padding rows in workgroups whose other rows see whole turns of keys, cut and uncut
-    _check_hybrid(dtype, D, 32, 2, 2, [300, 150], [270, 120], 80, 4, seed=12)
-    _check_hybrid(dtype, D, 32, 1, 1, [900], [880], 90, 4, seed=13)
+    for more in (0, 3000):
+        _check_hybrid(dtype, D, 32, 2, 2, [300, 150], [270, 120], 80, 4, seed=12, more=more)
+        _check_hybrid(dtype, D, 32, 1, 1, [900], [880], 90, 4, seed=13, more=more)
+        _check_hybrid(dtype, D, 32, 2, 1, [900, 333], [880, 200], 150, 4, seed=14, more=more)
 
 
 def test_hybrid_room_cuts_the_input():
@@ -323,22 +337,35 @@ def test_hybrid_more_pages_than_are_looked_up_at_once(dtype, B, n_q, Hq):
 
 @pytest.mark.parametrize("dtype", [F8, BF16])
 @pytest.mark.parametrize("n_q,Hq", [(3, 2), (40, 8), (140, 2)])
-def test_hybrid_pieces_of_many_rows(dtype, n_q, Hq):
+@pytest.mark.parametrize("more", [0, 3000])
+def test_hybrid_pieces_of_many_rows(dtype, n_q, Hq, more):
     # cut over the keys with few rows, 160 of a group, and context queries that see some pieces only
-    _check_hybrid(dtype, 128, 32, Hq, 2, [1900, 700], [1850, 640], n_q, 7, seed=n_q)
+    _check_hybrid(dtype, 128, 32, Hq, 2, [1900, 700], [1850, 640], n_q, 7, seed=n_q, more=more)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("D,P,n_q,K", [(128, 64, 13, 5), (128, 16, 17, 7), (64, 32, 24, 2), (128, 128, 22, 0)])
+def test_hybrid_of_many_groups(dtype, D, P, n_q, K):
+    # 256 groups of 52 to 96 rows: waves that share their keys, padding and context queries among the rows
+    B = 32
+    ctx = [30 + 67 * (b % 4) for b in range(B)]
+    start = [c - 3 * (b % 3) for b, c in enumerate(ctx)]
+    _check_hybrid(dtype, D, P, 32, 8, ctx, start, n_q, K, seed=n_q, only=[0, 1, 2, 7], more=40)
 
 
 @pytest.mark.parametrize("dtype", [F8, BF16])
 @pytest.mark.parametrize("scale", [-0.1, 0.0, 0.9])
-def test_hybrid_scales(dtype, scale):
-    _check_hybrid(dtype, 64, 32, 4, 2, [90, 33], [90, 33], 5, 1, scale=scale, seed=7)
+@pytest.mark.parametrize("n_q", [5, 70])
+def test_hybrid_scales(dtype, scale, n_q):
+    _check_hybrid(dtype, 64, 32, 4, 2, [90, 33], [50, 13], n_q, 1, scale=scale, seed=7, more=3000)
 
 
 @pytest.mark.parametrize("dtype", [F8, BF16])
 def test_hybrid_entries_that_name_no_page(dtype):
     def spoil(table):
         table[0, 1], table[1, 0], table[2, :] = -1, 2 ** 30, -7
-    _check_hybrid(dtype, 128, 16, 4, 2, [60, 10, 30, 50], [60, 0, 30, 50], 13, 5, seed=8, spoil=spoil)
+    for n_q, Hq, more in ((13, 4, 0), (13, 12, 3000), (70, 6, 3000)):
+        _check_hybrid(dtype, 128, 16, Hq, 2, [60, 10, 30, 50], [60, 0, 30, 50], n_q, 5, seed=8, spoil=spoil, more=more)
 
 
 def test_scales_count_by_their_power_of_two():
@@ -352,19 +379,20 @@ def test_scales_count_by_their_power_of_two():
     assert _same(cs.hybrid_attention_paged(q, cache, table.to(DEV), ctx, ctx, 1, 0.125), want)
 
 
-def _check_tree(dtype, D, P, Hq, H, ctx, parent, T=None, seed=0):
+def _check_tree(dtype, D, P, Hq, H, ctx, parent, T=None, seed=0, more=0, only=None):
     B, N = len(ctx), len(parent[0])
     T = T or (max(max(c, 0) for c in ctx) + N + P - 1) // P
     table, n_pages = ref.make_table(B, T, seed)
-    room = T * P
+    room = (T + more) * P
     lengths = [min(max(c, 0) + N, room) for c in ctx]
     cache = _filled(table, n_pages, H, D, P, dtype, lengths, seed)
+    table = _longer(table, more)
     q = torch.randn(B, N, Hq, D, generator=_gen(seed + 1)).to(BF16)
     i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
     got = cs.tree_attention(q.to(DEV), cache, table.to(DEV), i32(ctx), i32(parent), D ** -0.5)
     torch.cuda.synchronize()
     host = _host(cache)
-    for b in range(B):
+    for b in only or range(B):
         lc = max(ctx[b], 0)
         mask = torch.zeros(N, lengths[b], dtype=torch.bool)
         mask[:, :min(lc, room)] = True
@@ -384,15 +412,25 @@ def _random_tree(N, seed, near=None):
 @pytest.mark.parametrize("dtype", [F8, BF16])
 @pytest.mark.parametrize("D,P,Hq,H,ctx,N", [(128, 64, 8, 2, [50, 0, 333], 33), (64, 16, 3, 3, [7, 16], 60),
                                             (128, 128, 4, 1, [700], 256), (64, 32, 8, 2, [5], 1)])
-def test_tree(dtype, D, P, Hq, H, ctx, N):
-    _check_tree(dtype, D, P, Hq, H, ctx, [_random_tree(N, b, near=6) for b in range(len(ctx))], seed=N)
+@pytest.mark.parametrize("more", [0, 3000])
+def test_tree(dtype, D, P, Hq, H, ctx, N, more):
+    _check_tree(dtype, D, P, Hq, H, ctx, [_random_tree(N, b, near=6) for b in range(len(ctx))], seed=N, more=more)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("D,N", [(128, 13), (64, 24), (128, 60)])
+def test_tree_of_many_groups(dtype, D, N):
+    # 256 groups of 52, 96 and 240 rows
+    ctx = [25 + 41 * (b % 5) for b in range(32)]
+    _check_tree(dtype, D, 32, 32, 8, ctx, [_random_tree(N, b, near=5) for b in range(32)], seed=N, more=40, only=[1, 4, 31])
 
 
 @pytest.mark.parametrize("N", [2, 65, 256])
 def test_tree_shapes(N):
     # a path, a star, and parents that break the rule (the node itself, later ones, none)
     bad = [n - 1 if n % 5 else (n, n + 3, -4, 10 ** 6)[n % 4] for n in range(N)]
-    _check_tree(F8, 64, 32, 4, 2, [20, 61, 90], [list(range(-1, N - 1)), [-1] + [0] * (N - 1), bad], seed=N)
+    for more in (0, 3000):
+        _check_tree(F8, 64, 32, 4, 2, [20, 61, 90], [list(range(-1, N - 1)), [-1] + [0] * (N - 1), bad], seed=N, more=more)
 
 
 @pytest.mark.parametrize("dtype", [F8, BF16])
