@@ -548,13 +548,15 @@ cospec_status cospec_cache_keep(const cospec_cache *cache, const int32_t *ctx_le
 
 /*
  * cospec_hybrid_attention over the cache: the same mask, for the positions the cache holds
- * (l = l_c + 2K + 3, at most max_pages * page).  Positions [0, l) that a query may see must hold
- * finite keys and values; what stands past them is not used.  With n_q = 1, q_start = l_c - 1
- * this is plain decoding of the last of l_c positions.
+ * (l = l_c + 2K + 3, at most max_pages * page).  With n_q = 1, q_start = l_c - 1 this is plain
+ * decoding of the last of l_c positions.  What a query sees must be finite, else its result is
+ * unspecified; what it does not see does not reach it, whatever it holds (a place never
+ * written, a page that has no scale yet).
  *  q    [B][n_q][Hq][d] bf16; Hq a multiple of cache->heads; out the same shape.  A query
  *       outside [0, l), or that sees only positions on no page, gets zeros.
  * fp32 sums; the attention weights enter the second product, and their sum, rounded to bf16;
- * e4m3 keys and values times their scale are taken exactly.
+ * e4m3 keys and values times their scale are taken exactly (scales by their power of two, of
+ * more than 2^119 as 2^119).
  *  workspace  256-byte aligned, at least cospec_paged_attention_workspace_size(cache, B, n_q,
  *             Hq) bytes (0: none is needed, and NULL will do): few query groups are
  *             cut into pieces of their keys, by each sequence's own length, and merged by

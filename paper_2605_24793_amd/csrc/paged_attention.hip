@@ -114,6 +114,20 @@ __device__ inline Cut cut_of(const PagedArgs &a, const Seq &s, int q0, int q1) {
     return Cut{kend, chunk, max((kend + chunk - 1) / chunk, 1)};
 }
 
+// Keys [0, result) of a piece's [.., kend) are seen by every row of [q0, q1) that sees any.
+__device__ inline int seen_by_all(const PagedArgs &a, const Seq &s, int q0, int kend) {
+    if (a.parent) return min(s.lc, kend);
+    const int64_t p = max(s.qs + quot(a.by_grp, q0), static_cast<int64_t>(0));
+    return p >= s.lc ? kend : min(static_cast<int>(p) + 1, kend);
+}
+
+// Four bytes of values with those that are not finite made zero: among keys that some rows see and others
+// do not, a weight of zero would not keep them from the others.
+template <bool F8> __device__ inline uint32_t finite(uint32_t x) {
+    const uint32_t top = F8 ? ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+    return x & ~(top | (top - (top >> (F8 ? 7 : 15))));
+}
+
 // The sixteen bits from bit `at` (may be negative) of a set of 256.
 __device__ inline uint32_t window16(const uint32_t *set, int at) {
     if (at <= -16 || at >= 256) return 0;
@@ -206,8 +220,11 @@ __device__ inline Place place_of(const PagedArgs &a) {
 typedef uint2 PageEntry;
 constexpr uint32_t kNone = 0x80000000u;
 
+// (448 times 2^119 is still finite as bf16: no scale, of a page in use or not, makes a zero or a finite
+// value anything else)
 __device__ inline uint32_t pack_scales(float k, float v) {
-    return (__float_as_uint(k) & 0x7f800000u) | (__float_as_uint(v) & 0x7f800000u) >> 16;
+    const uint32_t most = 0x7b000000u;
+    return min(__float_as_uint(k) & 0x7f800000u, most) | min(__float_as_uint(v) & 0x7f800000u, most) >> 16;
 }
 __device__ inline float key_scale(PageEntry e) { return __uint_as_float(e.y & 0xffff0000u); }
 __device__ inline float value_scale(PageEntry e) { return __uint_as_float(e.y << 16); }
@@ -330,23 +347,19 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
 
     // Scores are taken as |scale| (+-q) . k, so that the largest product is the largest score.
     int vis[RT];                                            // keys [0, vis) are seen
-    int vis_min = INT32_MAX;
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const int64_t p = s.qs + node[rt];
         const bool live = q0 + (rw * RT + rt) * 16 + l16 < q1 && p >= 0 && p < s.end;
         vis[rt] = !live ? 0 : a.parent ? s.lc : p >= s.lc ? s.end : static_cast<int>(p) + 1;
-        if (live) vis_min = min(vis_min, vis[rt]);
-        else node[rt] = -1;
+        if (!live) node[rt] = -1;
 #pragma unroll
         for (int c = 0; c < DS; ++c)
 #pragma unroll
             for (int w = 0; w < 4; ++w) qf[rt][c][w] = live ? qf[rt][c][w] ^ flip : 0u;
     }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) vis_min = min(vis_min, __shfl_xor(vis_min, off));
-    const int clear = uniform(min(vis_min, kend));          // turns that end here or before mask nothing
+    const int clear = seen_by_all(a, s, q0, kend);          // turns that end here or before mask nothing
 
     floatx4 o[RT][DT];
     float m[RT];
@@ -393,7 +406,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
             }
             const float ksc = key_scale(page_of(k0 + kg * GK));
             const PageEntry page_v = page_of(k0 + g * GK);
-            float vsc = value_scale(page_v);
+            const float vsc = value_scale(page_v);
             const bool none = page_v.x >= kNone;
             // wave-uniform: a key that some query does not see, or that does not exist
             const bool masked = k0 + KS > clear || __ballot(none) != 0;
@@ -476,23 +489,33 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
                 else wait_vm<0>();
             }
             if (masked) {
-                // places that hold no key of the sequence may hold anything, as may the scale of a
-                // page without one: a weight of zero does not make a NaN harmless
+                // places that hold no key of the sequence may hold anything: a weight of zero does not make
+                // a NaN harmless
                 const int real = none ? 0 : min(max(kend - (k0 + g * GK), 0), GK);
-                if (real == 0) vsc = 1.f;
+                const bool some_see = k0 + KS > clear && clear < kend;
 #pragma unroll
-                for (int c = 0; c < VC; ++c)
+                for (int c = 0; c < VC; ++c) {
+                    u32x4 keep;
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
                         constexpr int EW = 4 / EB;              // elements of a word
                         const int in = real - (c * 4 + w) * EW;
-                        const uint32_t keep = in >= EW ? 0xffffffffu : in > 0 ? (1u << (in * 8 * EB)) - 1u : 0u;
-#pragma unroll
-                        for (int t = 0; t < DT; ++t) {          // waves that share the turn store the same
-                            uint32_t *word = reinterpret_cast<uint32_t *>(values + (t * VC + c) * 64) + w;
-                            *word &= keep;
-                        }
+                        keep[w] = in >= EW ? 0xffffffffu : in > 0 ? (1u << (in * 8 * EB)) - 1u : 0u;
                     }
+                    // waves that share the turn store the same, and each word once
+                    if (some_see) {
+#pragma unroll
+                        for (int t = 0; t < DT; ++t) {
+                            u32x4 x = values[(t * VC + c) * 64] & keep;
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) x[w] = finite<F8>(x[w]);
+                            values[(t * VC + c) * 64] = x;
+                        }
+                    } else {
+#pragma unroll
+                        for (int t = 0; t < DT; ++t) values[(t * VC + c) * 64] &= keep;
+                    }
+                }
             }
             u32x4 pb[RT][NU];
 #pragma unroll
@@ -544,7 +567,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
     // join the sets
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const bool live = node[rt] >= 0;                    // else unmasked turns weighed its zeros evenly
+        const bool live = node[rt] >= 0;                    // else unmasked turns gave it some weights
         if (!live) m[rt] = -INFINITY;
         if (g == 0) s_ml[wave][rt * 16 + l16] = make_float2(m[rt], live ? ol[rt][0] : 0.f);
     }
@@ -562,7 +585,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
         const float f = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[rt] - M);
 #pragma unroll
         for (int t = 0; t < DT; ++t)
-            *reinterpret_cast<floatx4 *>(s_o + (wave * 16 + l16) * OS + t * 16 + g * 4) = o[rt][t] * f;
+            *reinterpret_cast<floatx4 *>(s_o + (wave * 16 + l16) * OS + t * 16 + g * 4) = node[rt] >= 0 ? o[rt][t] * f : floatx4{0.f, 0.f, 0.f, 0.f};
         __syncthreads();
         const int qi = q0 + (rw_ * RT + rt) * 16 + row;
         float RM = -INFINITY, L = 0.f;
@@ -656,6 +679,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs 
     const Cut cut = cut_of(a, s, q0, q1);
     if (w.piece >= cut.pieces) return;
     const int kbeg = w.piece * cut.chunk, kend = min(kbeg + cut.chunk, cut.kend);
+    const int all_see = seen_by_all(a, s, q0, kend);        // keys below are seen by every row that sees any
 
     const int P1 = (1 << a.c.log_page) - 1;
     int first_page = 0, last_page = 0;                      // of those in LDS
@@ -685,8 +709,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs 
         }
     };
     // widened into LDS; values of places that hold no key of the sequence become zeros (such places
-    // may hold anything, as may the scale of a page without one, and a weight of zero does
-    // not make a NaN harmless)
+    // may hold anything, and a weight of zero does not make a NaN harmless)
     auto stage = [&](int k0, char *to) {
 #pragma unroll
         for (int i = 0; i < LK; ++i) {
@@ -701,20 +724,20 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs 
                 *reinterpret_cast<u32x4 *>(tile + (key_piece(i) >> 1) * 1024 + (key_piece(i) & 1) * 512) = kr[i];
             }
         }
-        const bool tail = k0 + KS > kend || any_none;
+        const bool some_see = k0 + KS > all_see && all_see < kend, special = some_see || k0 + KS > kend || any_none;
 #pragma unroll
         for (int i = 0; i < LV; ++i) {
             const int at = comp_piece(i) * (16 / EB);        // first of the piece's keys
             const PageEntry page = page_of(k0 + at);
-            float scale = value_scale(page);
-            if (tail) {
+            const float scale = value_scale(page);
+            if (special) {
                 const int real = page.x >= kNone ? 0 : min(max(kend - (k0 + at), 0), 16 / EB);
-                if (real == 0) scale = 1.f;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     constexpr int EW = 4 / EB;
                     const int in = real - x * EW;
                     vr[i][x] &= in >= EW ? 0xffffffffu : in > 0 ? (1u << (in * 8 * EB)) - 1u : 0u;
+                    if (some_see) vr[i][x] = finite<F8>(vr[i][x]);
                 }
             }
             const int d = comp_at(i);
@@ -848,7 +871,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs 
 
     if (!valid) return;
     // O^T tile t, elements 4e .. 4e + 3: d = 32 t + 8 e + 4 gh + 0..3 of this lane's query
-    const float l = live ? ol[0] : 0.f;                     // no query: unmasked turns weighed its zeros evenly
+    const float l = live ? ol[0] : 0.f;                     // no query: unmasked turns gave it some weights
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = live ? o[t][i] : 0.f;
     if (cut.pieces == 1) {
         const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;   // NaN stays
         char *dst = static_cast<char *>(a.out) + (R * D + 4 * gh) * 2;
@@ -861,13 +888,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs 
     } else {
         const int64_t at = w.piece * (static_cast<int64_t>(a.B) * a.n_q * a.Hq) + R;
         float *po = a.part_o + at * D + 4 * gh;
-        const float f = live ? 1.f : 0.f;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 *reinterpret_cast<floatx4 *>(po + 32 * t + 8 * e) =
-                    floatx4{o[t][4 * e], o[t][4 * e + 1], o[t][4 * e + 2], o[t][4 * e + 3]} * f;
+                    floatx4{o[t][4 * e], o[t][4 * e + 1], o[t][4 * e + 2], o[t][4 * e + 3]};
         if (gh == 0) a.part_ml[at] = make_float2(live ? m : -INFINITY, l);
     }
 }

@@ -440,6 +440,123 @@ def test_tree_room_cuts_the_nodes(dtype):
 
 # ---------------------------------------------------------------------------------- keep
 
+# What a query does not see is not to reach it, whatever it holds: bit by bit the result with good values there.
+
+def _spoil(cache, table, b, positions, how):
+    """Bad keys and values at positions of sequence b, and for "scales" a bad scale of their pages as well
+    (whose every position must be among them, or past the sequence)."""
+    nan = {"nan": math.nan, "inf": math.inf, "scales": 1.0}[how]
+    for p in positions:
+        pid, place = int(table[b, p // cache.page]), p % cache.page
+        for x, at in ((cache.k, (pid, slice(None), place)), (cache.v, (pid, slice(None), slice(None), place))):
+            good = x[at].float()
+            good[..., 3::7] = nan
+            x[at] = good.to(x.dtype)
+        if how == "scales":
+            cache.k_scale[pid], cache.v_scale[pid] = math.inf, math.inf
+
+
+def _check_unseen(attend, cache, table, masks, bad, how):
+    """masks[b] [n, length]: what the queries see; bad[b]: positions to spoil."""
+    want = attend()
+    for b, positions in enumerate(bad):
+        _spoil(cache, table, b, positions, how)
+    got = attend()
+    torch.cuda.synchronize()
+    for b, positions in enumerate(bad):
+        hit = masks[b][:, positions].any(1)
+        assert 0 < int((~hit).sum()), "some query sees none of them"
+        assert torch.equal(got[b][~hit].float(), want[b][~hit].float())
+
+
+def _hows(dtype):
+    return ("nan", "scales") if dtype == F8 else ("nan", "inf")
+
+
+# few rows, spread out; 58 and 90 rows in many groups; up to 45 in some; over 200 in one group, and in some
+_ROWS = [(1, 4, 2, 1, 0), (1, 8, 2, 3, 0), (32, 16, 8, 1, 40), (4, 8, 8, 1, 3000), (1, 8, 1, 1, 3000), (4, 16, 8, 5, 3000)]
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("D,P", [(128, 32), (64, 16), (128, 128)])
+@pytest.mark.parametrize("B,Hq,H,times,more", _ROWS)
+@pytest.mark.parametrize("how", [0, 1])
+def test_tree_nodes_not_seen(dtype, D, P, B, Hq, H, times, more, how):
+    # the nodes behind the first 20, at the start of a page, and some before them, hold nothing good
+    N = 20 * times + 9
+    ctx = [3 * P - 20 * times] * B if 3 * P > 20 * times else [7 * P - 20 * times] * B
+    T = (max(ctx) + N + P - 1) // P
+    table, n_pages = ref.make_table(B, T, 5)
+    cache = _filled(table, n_pages, H, D, P, dtype, [c + N for c in ctx], 5)
+    parent = [_random_tree(20 * times, b, near=4) + [0] * 9 for b in range(B)]
+    q = torch.randn(B, N, Hq, D, generator=_gen(6)).to(BF16).to(DEV)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    args = (q, cache, _longer(table, more).to(DEV), i32(ctx), i32(parent), D ** -0.5)
+    masks, bad = [], []
+    for b in range(B):
+        mask = torch.zeros(N, ctx[b] + N, dtype=torch.bool)
+        mask[:, :ctx[b]] = True
+        mask[:, ctx[b]:] = ref.ancestors(parent[b])
+        masks.append(mask)
+        bad.append(list(range(ctx[b] + 20 * times, ctx[b] + N)) + ([ctx[b] + 9, ctx[b] + 13] if how == 0 else []))
+    _check_unseen(lambda: cs.tree_attention(*args), cache, table, masks, bad, _hows(dtype)[how])
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("D,P", [(128, 32), (64, 16), (128, 128)])
+@pytest.mark.parametrize("B,Hq,H,times,more", _ROWS)
+@pytest.mark.parametrize("how", [0, 1])
+def test_hybrid_positions_not_seen(dtype, D, P, B, Hq, H, times, more, how):
+    # context queries, padding behind them, and positions after the first of them that hold nothing good
+    n_q, K = 20 * times + 25, 3
+    ctx = [2 * P + 20 * times] * B
+    T = (max(ctx) + 2 * K + 3 + P - 1) // P
+    table, n_pages = ref.make_table(B, T, 7)
+    lengths = [c + 2 * K + 3 for c in ctx]
+    cache = _filled(table, n_pages, H, D, P, dtype, lengths, 7)
+    start = [2 * P - 3] * B
+    q = torch.randn(B, n_q, Hq, D, generator=_gen(8)).to(BF16).to(DEV)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    args = (q, cache, _longer(table, more).to(DEV), i32(ctx), i32(start), K, D ** -0.5)
+    sees = torch.tensor(ref.hybrid_sees(ctx[0], start[0], n_q, K, T * P))
+    masks = [torch.arange(lengths[0]) < sees[:, None]] * B
+    first = [2 * P + (0 if how else 7 + b % 5) for b in range(B)]
+    bad = [list(range(f, lengths[b])) if how else [f, f + 5] for b, f in enumerate(first)]
+    _check_unseen(lambda: cs.hybrid_attention_paged(*args), cache, table, masks, bad, _hows(dtype)[how])
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("more", [0, 3000])
+def test_hybrid_not_seen_where_pages_are_looked_up_anew(dtype, more):
+    # positions on both sides of the 252nd page, which waves share (52 rows a group) or not
+    for B in (1, 32):
+        ctx, K, n_q, P = [252 * 16 + 9] * B, 2, 13, 16
+        T = (ctx[0] + 2 * K + 3 + P - 1) // P
+        table, n_pages = ref.make_table(B, T, 9)
+        lengths = [c + 2 * K + 3 for c in ctx]
+        cache = _filled(table, n_pages, 8, 64, P, dtype, lengths, 9)
+        q = torch.randn(B, n_q, 32, 64, generator=_gen(10)).to(BF16).to(DEV)
+        start = [252 * 16 - 6] * B
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+        args = (q, cache, _longer(table, more).to(DEV), i32(ctx), i32(start), K, 0.125)
+        sees = torch.tensor(ref.hybrid_sees(ctx[0], start[0], n_q, K, T * P))
+        masks = [torch.arange(lengths[0]) < sees[:, None]] * B
+        bad = [[252 * 16 - 4 + b % 3, 252 * 16 + 2 + b % 2] for b in range(B)]
+        _check_unseen(lambda: cs.hybrid_attention_paged(*args), cache, table, masks, bad, "nan")
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("Hq,n_q,more", [(8, 9, 0), (8, 9, 3000), (16, 60, 3000)])
+def test_padding_beside_bad_values_gets_zeros(dtype, Hq, n_q, more):
+    table, n_pages = ref.make_table(1, 8, 3)
+    cache = _filled(table, n_pages, 2, 64, 64, dtype, [409], 3)
+    _spoil(cache, table, 0, [5, 70, 200, 405], "nan")
+    q = torch.randn(1, n_q, Hq, 64, generator=_gen(4)).to(BF16).to(DEV)
+    at = torch.tensor([400], dtype=torch.int32, device=DEV)
+    got = cs.hybrid_attention_paged(q, cache, _longer(table, more).to(DEV), at, at + 5, 3, 0.125)
+    assert not got[0, 4:].float().ne(0).any()
+
+
 def _check_keep(dtype, D, P, H, ctx, path, N, T=None, seed=0):
     B = len(ctx)
     T = T or (max(max(c, 0) for c in ctx) + N + P - 1) // P
