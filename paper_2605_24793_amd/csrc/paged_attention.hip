@@ -239,7 +239,7 @@ __device__ inline uint32_t table_entry(const PagedArgs &a, int b, int first) {
 // take turns at the keys.
 //
 // A round of 64 sequences at 1536 to 2065 positions, 32/8 heads, D = 128, e4m3 (68 rows a group, 255 MB, 32 GFLOP):
-// 64.5 us, 3.9 TB/s.  Its vector and matrix instructions share one issue port and fill 70% of the
+// 65.7 us, 3.9 TB/s.  Its vector and matrix instructions share one issue port and fill 70% of the
 // time a wave is there; a workgroup starts to work some 8 us after its launch, and
 // sequences of different lengths leave 1.4 waves per SIMD on average.  Measured on the way: keys and values in
 // registers with no LDS 114, through LDS (a wave's next turn in flight without a register) 87, 48 rows a wave
@@ -636,9 +636,10 @@ __device__ inline floatx16 mfma32(u32x4 a, u32x4 b, floatx16 c) {
 // products' operands, while the turn before is worked on.
 //
 // Whole inputs of 4 x 1820 to 2063 positions, 32/8 heads, D = 128, e4m3 (121 GFLOP): 160 us, 757 TFLOP/s; trees of
-// 60 nodes after 64 contexts of 1536 to 2048 (113 GFLOP) 161 us.  The LDS reads of the operands bound it, 1 KB a product
-// of 32 cycles, 128 bytes a cycle for the four SIMDs at full rate: without them the same code takes 116 to 125 us, without
-// staging 124 to 132, without the products 139 to 145, without the exponentials 150.  Measured and not
+// 60 nodes after 64 contexts of 1536 to 2048 (113 GFLOP) 164 us.  No pipe is full: matrix instructions take 36% of
+// the time, vector ones 31% on the same port, the LDS reads of the operands (1 KB a product of 32 cycles) 43%; the
+// waits between them bound it.  Without those reads the same code takes 116 to 125 us, without staging 124 to 132,
+// without the products 139 to 145, without the exponentials 150.  Measured and not
 // taken: 16 x 16 products 163 to 175, each wave widening for itself 170, products and weights interleaved by
 // scheduling groups 157 to 168, 32-key turns with three workgroups a CU 165 to 178, 64 rows a wave spills.
 //
