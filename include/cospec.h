@@ -65,7 +65,8 @@ typedef enum {
     COSPEC_OK = 0,
     COSPEC_ERR_INVALID_ARG = -1,  /* null/misaligned pointer, bad size, NaN lambda ... */
     COSPEC_ERR_UNSUPPORTED = -2,  /* K, N or split count above the documented maximum,
-                                     or a logit row (V * element bytes) over 2^31 - 1 B */
+                                     a logit row (V * element bytes) over 2^31 - 1 B, or
+                                     a paged cache or call on it beyond what a launch holds */
     COSPEC_ERR_WORKSPACE = -3,    /* workspace missing, misaligned or too small         */
     COSPEC_ERR_HIP = -4,          /* a HIP call or kernel launch failed                 */
     COSPEC_ERR_SCRATCH_LIMIT = -5 /* cospec_verify_block_static: the sizes need more than

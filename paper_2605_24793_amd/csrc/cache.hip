@@ -19,7 +19,6 @@ typedef __attribute__((ext_vector_type(2))) float floatx2;
 
 constexpr int kCacheThreads = 256;
 constexpr int kMaxPage = 128;
-constexpr int kQueryTokens = 8;       // tokens of a query workgroup
 // new tokens of a page whose values are stored one by one: 64 x 1 token 7.5 us so and 8.0 by sixteen
 // places, 64 x 4 9.3 and 8.8
 constexpr int kFewTokens = 2;
@@ -530,8 +529,7 @@ template <int D, bool F8> void run_append(const AppendArgs &a, unsigned grid, si
 }  // namespace
 
 hipError_t launch_cache_append(AppendArgs a, hipStream_t s) {
-    // pages a sequence's n positions can touch, wherever they start
-    const int64_t pages = ((static_cast<int64_t>(a.n) + (1 << a.c.log_page) - 2) >> a.c.log_page) + 1;
+    const int64_t pages = pages_touched(a.n, a.c.log_page);
     const int64_t page_wgs = a.B * pages * a.c.H;
     const int64_t query_wgs = a.q ? (static_cast<int64_t>(a.B) * a.n + kQueryTokens - 1) / kQueryTokens : 0;
     a.page_wgs = static_cast<uint32_t>(page_wgs);

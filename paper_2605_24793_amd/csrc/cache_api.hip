@@ -76,6 +76,7 @@ cospec_status attend(PagedArgs &a, const cospec_cache *cache, void *workspace, s
     if (!given(a.q, 16) || !given(a.out, 16) || !given(a.ctx_len, 4)) return COSPEC_ERR_INVALID_ARG;
     a.c = page_args(cache);
     const PagedPlan p = paged_plan(a.c, a.B, a.n_q, a.Hq);
+    if (p.grid > kMaxWorkgroups) return COSPEC_ERR_UNSUPPORTED;
     if (p.splits > 1) {
         if (!given(workspace, kAlign) || workspace_bytes < plan_bytes(p, a.c.D)) return COSPEC_ERR_WORKSPACE;
         a.part_o = static_cast<float *>(workspace);
@@ -112,11 +113,12 @@ cospec_status cospec_cache_append(const cospec_cache *cache, const int32_t *star
     if (!given(k, 16) || !given(v, 16) || !given(start, 4) || (count && !aligned(count, 4)) ||
         (positions && !aligned(positions, 4)) || (q && (!aligned(q, 16) || !given(q_out, 16))))
         return COSPEC_ERR_INVALID_ARG;
-    const int64_t pages = (static_cast<int64_t>(n) + 2 * cache->page) / cache->page;
-    if (static_cast<int64_t>(B) * n > INT32_MAX / 2 || pages * cache->heads > INT32_MAX / 2 / B ||
-        static_cast<int64_t>(Hq) * cache->d > INT32_MAX / 16)
-        return COSPEC_ERR_UNSUPPORTED;
     a.c = page_args(cache);
+    const int64_t per_sequence = pages_touched(n, a.c.log_page) * cache->heads;
+    const int64_t query_groups = q ? (static_cast<int64_t>(B) * n + kQueryTokens - 1) / kQueryTokens : 0;
+    if (static_cast<int64_t>(B) * n > INT32_MAX / 2 || per_sequence > kMaxWorkgroups / B ||
+        per_sequence * B + query_groups > kMaxWorkgroups || static_cast<int64_t>(Hq) * cache->d > INT32_MAX / 16)
+        return COSPEC_ERR_UNSUPPORTED;
     a.start = start; a.count = count; a.positions = positions;
     a.k = static_cast<const char *>(k); a.v = static_cast<const char *>(v); a.q = static_cast<const char *>(q);
     a.ld_k = ld_k; a.ld_v = ld_v; a.ld_q = ld_q;
@@ -130,7 +132,7 @@ cospec_status cospec_cache_keep(const cospec_cache *cache, const int32_t *ctx_le
     cospec_status st = check_cache_sizes(cache);
     if (st != COSPEC_OK) return st;
     if (B < 0 || N < 1) return COSPEC_ERR_INVALID_ARG;
-    if (N > COSPEC_MAX_N || cache->heads > INT32_MAX / 4 / (B > 0 ? B : 1)) return COSPEC_ERR_UNSUPPORTED;
+    if (N > COSPEC_MAX_N || cache->heads > kMaxWorkgroups / 2 / (B > 0 ? B : 1)) return COSPEC_ERR_UNSUPPORTED;
     if (B == 0) return COSPEC_OK;
     if ((st = check_cache(cache)) != COSPEC_OK) return st;
     if (!given(ctx_len, 4) || !given(path, 4)) return COSPEC_ERR_INVALID_ARG;

@@ -9,6 +9,9 @@
 
 namespace cospec {
 
+// Workgroups of a launch, at most: a grid holds fewer than 2^32 threads, and they have 256.
+constexpr int64_t kMaxWorkgroups = (1 << 24) - 1;
+
 // Keys [n_pages][H][P][D], values [n_pages][H][D][P], P = 1 << log_page.
 struct PageArgs {
     char *k, *v;
@@ -60,7 +63,13 @@ struct PagedArgs {
 struct PagedPlan {
     int32_t row_tiles, row_waves, blocks, splits, min_piece;   // blocks: workgroups that share a group's rows
     int64_t rows;                        // B * n_q * Hq
+    int64_t grid;                        // workgroups
 };
+
+// Pages that a sequence's n new positions can touch, wherever they start.
+inline int64_t pages_touched(int64_t n, int32_t log_page) { return ((n + (1 << log_page) - 2) >> log_page) + 1; }
+
+constexpr int kQueryTokens = 8;          // tokens of a workgroup that rotates queries
 
 PagedPlan paged_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq);
 hipError_t launch_cache_append(AppendArgs a, hipStream_t s);

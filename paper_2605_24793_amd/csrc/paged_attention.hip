@@ -982,7 +982,7 @@ constexpr int64_t kCus = 256;         // compute units of an MI355X
 }  // namespace
 
 PagedPlan paged_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq) {
-    PagedPlan p{1, 1, 0, 1, kMinPiece, static_cast<int64_t>(B) * n_q * Hq};
+    PagedPlan p{1, 1, 0, 1, kMinPiece, static_cast<int64_t>(B) * n_q * Hq, 0};
     const int64_t tiles = (static_cast<int64_t>(n_q) * (Hq / c.H) + 15) / 16;
     if (B <= 0 || tiles == 0) return p;
     const int64_t groups = static_cast<int64_t>(B) * c.H, room = static_cast<int64_t>(c.max_pages) << c.log_page;
@@ -1008,9 +1008,10 @@ PagedPlan paged_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq) {
     // Cut only while that fills CUs: each has two workgroups then.  16 x 8 groups in two blocks, 1037
     // positions: uncut 17.3 us, in two pieces 24.6; 8 x 17 blocks, 515 positions 19.1 and 27.6; 16 groups in two
     // blocks, 16401 positions: 8 pieces 35.0, 16 pieces 29.8.
-    if (units > kCus / 2) return p;
-    p.splits = static_cast<int32_t>(std::min({2 * kCus / units, (room + p.min_piece - 1) / p.min_piece, kMaxPieces}));
-    if (p.splits < 1) p.splits = 1;
+    if (units <= kCus / 2)
+        p.splits = static_cast<int32_t>(std::max<int64_t>(
+            std::min({2 * kCus / units, (room + p.min_piece - 1) / p.min_piece, kMaxPieces}), 1));
+    p.grid = (groups * p.splits + kXcds - 1) / kXcds * kXcds * p.blocks;     // each XCD takes as many
     return p;
 }
 
@@ -1025,8 +1026,7 @@ hipError_t launch_paged_attention(PagedArgs a, const PagedPlan &p, hipStream_t s
     a.by_splits = fast_div(p.splits);
     a.by_seq_rows = fast_div(static_cast<uint32_t>(a.n_q) * static_cast<uint32_t>(a.Hq));
     a.by_hq = fast_div(a.Hq);
-    const int64_t turns = (static_cast<int64_t>(a.B) * a.c.H * p.splits + kXcds - 1) / kXcds;
-    const unsigned grid = static_cast<unsigned>(turns * kXcds * p.blocks);
+    const unsigned grid = static_cast<unsigned>(p.grid);
     if (a.c.D == 128) a.c.f8 ? run_attention<128, true>(a, grid, s) : run_attention<128, false>(a, grid, s);
     else a.c.f8 ? run_attention<64, true>(a, grid, s) : run_attention<64, false>(a, grid, s);
     if (p.splits > 1) {

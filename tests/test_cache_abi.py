@@ -104,6 +104,16 @@ def test_attention_refuses(call, kw, code):
     assert call(cs.lib(), **kw) == code
 
 
+@pytest.mark.parametrize("call,kw", [
+    (_append, dict(B=1 << 21, n=1)), (_append, dict(B=1 << 18, n=129, cache=_cache(page=16))),
+    (_append, dict(cache=_cache(heads=1), B=1 << 24, n=8, q=FAKE, Hq=1, ld_q=128, q_out=FAKE)),
+    (_keep, dict(B=1 << 20)), (_hybrid, dict(B=1 << 21, n=1)), (_tree, dict(B=1 << 21, N=5)),
+])
+def test_more_workgroups_than_a_launch_holds(call, kw):
+    # 2^24 workgroups of 256 threads and more: refused, not left to the launch
+    assert call(cs.lib(), **kw) == UNSUPPORTED
+
+
 def test_workspace_size():
     L = cs.lib()
 
