@@ -7,7 +7,7 @@
 // joined the same way.
 //
 // Work split: the query rows (position x head) that share a key/value head of a sequence form
-// a group.  A workgroup takes rows of a group; with up to 48 of them (96 in many groups) its waves
+// a group.  A workgroup takes rows of a group; with up to 48 of them (96 of many groups' workgroups) its waves
 // take turns at the group's keys (k_paged_attention): a wave's keys and values of a turn go from the
 // pages into LDS of its own with loads that pass no register, each lane's operands where the
 // lane reads them back, so that the wave has its next turn under way without a barrier, and the
@@ -25,6 +25,7 @@
 // e4m3: v_cvt_scalef32_pk_bf16_fp8 widens two elements and applies the page's power of two;
 // e4m3 has fewer bits than bf16, so nothing is rounded, and one conversion serves all rows.
 #include <algorithm>
+#include <type_traits>
 
 #include "paged.h"
 
@@ -239,12 +240,12 @@ __device__ inline uint32_t table_entry(const PagedArgs &a, int b, int first) {
 // take turns at the keys.
 //
 // A round of 64 sequences at 1536 to 2065 positions, 32/8 heads, D = 128, e4m3 (68 rows a group, 255 MB, 32 GFLOP):
-// 65.7 us, 3.9 TB/s.  Its vector and matrix instructions share one issue port and fill 70% of the
+// 61.5 us, 4.1 TB/s.  Its vector and matrix instructions share one issue port and fill 70% of the
 // time a wave is there; a workgroup starts to work some 8 us after its launch, and
 // sequences of different lengths leave 1.4 waves per SIMD on average.  Measured on the way: keys and values in
 // registers with no LDS 114, through LDS (a wave's next turn in flight without a register) 87, 48 rows a wave
 // and no branch to choose a page 77, two waves sharing keys 69, the weights' sum by the matrix
-// cores and raised priority there 65.  64 single tokens at about 3600 positions (471 MB): 80 us, 5.9 TB/s.
+// cores and raised priority there 65.7, no turns for a tile without rows 61.5.  64 single tokens at about 3600 positions (471 MB): 80 us, 5.9 TB/s.
 // A fifth row tile per wave spills (190 us); a wave alone on its SIMD, whatever its rows, is slower than two.
 template <int D, bool F8, int RT, int RW, bool ONCE = false>
 __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
@@ -373,196 +374,207 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
         for (int t = 0; t < DT; ++t) o[rt][t] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
     const float sc = fmaxf(fabsf(a.scale) * kLog2eP, 1.17549435e-38f);
-    for (int seg = kbeg; seg < kend; seg += segment) {
-        const int seg_end = min(seg + segment, kend);
-        if (seg > kbeg || a.splits > 1) id = table_entry(a, b, seg >> a.c.log_page);
-        if (seg > kbeg) __syncthreads();                    // the pages of the segment before are used up
-        look_up(seg, seg_end, id);
-        lds_barrier();
-        const int k_first = seg + kw * KS;
-        const int turns = k_first < seg_end ? (seg_end - k_first + kTurn - 1) / kTurn : 0;
-        const int all_turns = (seg_end - seg + kTurn - 1) / kTurn;   // of the set that has most
-        if (turns > 0) {                                    // a set is one turn ahead in its loads
-            load_keys(k_first, ring);
-            load_values(k_first, ring);
-        }
-        if (F8 && tid <= last_page - first_page) s_page[tid].y = scales;
-        lds_barrier();
-        for (int j = 0; j < (RW > 1 ? all_turns : turns); ++j) {
-            const int k0 = k_first + j * kTurn;
-            const bool more = j + 1 < turns;
-            const uint32_t at = RW > 1 ? (j % NS) * kStage : 0;
-            const u32x4 *keys = reinterpret_cast<const u32x4 *>(set_lds + at) + lane;
-            u32x4 *values = reinterpret_cast<u32x4 *>(s_ring + kw * NS * kStage + at + kValuesAt) + lane;
-            if constexpr (RW > 1) {
-                wait_vm<0>();                               // this wave's loads of the turn
-                lds_barrier();                              // ... and the others'; the turn before is used up
-                if (more) {
-                    const uint32_t to = ring + ((j + 1) % NS) * kStage;
-                    load_keys(k0 + kTurn, to);
-                    load_values(k0 + kTurn, to);
-                }
-                if (j >= turns) continue;                   // wave-uniform; another set has one more
+    auto attend = [&](auto tiles) {                         // the wave's first R row tiles
+        constexpr int R = decltype(tiles)::value;
+        for (int seg = kbeg; seg < kend; seg += segment) {
+            const int seg_end = min(seg + segment, kend);
+            if (seg > kbeg || a.splits > 1) id = table_entry(a, b, seg >> a.c.log_page);
+            if (seg > kbeg) __syncthreads();                    // the pages of the segment before are used up
+            look_up(seg, seg_end, id);
+            lds_barrier();
+            const int k_first = seg + kw * KS;
+            const int turns = k_first < seg_end ? (seg_end - k_first + kTurn - 1) / kTurn : 0;
+            const int all_turns = (seg_end - seg + kTurn - 1) / kTurn;   // of the set that has most
+            if (turns > 0) {                                    // a set is one turn ahead in its loads
+                load_keys(k_first, ring);
+                load_values(k_first, ring);
             }
-            const float ksc = key_scale(page_of(k0 + kg * GK));
-            const PageEntry page_v = page_of(k0 + g * GK);
-            const float vsc = value_scale(page_v);
-            const bool none = page_v.x >= kNone;
-            // wave-uniform: a key that some query does not see, or that does not exist
-            const bool masked = k0 + KS > clear || __ballot(none) != 0;
-            // S^T of the turn
-            floatx4 st[RT][NT];
-            if (RW == 1) wait_vm<NV>();                         // its keys have landed
-            __builtin_amdgcn_s_setprio(1);
+            if (F8 && tid <= last_page - first_page) s_page[tid].y = scales;
+            lds_barrier();
+            for (int j = 0; j < (RW > 1 ? all_turns : turns); ++j) {
+                const int k0 = k_first + j * kTurn;
+                const bool more = j + 1 < turns;
+                const uint32_t at = RW > 1 ? (j % NS) * kStage : 0;
+                const u32x4 *keys = reinterpret_cast<const u32x4 *>(set_lds + at) + lane;
+                u32x4 *values = reinterpret_cast<u32x4 *>(s_ring + kw * NS * kStage + at + kValuesAt) + lane;
+                if constexpr (RW > 1) {
+                    wait_vm<0>();                               // this wave's loads of the turn
+                    lds_barrier();                              // ... and the others'; the turn before is used up
+                    if (more) {
+                        const uint32_t to = ring + ((j + 1) % NS) * kStage;
+                        load_keys(k0 + kTurn, to);
+                        load_values(k0 + kTurn, to);
+                    }
+                    if (j >= turns) continue;                   // wave-uniform; another set has one more
+                }
+                const float ksc = key_scale(page_of(k0 + kg * GK));
+                const PageEntry page_v = page_of(k0 + g * GK);
+                const float vsc = value_scale(page_v);
+                const bool none = page_v.x >= kNone;
+                // wave-uniform: a key that some query does not see, or that does not exist
+                const bool masked = k0 + KS > clear || __ballot(none) != 0;
+                // S^T of the turn
+                floatx4 st[R][NT];
+                if (RW == 1) wait_vm<NV>();                         // its keys have landed
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int th = 0; th < NT; th += HT) {
-                u32x4 kf[HT][DS];
+                for (int th = 0; th < NT; th += HT) {
+                    u32x4 kf[HT][DS];
 #pragma unroll
-                for (int t = 0; t < HT; ++t) {
-                    u32x4 raw[KC];
+                    for (int t = 0; t < HT; ++t) {
+                        u32x4 raw[KC];
 #pragma unroll
-                    for (int c = 0; c < KC; ++c) raw[c] = keys[((th + t) * KC + c) * 64];
+                        for (int c = 0; c < KC; ++c) raw[c] = keys[((th + t) * KC + c) * 64];
 #pragma unroll
-                    for (int c = 0; c < DS; ++c) {
-                        if constexpr (F8) kf[t][c] = widen(raw[c / 2][2 * (c % 2)], raw[c / 2][2 * (c % 2) + 1], ksc);
-                        else kf[t][c] = raw[c];
+                        for (int c = 0; c < DS; ++c) {
+                            if constexpr (F8) kf[t][c] = widen(raw[c / 2][2 * (c % 2)], raw[c / 2][2 * (c % 2) + 1], ksc);
+                            else kf[t][c] = raw[c];
+                        }
+                    }
+#pragma unroll
+                    for (int rt = 0; rt < R; ++rt)
+#pragma unroll
+                        for (int t = 0; t < HT; ++t) st[rt][th + t] = floatx4{0.f, 0.f, 0.f, 0.f};
+                    // products that follow each other are of different sums
+#pragma unroll
+                    for (int i = 0; i < DS * R; ++i) {
+                        const int c = RT > 2 ? i / R : i % DS, rt = RT > 2 ? i % R : i / DS;
+#pragma unroll
+                        for (int t = 0; t < HT; ++t) st[rt][th + t] = mfma(kf[t][c], qf[rt][c], st[rt][th + t]);
                     }
                 }
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int t = 0; t < HT; ++t) st[rt][th + t] = floatx4{0.f, 0.f, 0.f, 0.f};
-                // products that follow each other are of different sums
-#pragma unroll
-                for (int i = 0; i < DS * RT; ++i) {
-                    const int c = RT > 2 ? i / RT : i % DS, rt = RT > 2 ? i % RT : i / DS;
-#pragma unroll
-                    for (int t = 0; t < HT; ++t) st[rt][th + t] = mfma(kf[t][c], qf[rt][c], st[rt][th + t]);
+                __builtin_amdgcn_s_setprio(0);
+                if constexpr (RW == 1) {
+                    wait_lds();
+                    if (more) load_keys(k0 + kTurn, ring);
                 }
-            }
-            __builtin_amdgcn_s_setprio(0);
-            if constexpr (RW == 1) {
-                wait_lds();
-                if (more) load_keys(k0 + kTurn, ring);
-            }
-            if (masked) {
-                const int kb = k0 + g * GK;                     // this lane's first key
-                const int real = none ? 0 : min(max(kend - kb, 0), GK);
+                if (masked) {
+                    const int kb = k0 + g * GK;                     // this lane's first key
+                    const int real = none ? 0 : min(max(kend - kb, 0), GK);
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    const int top = min(max(vis[rt] - kb, 0), real);
-                    uint32_t see = (1u << top) - 1u;
-                    if (a.parent && node[rt] >= 0) see |= window16(s_anc[node[rt]], kb - s.lc) & ((1u << real) - 1u);
+                    for (int rt = 0; rt < R; ++rt) {
+                        const int top = min(max(vis[rt] - kb, 0), real);
+                        uint32_t see = (1u << top) - 1u;
+                        if (a.parent && node[rt] >= 0) see |= window16(s_anc[node[rt]], kb - s.lc) & ((1u << real) - 1u);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (!(see >> (4 * t + r) & 1)) st[rt][t][r] = -INFINITY;
+                    }
+                }
+                float bm[R];
+                bool raise = false;
+#pragma unroll
+                for (int rt = 0; rt < R; ++rt) {
+                    bm[rt] = -INFINITY;
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (!(see >> (4 * t + r) & 1)) st[rt][t][r] = -INFINITY;
+                        for (int r = 0; r < 4; ++r) bm[rt] = fmaxf(bm[rt], st[rt][t][r]);
+                    bm[rt] = max_rows(bm[rt]) * sc;
+                    raise |= bm[rt] > m[rt] + kLazyRescale;         // always when m is still -inf
                 }
-            }
-            float bm[RT];
-            bool raise = false;
+                if (__builtin_expect(__ballot(raise) != 0, 0)) {
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                bm[rt] = -INFINITY;
+                    for (int rt = 0; rt < R; ++rt) {
+                        const bool up = bm[rt] > m[rt] + kLazyRescale;
+                        const float alpha = up ? __builtin_amdgcn_exp2f(m[rt] - bm[rt]) : 1.f;   // 0 from -inf
+                        if (up) m[rt] = bm[rt];
+                        ol[rt] *= alpha;
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) bm[rt] = fmaxf(bm[rt], st[rt][t][r]);
-                bm[rt] = max_rows(bm[rt]) * sc;
-                raise |= bm[rt] > m[rt] + kLazyRescale;         // always when m is still -inf
-            }
-            if (__builtin_expect(__ballot(raise) != 0, 0)) {
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    const bool up = bm[rt] > m[rt] + kLazyRescale;
-                    const float alpha = up ? __builtin_amdgcn_exp2f(m[rt] - bm[rt]) : 1.f;   // 0 from -inf
-                    if (up) m[rt] = bm[rt];
-                    ol[rt] *= alpha;
-#pragma unroll
-                    for (int t = 0; t < DT; ++t) o[rt][t] *= alpha;
-                }
-            }
-            // O^T += V^T P^T
-            if constexpr (RW == 1) {
-                if (more) wait_vm<NK>();
-                else wait_vm<0>();
-            }
-            if (masked) {
-                // places that hold no key of the sequence may hold anything: a weight of zero does not make
-                // a NaN harmless
-                const int real = none ? 0 : min(max(kend - (k0 + g * GK), 0), GK);
-                const bool some_see = k0 + KS > clear && clear < kend;
-#pragma unroll
-                for (int c = 0; c < VC; ++c) {
-                    u32x4 keep;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        constexpr int EW = 4 / EB;              // elements of a word
-                        const int in = real - (c * 4 + w) * EW;
-                        keep[w] = in >= EW ? 0xffffffffu : in > 0 ? (1u << (in * 8 * EB)) - 1u : 0u;
+                        for (int t = 0; t < DT; ++t) o[rt][t] *= alpha;
                     }
-                    // waves that share the turn store the same, and each word once
-                    if (some_see) {
+                }
+                // O^T += V^T P^T
+                if constexpr (RW == 1) {
+                    if (more) wait_vm<NK>();
+                    else wait_vm<0>();
+                }
+                if (masked) {
+                    // places that hold no key of the sequence may hold anything: a weight of zero does not make
+                    // a NaN harmless
+                    const int real = none ? 0 : min(max(kend - (k0 + g * GK), 0), GK);
+                    const bool some_see = k0 + KS > clear && clear < kend;
 #pragma unroll
-                        for (int t = 0; t < DT; ++t) {
-                            u32x4 x = values[(t * VC + c) * 64] & keep;
+                    for (int c = 0; c < VC; ++c) {
+                        u32x4 keep;
 #pragma unroll
-                            for (int w = 0; w < 4; ++w) x[w] = finite<F8>(x[w]);
-                            values[(t * VC + c) * 64] = x;
+                        for (int w = 0; w < 4; ++w) {
+                            constexpr int EW = 4 / EB;              // elements of a word
+                            const int in = real - (c * 4 + w) * EW;
+                            keep[w] = in >= EW ? 0xffffffffu : in > 0 ? (1u << (in * 8 * EB)) - 1u : 0u;
                         }
-                    } else {
+                        // waves that share the turn store the same, and each word once
+                        if (some_see) {
 #pragma unroll
-                        for (int t = 0; t < DT; ++t) values[(t * VC + c) * 64] &= keep;
+                            for (int t = 0; t < DT; ++t) {
+                                u32x4 x = values[(t * VC + c) * 64] & keep;
+#pragma unroll
+                                for (int w = 0; w < 4; ++w) x[w] = finite<F8>(x[w]);
+                                values[(t * VC + c) * 64] = x;
+                            }
+                        } else {
+#pragma unroll
+                            for (int t = 0; t < DT; ++t) values[(t * VC + c) * 64] &= keep;
+                        }
                     }
                 }
-            }
-            u32x4 pb[RT][NU];
+                u32x4 pb[R][NU];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                // a query that has seen nothing yet keeps m = -inf and adds nothing
-                const float mm = m[rt] == -INFINITY ? INFINITY : m[rt];
-#pragma unroll
-                for (int u = 0; u < NU; ++u) {
-                    float p[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(st[rt][2 * u + i / 4][i % 4], sc, -mm));
-                    pb[rt][u] = u32x4{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3]), bf16_pair(p[4], p[5]), bf16_pair(p[6], p[7])};
-                }
-            }
-            __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-            for (int u = 0; u < NU; ++u)
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) ol[rt] = mfma(ones, pb[rt][u], ol[rt]);
-#pragma unroll
-            for (int th = 0; th < DT; th += HD) {
-                u32x4 vf[HD][NU];
-#pragma unroll
-                for (int t = 0; t < HD; ++t) {
-                    u32x4 raw[VC];
-#pragma unroll
-                    for (int c = 0; c < VC; ++c) raw[c] = values[((th + t) * VC + c) * 64];
+                for (int rt = 0; rt < R; ++rt) {
+                    // a query that has seen nothing yet keeps m = -inf and adds nothing
+                    const float mm = m[rt] == -INFINITY ? INFINITY : m[rt];
 #pragma unroll
                     for (int u = 0; u < NU; ++u) {
-                        if constexpr (F8) vf[t][u] = widen(raw[0][2 * u], raw[0][2 * u + 1], vsc);
-                        else vf[t][u] = raw[u];
+                        float p[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(st[rt][2 * u + i / 4][i % 4], sc, -mm));
+                        pb[rt][u] = u32x4{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3]), bf16_pair(p[4], p[5]), bf16_pair(p[6], p[7])};
                     }
                 }
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int u = 0; u < NU; ++u)
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
+                    for (int rt = 0; rt < R; ++rt) ol[rt] = mfma(ones, pb[rt][u], ol[rt]);
 #pragma unroll
-                        for (int t = 0; t < HD; ++t) o[rt][th + t] = mfma(vf[t][u], pb[rt][u], o[rt][th + t]);
-            }
-            __builtin_amdgcn_s_setprio(0);
-            if constexpr (RW == 1) {
-                wait_lds();
-                if (more) load_values(k0 + kTurn, ring);
+                for (int th = 0; th < DT; th += HD) {
+                    u32x4 vf[HD][NU];
+#pragma unroll
+                    for (int t = 0; t < HD; ++t) {
+                        u32x4 raw[VC];
+#pragma unroll
+                        for (int c = 0; c < VC; ++c) raw[c] = values[((th + t) * VC + c) * 64];
+#pragma unroll
+                        for (int u = 0; u < NU; ++u) {
+                            if constexpr (F8) vf[t][u] = widen(raw[0][2 * u], raw[0][2 * u + 1], vsc);
+                            else vf[t][u] = raw[u];
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < NU; ++u)
+#pragma unroll
+                        for (int rt = 0; rt < R; ++rt)
+#pragma unroll
+                            for (int t = 0; t < HD; ++t) o[rt][th + t] = mfma(vf[t][u], pb[rt][u], o[rt][th + t]);
+                }
+                __builtin_amdgcn_s_setprio(0);
+                if constexpr (RW == 1) {
+                    wait_lds();
+                    if (more) load_values(k0 + kTurn, ring);
+                }
             }
         }
+    };
+    // Of up to 80 rows the second wave's third tile has none: left out, 68 rows take 61.5 us, with it 65.7.  (Of
+    // workgroups whose waves take the same rows it is not worth the code: 30.3 and 30.4 for two long sequences.)
+    bool all_tiles = true;
+    if constexpr (RW > 1 && RT > 2) {
+        all_tiles = q0 + (rw * RT + RT - 1) * 16 < q1;
+        if (!all_tiles) attend(std::integral_constant<int, RT - 1>{});
     }
+    if (all_tiles) attend(std::integral_constant<int, RT>{});
 
     // join the sets
 #pragma unroll
@@ -793,82 +805,90 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs 
     }
     float m = -INFINITY;
 
-    for (int seg = kbeg; seg < kend; seg += segment) {
-        const int seg_end = min(seg + segment, kend);
-        if (seg > kbeg || a.splits > 1) id = table_entry(a, b, seg >> a.c.log_page);
-        if (seg > kbeg) __syncthreads();                    // the pages of the segment before are used up
-        look_up(seg, seg_end, id);
-        stage(seg, s_stage[0]);
-        for (int k0 = seg, buf = 0; k0 < seg_end; k0 += KS, buf ^= 1) {
-            const bool more = k0 + KS < seg_end;
-            lds_barrier();                                  // the turn is staged; the one before is used up
-            if (more) load(k0 + KS);
-            const u32x4 *keys = reinterpret_cast<const u32x4 *>(s_stage[buf]) + lane;
-            const u32x4 *values = reinterpret_cast<const u32x4 *>(s_stage[buf] + kValuesAt) + lane;
-            floatx16 st[KT];
+    // A wave without rows stages its share only (256 groups of 132 rows: 106.6 us, then 100.8).
+    auto attend = [&](auto works) {
+        constexpr bool WORKS = decltype(works)::value;
+        for (int seg = kbeg; seg < kend; seg += segment) {
+            const int seg_end = min(seg + segment, kend);
+            if (seg > kbeg || a.splits > 1) id = table_entry(a, b, seg >> a.c.log_page);
+            if (seg > kbeg) __syncthreads();                    // the pages of the segment before are used up
+            look_up(seg, seg_end, id);
+            stage(seg, s_stage[0]);
+            for (int k0 = seg, buf = 0; k0 < seg_end; k0 += KS, buf ^= 1) {
+                const bool more = k0 + KS < seg_end;
+                lds_barrier();                                  // the turn is staged; the one before is used up
+                if (more) load(k0 + KS);
+                if constexpr (WORKS) {
+                    const u32x4 *keys = reinterpret_cast<const u32x4 *>(s_stage[buf]) + lane;
+                    const u32x4 *values = reinterpret_cast<const u32x4 *>(s_stage[buf] + kValuesAt) + lane;
+                    floatx16 st[KT];
 #pragma unroll
-            for (int t = 0; t < KT; ++t)
+                    for (int t = 0; t < KT; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) st[t][i] = 0.f;
+                        for (int i = 0; i < 16; ++i) st[t][i] = 0.f;
 #pragma unroll
-            for (int c = 0; c < DS; ++c)
+                    for (int c = 0; c < DS; ++c)
 #pragma unroll
-                for (int t = 0; t < KT; ++t) st[t] = mfma32(keys[(t * DS + c) * 64], qf[c], st[t]);
-            if (k0 + KS > clear || any_none) {
+                        for (int t = 0; t < KT; ++t) st[t] = mfma32(keys[(t * DS + c) * 64], qf[c], st[t]);
+                    if (k0 + KS > clear || any_none) {
 #pragma unroll
-                for (int t = 0; t < KT; ++t) {
-                    const int kb = k0 + 32 * t + 16 * gh;   // this lane's first key of the tile
-                    const int real = page_of(kb).x >= kNone ? 0 : min(max(kend - kb, 0), 16);
-                    const int top = min(max(vis - kb, 0), real);
-                    uint32_t see = (1u << top) - 1u;
-                    if (a.parent && live) see |= window16(s_anc[r], kb - s.lc) & ((1u << real) - 1u);
+                        for (int t = 0; t < KT; ++t) {
+                            const int kb = k0 + 32 * t + 16 * gh;   // this lane's first key of the tile
+                            const int real = page_of(kb).x >= kNone ? 0 : min(max(kend - kb, 0), 16);
+                            const int top = min(max(vis - kb, 0), real);
+                            uint32_t see = (1u << top) - 1u;
+                            if (a.parent && live) see |= window16(s_anc[r], kb - s.lc) & ((1u << real) - 1u);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (!(see >> i & 1)) st[t][i] = -INFINITY;
+                            for (int i = 0; i < 16; ++i)
+                                if (!(see >> i & 1)) st[t][i] = -INFINITY;
+                        }
+                    }
+                    float bm = -INFINITY;
+#pragma unroll
+                    for (int t = 0; t < KT; ++t)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) bm = fmaxf(bm, st[t][i]);
+                    {
+                        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
+                        bm = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * sc;
+                    }
+                    const bool raise = bm > m + kLazyRescale;       // always when m is still -inf
+                    if (__builtin_expect(__ballot(raise) != 0, 0)) {
+                        const float alpha = raise ? __builtin_amdgcn_exp2f(m - bm) : 1.f;   // 0 from -inf
+                        if (raise) m = bm;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            ol[i] *= alpha;
+#pragma unroll
+                            for (int t = 0; t < DT; ++t) o[t][i] *= alpha;
+                        }
+                    }
+                    // a query that has seen nothing yet keeps m = -inf and adds nothing
+                    const float mm = m == -INFINITY ? INFINITY : m;
+                    u32x4 pb[KT][2];
+#pragma unroll
+                    for (int t = 0; t < KT; ++t)
+#pragma unroll
+                        for (int v = 0; v < 2; ++v)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                pb[t][v][i] = bf16_pair(__builtin_amdgcn_exp2f(fmaf(st[t][8 * v + 2 * i], sc, -mm)),
+                                                        __builtin_amdgcn_exp2f(fmaf(st[t][8 * v + 2 * i + 1], sc, -mm)));
+#pragma unroll
+                    for (int t = 0; t < KT; ++t)
+#pragma unroll
+                        for (int v = 0; v < 2; ++v) {
+                            ol = mfma32(ones, pb[t][v], ol);
+#pragma unroll
+                            for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32(values[((dt * KT + t) * 2 + v) * 64], pb[t][v], o[dt]);
+                        }
                 }
+                if (more) stage(k0 + KS, s_stage[buf ^ 1]);
             }
-            float bm = -INFINITY;
-#pragma unroll
-            for (int t = 0; t < KT; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) bm = fmaxf(bm, st[t][i]);
-            {
-                const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
-                bm = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * sc;
-            }
-            const bool raise = bm > m + kLazyRescale;       // always when m is still -inf
-            if (__builtin_expect(__ballot(raise) != 0, 0)) {
-                const float alpha = raise ? __builtin_amdgcn_exp2f(m - bm) : 1.f;   // 0 from -inf
-                if (raise) m = bm;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    ol[i] *= alpha;
-#pragma unroll
-                    for (int t = 0; t < DT; ++t) o[t][i] *= alpha;
-                }
-            }
-            // a query that has seen nothing yet keeps m = -inf and adds nothing
-            const float mm = m == -INFINITY ? INFINITY : m;
-            u32x4 pb[KT][2];
-#pragma unroll
-            for (int t = 0; t < KT; ++t)
-#pragma unroll
-                for (int v = 0; v < 2; ++v)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        pb[t][v][i] = bf16_pair(__builtin_amdgcn_exp2f(fmaf(st[t][8 * v + 2 * i], sc, -mm)),
-                                                __builtin_amdgcn_exp2f(fmaf(st[t][8 * v + 2 * i + 1], sc, -mm)));
-#pragma unroll
-            for (int t = 0; t < KT; ++t)
-#pragma unroll
-                for (int v = 0; v < 2; ++v) {
-                    ol = mfma32(ones, pb[t][v], ol);
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32(values[((dt * KT + t) * 2 + v) * 64], pb[t][v], o[dt]);
-                }
-            if (more) stage(k0 + KS, s_stage[buf ^ 1]);
         }
-    }
+    };
+    if (__ballot(live) == 0) attend(std::false_type{});
+    else attend(std::true_type{});
 
     if (!valid) return;
     // O^T tile t, elements 4e .. 4e + 3: d = 32 t + 8 e + 4 gh + 0..3 of this lane's query
@@ -994,9 +1014,16 @@ PagedPlan paged_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq) {
     for (int rt = 1; rt <= kMaxRowTiles && !per_block; ++rt)
         if (groups * ((tiles + rt - 1) / rt) * pieces <= kCus) per_block = p.row_tiles = rt;
     if (!per_block) {
-        if (tiles > 2 * kMaxRowTiles) p.row_waves = 4;
-        // 68 rows in 512 groups: two waves sharing keys 64.5 us, two workgroups 77; in 16 groups 45 and 29.8
-        else if (tiles > kMaxRowTiles && groups >= kCus) p.row_waves = 2;
+        // With over three tiles two waves of up to three share keys where that makes a workgroup for every CU (68
+        // rows in 512 groups: 65.7 us, as two workgroups that share nothing 77; in 16 groups 45 and 29.8).  Over six
+        // tiles the wide kernel's cost less each, but it takes them by eight: sharing waves where they take
+        // under four fifths as many.  Of 32 + 2000 positions, 288 groups, e4m3: 132 to 188 rows 81 to 83 us and
+        // wide 101 to 102, 276 rows 102 and 123; bf16 108 to 111 and 111 to 117, 127 and 140; 100 rows (as many tiles) 85.1 and
+        // 85.6; 124 rows of bf16 as two workgroups 90, wide 63.  128 groups of 164 rows 40.2 and 51.1, 64 31.9 and 31.2.
+        const int64_t pairs = (tiles + 2 * kMaxRowTiles - 1) / (2 * kMaxRowTiles);
+        const int64_t shared = pairs * 2 * ((tiles + 2 * pairs - 1) / (2 * pairs)), wide = (tiles + 7) / 8 * 8;
+        if (tiles > kMaxRowTiles && groups * pairs >= kCus && (pairs == 1 || 5 * shared < 4 * wide)) p.row_waves = 2;
+        else if (tiles > 2 * kMaxRowTiles) p.row_waves = 4;
         // rows shared out evenly over the fewest workgroups
         const int64_t most = p.row_waves == 4 ? kWideRows / 16 : kMaxRowTiles * p.row_waves, blocks = (tiles + most - 1) / most;
         p.row_tiles = p.row_waves == 4 ? kWideRows / 64 : static_cast<int32_t>((tiles + blocks * p.row_waves - 1) / (blocks * p.row_waves));

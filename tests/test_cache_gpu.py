@@ -328,9 +328,9 @@ def test_hybrid_long_in_pieces(dtype):
 
 
 @pytest.mark.parametrize("dtype", [F8, BF16])
-@pytest.mark.parametrize("B,n_q,Hq", [(17, 1, 8), (32, 13, 32), (17, 25, 32)])
+@pytest.mark.parametrize("B,n_q,Hq", [(17, 1, 8), (32, 13, 32), (32, 17, 32), (17, 25, 32)])
 def test_hybrid_more_pages_than_are_looked_up_at_once(dtype, B, n_q, Hq):
-    # groups enough that nothing is cut, more than 252 pages each: few rows, 52 and 100 of a group
+    # groups enough that nothing is cut, more than 252 pages each: few rows, 52, 68 and 100 of a group
     ctx = [4100 - 31 * (b % 5) for b in range(B)]
     _check_hybrid(dtype, 64, 16, Hq, 8, ctx, ctx, n_q, 3, seed=B, only=[0, B - 1])
 
@@ -344,9 +344,10 @@ def test_hybrid_pieces_of_many_rows(dtype, n_q, Hq, more):
 
 
 @pytest.mark.parametrize("dtype", [F8, BF16])
-@pytest.mark.parametrize("D,P,n_q,K", [(128, 64, 13, 5), (128, 16, 17, 7), (64, 32, 24, 2), (128, 128, 22, 0)])
+@pytest.mark.parametrize("D,P,n_q,K", [(128, 64, 13, 5), (128, 16, 17, 7), (64, 32, 24, 2), (128, 128, 22, 0),
+                                       (128, 64, 33, 15), (64, 16, 41, 19), (128, 32, 48, 20), (128, 128, 68, 30)])
 def test_hybrid_of_many_groups(dtype, D, P, n_q, K):
-    # 256 groups of 52 to 96 rows: waves that share their keys, padding and context queries among the rows
+    # 256 groups of 52 to 272 rows: waves that share their keys, padding and context queries among the rows
     B = 32
     ctx = [30 + 67 * (b % 4) for b in range(B)]
     start = [c - 3 * (b % 3) for b, c in enumerate(ctx)]
@@ -418,9 +419,9 @@ def test_tree(dtype, D, P, Hq, H, ctx, N, more):
 
 
 @pytest.mark.parametrize("dtype", [F8, BF16])
-@pytest.mark.parametrize("D,N", [(128, 13), (64, 24), (128, 60)])
+@pytest.mark.parametrize("D,N", [(128, 13), (64, 24), (128, 60), (128, 33), (64, 68)])
 def test_tree_of_many_groups(dtype, D, N):
-    # 256 groups of 52, 96 and 240 rows
+    # 256 groups of 52, 96, 240, 132 and 272 rows
     ctx = [25 + 41 * (b % 5) for b in range(32)]
     _check_tree(dtype, D, 32, 32, 8, ctx, [_random_tree(N, b, near=5) for b in range(32)], seed=N, more=40, only=[1, 4, 31])
 
@@ -473,8 +474,10 @@ def _hows(dtype):
     return ("nan", "scales") if dtype == F8 else ("nan", "inf")
 
 
-# few rows, spread out; 58 and 90 rows in many groups; up to 45 in some; over 200 in one group, and in some
-_ROWS = [(1, 4, 2, 1, 0), (1, 8, 2, 3, 0), (32, 16, 8, 1, 40), (4, 8, 8, 1, 3000), (1, 8, 1, 1, 3000), (4, 16, 8, 5, 3000)]
+# few rows, spread out; 58 and 90 rows in many groups; up to 45 in some; over 200 in one group, and in some;
+# 116 and 180 of many
+_ROWS = [(1, 4, 2, 1, 0), (1, 8, 2, 3, 0), (32, 16, 8, 1, 40), (4, 8, 8, 1, 3000), (1, 8, 1, 1, 3000), (4, 16, 8, 5, 3000),
+         (32, 32, 8, 1, 40)]
 
 
 @pytest.mark.parametrize("dtype", [F8, BF16])
