@@ -647,7 +647,7 @@ __device__ inline floatx16 mfma32(u32x4 a, u32x4 b, floatx16 c) {
 // for its four waves: each takes a quarter through its registers into LDS, in the order of the
 // products' operands, while the turn before is worked on.
 //
-// Whole inputs of 4 x 1820 to 2063 positions, 32/8 heads, D = 128, e4m3 (121 GFLOP): 160 us, 757 TFLOP/s; trees of
+// Whole inputs of 4 x 1820 to 2063 positions, 32/8 heads, D = 128, e4m3 (121 GFLOP): 161 us, 753 TFLOP/s; trees of
 // 60 nodes after 64 contexts of 1536 to 2048 (113 GFLOP) 164 us.  No pipe is full: matrix instructions take 36% of
 // the time, vector ones 31% on the same port, the LDS reads of the operands (1 KB a product of 32 cycles) 43%; the
 // waits between them bound it.  Without those reads the same code takes 116 to 125 us, without staging 124 to 132,
@@ -699,8 +699,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs 
     bool any_none = false;                                  // among them
     auto page_of = [&](int key) { return s_page[min(key >> a.c.log_page, last_page) - first_page]; };
     // piece i of this thread: of key row key_at(i) the bytes 16 key_piece(i) .. + 15, and of component
-    // comp_at(i) the keys 16 / EB * comp_piece(i) ..; sixteen lanes side by side take sixteen rows
-    auto key_at = [&](int i) { return ((wave * LK + i) / (CPR / 4)) * 16 + (lane & 15); };
+    // comp_at(i) the keys 16 / EB * comp_piece(i) ..; sixteen lanes side by side take sixteen rows, of keys
+    // those that are side by side in the products' order too (consecutive ones meet in LDS banks: 4 x 2048
+    // positions of bf16, d = 64, 67.2 us; now 61.2; the same in e4m3, d = 128, 160 and 160)
+    auto key_at = [&](int i) {
+        const int t = (wave * LK + i) / (CPR / 4);
+        return (t >> 1) * 32 + ((lane >> 2) & 1) * 16 + (t & 1) * 8 + ((lane >> 3) & 1) * 4 + (lane & 3);
+    };
     auto key_piece = [&](int i) { return (wave * LK + i) % (CPR / 4) * 4 + (lane >> 4); };
     auto comp_at = [&](int i) { return ((wave * LV + i) / (CPD / 4)) * 16 + (lane & 15); };
     auto comp_piece = [&](int i) { return (wave * LV + i) % (CPD / 4) * 4 + (lane >> 4); };
