@@ -213,17 +213,15 @@ __global__ __launch_bounds__(kCacheThreads) void k_cache_append(AppendArgs a) {
     }
     uint32_t *s_v = reinterpret_cast<uint32_t *>(s_dyn);
 
-    const int P = 1 << a.c.log_page;
     const uint32_t bj = quot(a.by_heads, blockIdx.x);
     const int h = blockIdx.x - bj * a.by_heads.d;
     const int b = quot(a.by_pages, bj);
     const int64_t start = a.start[b];
     const int64_t cnt = a.count ? min(max(a.count[b], 0), a.n) : a.n;
     const int64_t j = (max(start, static_cast<int64_t>(0)) >> a.c.log_page) + (bj - b * a.by_pages.d);
-    // places [lo, hi) of the page are new; token of place s: base + s
-    const int64_t base = j * P - start;
-    const int lo = static_cast<int>(max(static_cast<int64_t>(0), -base));
-    const int hi = static_cast<int>(min(static_cast<int64_t>(P), cnt - base));
+    const NewPlaces places = new_places(start, cnt, j, a.c.log_page);
+    const int64_t base = places.base;
+    const int lo = places.lo, hi = places.hi;
     if (lo >= hi || j >= a.c.max_pages) return;
     const int32_t id = a.c.table[static_cast<int64_t>(b) * a.c.max_pages + j];
     const int T = hi - lo;

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "launch.h"
+#include "paged_ranges.h"
 
 namespace cospec {
 

@@ -174,6 +174,27 @@ def test_append_outside_the_room(dtype):
         assert _same(got.raw[side], want)
 
 
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("n", [2, 17, 200])
+@pytest.mark.parametrize("count", [None, 0, 1])
+def test_append_far_outside_writes_nothing(dtype, n, count):
+    # the lowest and the highest position that a start can name, and tokens that end before position 0
+    low, high = -(1 << 31), (1 << 31) - 1
+    start = [low, low + 1, low + n, high, high - n, -n]
+    B = len(start)
+    table, n_pages = ref.make_table(B, 16, 2)
+    cache = _filled(table, n_pages, 2, 128, 64, dtype, [1000] * B, 2, junk=False)
+    before = [t.clone() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale) if t is not None]
+    g = _gen(3)
+    k, v, q = (torch.randn(B, n, h, 128, generator=g).to(BF16).to(DEV) for h in (2, 2, 4))
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    got = cs.cache_append(cache, table.to(DEV), i32(start), k, v, count=None if count is None else i32([count] * B), q=q)
+    torch.cuda.synchronize()
+    for a, b in zip(before, (t for t in (cache.k, cache.v, cache.k_scale, cache.v_scale) if t is not None)):
+        assert _same(a, b)
+    assert torch.equal(got, q)
+
+
 @pytest.mark.parametrize("size", [300.0, 1e-3, 3e38, 1e-36])
 def test_append_scales_grow_and_keep(size):
     # far larger values: earlier ones are rounded anew; far smaller ones: the scale stays
