@@ -110,9 +110,8 @@ __device__ inline Cut cut_of(const PagedArgs &a, const Seq &s, int q0, int q1) {
     int kend = s.end;
     if (p_lo >= s.end) kend = 0;                            // all padding: no key
     else if (!a.parent && p_hi < s.lc) kend = max(static_cast<int>(p_hi) + 1, 0);
-    const int part = quot(a.by_splits, kend + a.splits - 1);
-    const int chunk = max((part + kStep - 1) / kStep * kStep, a.min_piece);
-    return Cut{kend, chunk, max((kend + chunk - 1) / chunk, 1)};
+    const Pieces p = pieces_of(kend, quot(a.by_splits, kend + a.splits - 1), kStep, a.min_piece);
+    return Cut{kend, p.chunk, p.count};
 }
 
 // Keys [0, result) of a piece's [.., kend) are seen by every row of [q0, q1) that sees any.

@@ -20,4 +20,16 @@ constexpr NewPlaces new_places(int64_t start, int64_t count, int64_t j, int log_
     return NewPlaces{base, static_cast<int>(lo < P ? lo : P), static_cast<int>(hi < 0 ? 0 : hi < P ? hi : P)};
 }
 
+// Keys [0, kend) cut into `count` pieces (at least one) of `chunk` keys, the last one shorter; `part`: the keys of
+// an even share, `step`: what a chunk is a multiple of, `least`: its least length.
+struct Pieces {
+    int chunk, count;
+};
+
+constexpr Pieces pieces_of(int kend, int part, int step, int least) {
+    const int even = (part + step - 1) / step * step, chunk = even > least ? even : least;
+    // (kend + chunk may be more than 31 bits hold)
+    return Pieces{chunk, kend > 0 ? (kend - 1) / chunk + 1 : 1};
+}
+
 }  // namespace cospec

@@ -348,6 +348,32 @@ def test_hybrid_long_in_pieces(dtype):
     _check_hybrid(dtype, 128, 64, 8, 2, [3001, 40, 2047], [3001, 40, 2047], 9, 3, seed=6)
 
 
+def test_hybrid_of_the_longest_sequence():
+    """2^31 - 65664 positions in pages that repeat: no piece of them is left out.  With keys of zeros every weight is
+    one, and the values are 0 in the first three fifths, then 1 and 2: all sums are whole numbers (up to 2^24 in a wave,
+    multiples of 64 above), so that only the quotient and the result's rounding are off."""
+    P, D = 128, 64
+    T = ((1 << 31) - 1 - 65536) // P
+    v = torch.zeros(2, 1, D, P)
+    v[1] = torch.arange(D)[:, None] % 2 + 1.0
+    cache = cs.PagedCache(torch.zeros(2, 1, P, D, dtype=BF16, device=DEV), v.to(BF16).to(DEV))
+    table = (torch.arange(T) >= T * 3 // 5).int()[None].to(DEV)
+    ctx = torch.tensor([T * P], dtype=torch.int32, device=DEV)
+    q = torch.ones(1, 1, 2, D, dtype=BF16, device=DEV)
+    got = cs.hybrid_attention_paged(q, cache, table, ctx, ctx - 1, 0, 0.125).double().cpu()
+    want = (T - T * 3 // 5) / T * (torch.arange(D) % 2 + 1.0).double()
+    assert ((got - want).abs() <= (2.0 ** -8 + 2.0 ** -20) * want).all()
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("n_q,Hq,more", [(3, 4, 0), (60, 8, 3000)])
+def test_hybrid_far_positions_of_queries(dtype, n_q, Hq, more):
+    # the lowest and the highest position and length that 32 bits name
+    low, high = -(1 << 31), (1 << 31) - 1
+    _check_hybrid(dtype, 128, 32, Hq, 2, [70, 70, low, 70], [low, high, high - n_q, low + 1], n_q, 2, seed=5, more=more)
+    _check_hybrid(dtype, 128, 32, Hq, 2, [high, high], [high, 90], n_q, 2, T=4, seed=6)
+
+
 @pytest.mark.parametrize("dtype", [F8, BF16])
 @pytest.mark.parametrize("B,n_q,Hq", [(17, 1, 8), (32, 13, 32), (32, 17, 32), (17, 25, 32)])
 def test_hybrid_more_pages_than_are_looked_up_at_once(dtype, B, n_q, Hq):

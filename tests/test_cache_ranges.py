@@ -14,6 +14,10 @@ extern "C" void places(int64_t start, int64_t count, int64_t j, int log_page, in
     const cospec::NewPlaces p = cospec::new_places(start, count, j, log_page);
     out[0] = p.base; out[1] = p.lo; out[2] = p.hi;
 }
+extern "C" void pieces(int kend, int part, int step, int least, int *out) {
+    const cospec::Pieces p = cospec::pieces_of(kend, part, step, least);
+    out[0] = p.chunk; out[1] = p.count;
+}
 """
 
 
@@ -48,3 +52,18 @@ def test_new_places_of_a_page(ranges, log_page, n):
                 else:
                     assert (lo, hi) == (want[0] - j * P, want[1] - j * P), (start, count, j)
                     assert 0 <= lo + base and hi + base <= count
+
+
+@pytest.mark.parametrize("least", [256, 512])
+def test_pieces_hold_every_key(ranges, least):
+    out = (ctypes.c_int * 2)()
+    room = HIGH - 65536                                     # positions of a sequence, at most
+    for splits in range(1, 65):
+        ends = [0, 1, 63, 64, 65, least, least + 1, splits * least, splits * least + 1, 10 ** 6 + 7, 10 ** 9, 3 * 10 ** 8 * 5,
+                1720000000, 2110000000, room - 127, room - 1, room]
+        for kend in ends:
+            ranges.pieces(kend, (kend + splits - 1) // splits, 64, least, out)
+            chunk, count = out
+            assert chunk % 64 == 0 and chunk >= least
+            assert 1 <= count <= splits and (count - 1) * chunk < max(kend, 1) and count * chunk >= kend, (kend, splits)
+            assert count * chunk <= HIGH                      # a piece's end, before it is cut to kend, fits
