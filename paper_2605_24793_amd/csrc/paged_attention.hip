@@ -987,6 +987,9 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
 // load takes whole 64-byte runs of keys and of values, as with e4m3 pages of 64 places.  64 single tokens
 // at about 3600 positions: kept 86.4 us, not kept 80.1; pages of 128, 128 tokens 168.6 and 191.7 (the
 // other half of a run is fetched again); of 16, 48 tokens 76.5 and 77.3; bf16 178 and 202.
+// Where several workgroups of up to 16 rows share a group (small calls spread theirs) they read the same keys,
+// which are then kept: one sequence of 334 positions and 17 queries 8.03 us, not kept 8.27; of 1511 and 11
+// queries 12.2 and 12.6; a tree of 60 nodes after 450 positions 10.1 and 10.4.
 constexpr int kNontemporalPage = 6;   // log2 of its places
 
 template <int D, bool F8>
@@ -997,7 +1000,8 @@ void run_attention(const PagedArgs &a, unsigned grid, hipStream_t s) {
     else if (a.row_waves == 2) hipLaunchKernelGGL((k_paged_attention<D, F8, 2, 2>), g, t, 0, s, a);
     else if (a.row_tiles == 3) hipLaunchKernelGGL((k_paged_attention<D, F8, 3, 1>), g, t, 0, s, a);
     else if (a.row_tiles == 2) hipLaunchKernelGGL((k_paged_attention<D, F8, 2, 1>), g, t, 0, s, a);
-    else if (F8 && a.c.log_page == kNontemporalPage) hipLaunchKernelGGL((k_paged_attention<D, F8, 1, 1, F8>), g, t, 0, s, a);
+    else if (F8 && a.c.log_page == kNontemporalPage && a.by_blocks.d == 1)
+        hipLaunchKernelGGL((k_paged_attention<D, F8, 1, 1, F8>), g, t, 0, s, a);
     else hipLaunchKernelGGL((k_paged_attention<D, F8, 1, 1>), g, t, 0, s, a);
 }
 
