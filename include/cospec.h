@@ -550,9 +550,10 @@ cospec_status cospec_cache_keep(const cospec_cache *cache, const int32_t *ctx_le
 /*
  * cospec_hybrid_attention over the cache: the same mask, for the positions the cache holds
  * (l = l_c + 2K + 3, at most max_pages * page).  With n_q = 1, q_start = l_c - 1 this is plain
- * decoding of the last of l_c positions.  What a query sees must be finite, else its result is
- * unspecified; what it does not see does not reach it, whatever it holds (a place never
- * written, a page that has no scale yet).
+ * decoding of the last of l_c positions.  What a query does not see does not reach it, whatever it
+ * holds (a place never written, a page that has no scale yet).  A value that it sees and that is not
+ * finite makes its result NaN or infinite in that component, and may make it NaN in the others; a key
+ * it sees whose score is NaN or plus infinity makes all of it NaN.
  *  q    [B][n_q][Hq][d] bf16; Hq a multiple of cache->heads; out the same shape.  A query
  *       outside [0, l), or that sees only positions on no page, gets zeros.
  * fp32 sums; the attention weights enter the second product, and their sum, rounded to bf16;

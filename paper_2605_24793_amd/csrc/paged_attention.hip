@@ -121,11 +121,23 @@ __device__ inline int seen_by_all(const PagedArgs &a, const Seq &s, int q0, int 
     return p >= s.lc ? kend : min(static_cast<int>(p) + 1, kend);
 }
 
-// Four bytes of values with those that are not finite made zero: among keys that some rows see and others
-// do not, a weight of zero would not keep them from the others.
-template <bool F8> __device__ inline uint32_t finite(uint32_t x) {
-    const uint32_t top = F8 ? ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+// Values that are not finite, among keys that some rows see and others do not.  A weight of zero would not keep them
+// from the others: they are made zero, and the weights of the rows that do see such a key NaN.
+// not_finite: the highest bit of every such element of four bytes; emptied: the four bytes without these
+// elements; element_bits: one bit per element of not_finite's.
+template <bool F8> __device__ inline uint32_t not_finite(uint32_t x) {
+    return F8 ? ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+}
+
+template <bool F8> __device__ inline uint32_t emptied(uint32_t x, uint32_t top) {
     return x & ~(top | (top - (top >> (F8 ? 7 : 15))));
+}
+
+template <bool F8> __device__ inline uint32_t element_bits(uint32_t top) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int e = 0; e < (F8 ? 4 : 2); ++e) bits |= (top >> (F8 ? 8 * e + 7 : 16 * e + 15) & 1u) << e;
+    return bits;
 }
 
 // The sixteen bits from bit `at` (may be negative) of a set of 256.
@@ -269,6 +281,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
     __shared__ PageEntry s_page[kThreads];
     __shared__ uint32_t s_anc[kMaxSeqRows][8];
     __shared__ int s_up[kMaxSeqRows];
+    // where waves share turns: {first key of a turn, which of a lane group's keys in it have values that are not finite},
+    // as the wave found them before it made these zero
+    __shared__ uint2 s_bad[kWaves][4];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int rw = wave % RW, kw = wave / RW;
@@ -373,6 +388,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
         for (int t = 0; t < DT; ++t) o[rt][t] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
     const float sc = fmaxf(fabsf(a.scale) * kLog2eP, 1.17549435e-38f);
+    if (RW > 1 && tid < kWaves * 4) s_bad[tid / 4][tid % 4].x = kNone;       // no key
     auto attend = [&](auto tiles) {                         // the wave's first R row tiles
         constexpr int R = decltype(tiles)::value;
         for (int seg = kbeg; seg < kend; seg += segment) {
@@ -494,28 +510,71 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
                     // places that hold no key of the sequence may hold anything: a weight of zero does not make
                     // a NaN harmless
                     const int real = none ? 0 : min(max(kend - (k0 + g * GK), 0), GK);
-                    const bool some_see = k0 + KS > clear && clear < kend;
+                    constexpr int EW = 4 / EB;                      // elements of a word
+                    if (__ballot(real < GK) != 0) {
 #pragma unroll
-                    for (int c = 0; c < VC; ++c) {
-                        u32x4 keep;
+                        for (int c = 0; c < VC; ++c) {
+                            u32x4 keep;
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            constexpr int EW = 4 / EB;              // elements of a word
-                            const int in = real - (c * 4 + w) * EW;
-                            keep[w] = in >= EW ? 0xffffffffu : in > 0 ? (1u << (in * 8 * EB)) - 1u : 0u;
-                        }
-                        // waves that share the turn store the same, and each word once
-                        if (some_see) {
-#pragma unroll
-                            for (int t = 0; t < DT; ++t) {
-                                u32x4 x = values[(t * VC + c) * 64] & keep;
-#pragma unroll
-                                for (int w = 0; w < 4; ++w) x[w] = finite<F8>(x[w]);
-                                values[(t * VC + c) * 64] = x;
+                            for (int w = 0; w < 4; ++w) {
+                                const int in = real - (c * 4 + w) * EW;
+                                keep[w] = in >= EW ? 0xffffffffu : in > 0 ? (1u << (in * 8 * EB)) - 1u : 0u;
                             }
-                        } else {
+                            // (waves that share the turn store the same)
 #pragma unroll
                             for (int t = 0; t < DT; ++t) values[(t * VC + c) * 64] &= keep;
+                        }
+                    }
+                    if (k0 + KS > clear && clear < kend) {          // some rows do not see all of them
+                        uint32_t top[VC * 4] = {}, any = 0;
+#pragma unroll
+                        for (int c = 0; c < VC; ++c)
+#pragma unroll
+                            for (int t = 0; t < DT; ++t) {
+                                const u32x4 x = values[(t * VC + c) * 64];
+#pragma unroll
+                                for (int w = 0; w < 4; ++w) top[c * 4 + w] |= not_finite<F8>(x[w]);
+                            }
+#pragma unroll
+                        for (int i = 0; i < VC * 4; ++i) any |= top[i];
+                        // Where another wave has made zero what this one would have found, it has said so before: it is
+                        // asked after the search.  (The values are read again for the products: kept in registers
+                        // they spill.)
+                        wait_lds();
+                        uint32_t others = 0;
+                        int here = g;
+                        if constexpr (RW > 1) {
+                            asm volatile("" : "+v"(here));          // (its address in no register between turns)
+                            static_assert(RW == 2, "one other wave");
+                            const uint2 other = s_bad[wave ^ 1][here];
+                            others = other.x == static_cast<uint32_t>(k0) ? other.y : 0u;
+                        }
+                        if (__builtin_expect(__ballot((any | others) != 0) != 0, 0)) {
+                            uint32_t bad = others;                  // keys of this lane group
+#pragma unroll
+                            for (int i = 0; i < VC * 4; ++i) bad |= element_bits<F8>(top[i]) << (i * EW);
+#pragma unroll
+                            for (int off = 1; off < 16; off <<= 1) bad |= __shfl_xor(bad, off);
+                            if constexpr (RW > 1) {
+                                s_bad[wave][here] = make_uint2(k0, bad);
+                                wait_lds();
+                            }
+#pragma unroll
+                            for (int c = 0; c < VC; ++c)
+#pragma unroll
+                                for (int t = 0; t < DT; ++t) {
+                                    u32x4 x = values[(t * VC + c) * 64];
+#pragma unroll
+                                    for (int w = 0; w < 4; ++w) x[w] = emptied<F8>(x[w], not_finite<F8>(x[w]));
+                                    values[(t * VC + c) * 64] = x;
+                                }
+#pragma unroll
+                            for (int rt = 0; rt < R; ++rt)
+#pragma unroll
+                                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                                    for (int r = 0; r < 4; ++r)
+                                        if ((bad >> (4 * t + r) & 1u) && st[rt][t][r] != -INFINITY) st[rt][t][r] = NAN;
                         }
                     }
                 }
@@ -656,8 +715,10 @@ __device__ inline floatx16 mfma32(u32x4 a, u32x4 b, floatx16 c) {
 //
 // S^T = K Q^T: row p of key tile kt is its key 16 (p / 4 % 2) + 4 (p / 8) + p % 4, so that lane half
 // gh's sixteen scores are those of the keys 16 gh + 0 .. 15 in order, P^T's operand as they stand.
+//
+// (three workgroups of e4m3, d = 64 fit on a CU: 95.4 us for such inputs, 101 with the registers of two)
 template <int D, bool F8>
-__global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs a) {
+__global__ __launch_bounds__(kThreads, D == 64 && F8 ? 3 : 2) void k_paged_attention_wide(PagedArgs a) {
     constexpr int KS = 64, KT = KS / 32;                    // keys of a turn, and tiles of them
     constexpr int DS = D / 16, DT = D / 32;                 // k-steps of the first product, component tiles
     constexpr int EB = F8 ? 1 : 2;
@@ -669,6 +730,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs 
     __shared__ PageEntry s_page[kThreads];
     __shared__ uint32_t s_anc[kMaxSeqRows][8];
     __shared__ int s_up[kMaxSeqRows];
+    __shared__ int s_met;                                   // values that are not finite, among keys that not all rows see
+    // with care: the 64 keys of a turn that have such values; of the turn that is worked on, of the one that is staged
+    // meanwhile, and of the one before, which are cleared
+    __shared__ uint32_t s_bad[3][2];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int gh = lane >> 5, l32 = lane & 31;
@@ -727,7 +792,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs 
     };
     // widened into LDS; values of places that hold no key of the sequence become zeros (such places
     // may hold anything, and a weight of zero does not make a NaN harmless)
-    auto stage = [&](int k0, char *to) {
+    // (inlined by request: a call puts what it captures on the stack)
+    auto stage = [&](int k0, char *to, uint32_t *bad, auto with_care) __attribute__((always_inline)) {
+        constexpr bool CARE = decltype(with_care)::value;
 #pragma unroll
         for (int i = 0; i < LK; ++i) {
             const int key = key_at(i), k32 = key & 31;
@@ -747,15 +814,31 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs 
             const int at = comp_piece(i) * (16 / EB);        // first of the piece's keys
             const PageEntry page = page_of(k0 + at);
             const float scale = value_scale(page);
+            constexpr int EW = 4 / EB;
             if (special) {
                 const int real = page.x >= kNone ? 0 : min(max(kend - (k0 + at), 0), 16 / EB);
+                uint32_t met = 0;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    constexpr int EW = 4 / EB;
                     const int in = real - x * EW;
                     vr[i][x] &= in >= EW ? 0xffffffffu : in > 0 ? (1u << (in * 8 * EB)) - 1u : 0u;
-                    if (some_see) vr[i][x] = finite<F8>(vr[i][x]);
+                    if (!CARE && some_see) {
+                        const uint32_t top = not_finite<F8>(vr[i][x]);
+                        met |= top;
+                        vr[i][x] = emptied<F8>(vr[i][x], top);
+                    }
                 }
+                if (!CARE && met != 0) s_met = 1;
+            }
+            if constexpr (CARE) {
+                uint32_t keys = 0;                           // of the piece's, from its first one on
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const uint32_t top = not_finite<F8>(vr[i][x]);
+                    keys |= element_bits<F8>(top) << (x * EW);
+                    vr[i][x] = emptied<F8>(vr[i][x], top);
+                }
+                if (keys) atomicOr(&bad[at >> 5], keys << (at & 31));
             }
             const int d = comp_at(i);
             // operand of component tile d / 32, key tile at / 32, k-step v: keys 16 gh + 8 v ..
@@ -801,27 +884,38 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs 
 
     floatx16 o[DT], ol;                                     // sums, and of the weights alone (rows all alike)
     const u32x4 ones{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+    float m;
+    auto start = [&] {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        ol[i] = 0.f;
+        for (int i = 0; i < 16; ++i) {
+            ol[i] = 0.f;
 #pragma unroll
-        for (int t = 0; t < DT; ++t) o[t][i] = 0.f;
-    }
-    float m = -INFINITY;
+            for (int t = 0; t < DT; ++t) o[t][i] = 0.f;
+        }
+        m = -INFINITY;
+    };
+    start();
+    if (tid == 0) s_met = 0;
 
     // A wave without rows stages its share only (256 groups of 132 rows: 106.6 us, then 100.8).
-    auto attend = [&](auto works) {
-        constexpr bool WORKS = decltype(works)::value;
+    auto attend = [&](auto works, auto with_care) {
+        constexpr bool WORKS = decltype(works)::value, CARE = decltype(with_care)::value;
+        int slot = 0;                                           // of s_bad, of the turn that is staged next
         for (int seg = kbeg; seg < kend; seg += segment) {
             const int seg_end = min(seg + segment, kend);
             if (seg > kbeg || a.splits > 1) id = table_entry(a, b, seg >> a.c.log_page);
             if (seg > kbeg) __syncthreads();                    // the pages of the segment before are used up
             look_up(seg, seg_end, id);
-            stage(seg, s_stage[0]);
+            stage(seg, s_stage[0], s_bad[slot], with_care);
             for (int k0 = seg, buf = 0; k0 < seg_end; k0 += KS, buf ^= 1) {
                 const bool more = k0 + KS < seg_end;
                 lds_barrier();                                  // the turn is staged; the one before is used up
                 if (more) load(k0 + KS);
+                [[maybe_unused]] const uint32_t *const bad = s_bad[slot];
+                if constexpr (CARE) {
+                    slot = slot == 2 ? 0 : slot + 1;
+                    if (tid < 2) s_bad[slot == 2 ? 0 : slot + 1][tid] = 0;
+                }
                 if constexpr (WORKS) {
                     const u32x4 *keys = reinterpret_cast<const u32x4 *>(s_stage[buf]) + lane;
                     const u32x4 *values = reinterpret_cast<const u32x4 *>(s_stage[buf] + kValuesAt) + lane;
@@ -845,6 +939,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs 
 #pragma unroll
                             for (int i = 0; i < 16; ++i)
                                 if (!(see >> i & 1)) st[t][i] = -INFINITY;
+                        }
+                    }
+                    if constexpr (CARE) {
+#pragma unroll
+                        for (int t = 0; t < KT; ++t) {
+                            const uint32_t in = bad[t] >> (16 * gh);    // this lane's keys of the tile
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                if ((in >> i & 1u) && st[t][i] != -INFINITY) st[t][i] = NAN;
                         }
                     }
                     float bm = -INFINITY;
@@ -887,12 +990,22 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention_wide(PagedArgs 
                             for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32(values[((dt * KT + t) * 2 + v) * 64], pb[t][v], o[dt]);
                         }
                 }
-                if (more) stage(k0 + KS, s_stage[buf ^ 1]);
+                if (more) stage(k0 + KS, s_stage[buf ^ 1], s_bad[slot], with_care);
             }
         }
     };
-    if (__ballot(live) == 0) attend(std::false_type{});
-    else attend(std::true_type{});
+    const bool idle = __ballot(live) == 0;
+    if (idle) attend(std::false_type{}, std::false_type{});
+    else attend(std::true_type{}, std::false_type{});
+    if (all_see < kend) {
+        __syncthreads();
+        if (__builtin_expect(uniform(s_met), 0)) {          // once more, with care
+            if (tid < 6) s_bad[tid / 2][tid % 2] = 0;
+            start();
+            id = table_entry(a, b, kbeg >> a.c.log_page);
+            attend(std::true_type{}, std::true_type{});
+        }
+    }
 
     if (!valid) return;
     // O^T tile t, elements 4e .. 4e + 3: d = 32 t + 8 e + 4 gh + 0..3 of this lane's query

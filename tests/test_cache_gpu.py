@@ -607,6 +607,98 @@ def test_padding_beside_bad_values_gets_zeros(dtype, Hq, n_q, more):
     assert not got[0, 4:].float().ne(0).any()
 
 
+def _check_seen(attend, cache, table, masks, bad, side, what):
+    """A bad key or value shows in the results of the queries that see it, and in no other's.  masks as for
+    _check_unseen; bad[b]: positions that get `what` in one component."""
+    want = attend()
+    for b, positions in enumerate(bad):
+        for p in positions:
+            pid, place = int(table[b, p // cache.page]), p % cache.page
+            x, at = (cache.k, (pid, slice(None), place, 5)) if side == "k" else (cache.v, (pid, slice(None), 5, place))
+            x[at] = torch.full((cache.heads,), what).to(x.dtype).to(DEV)
+    got = attend()
+    torch.cuda.synchronize()
+    for b, positions in enumerate(bad):
+        hit = masks[b][:, positions].any(1)
+        assert 0 < int(hit.sum()) < hit.numel()
+        assert torch.equal(got[b][~hit].float(), want[b][~hit].float())
+        assert not torch.isfinite(got[b][hit][..., 5].float()).any()
+
+
+_SEEN = [("v", math.nan), ("v", math.inf), ("k", math.nan), ("k", math.inf)]
+
+
+def _positive_there(q):
+    """Queries whose product with an infinity of _check_seen is plus infinity."""
+    q[..., 5] = q[..., 5].abs() + 0.1
+    return q.to(BF16).to(DEV)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("D,P", [(128, 32), (64, 16), (128, 128)])
+@pytest.mark.parametrize("B,Hq,H,times,more", _ROWS)
+@pytest.mark.parametrize("side,what", _SEEN)
+def test_tree_bad_nodes_show(dtype, D, P, B, Hq, H, times, more, side, what):
+    # two nodes, in different pages where trees are large
+    N = 20 * times
+    ctx = [3 * P + 11] * B
+    T = (max(ctx) + N + P - 1) // P
+    table, n_pages = ref.make_table(B, T, 5)
+    cache = _filled(table, n_pages, H, D, P, dtype, [c + N for c in ctx], 5)
+    parent = [_random_tree(N, b, near=4) for b in range(B)]
+    q = _positive_there(torch.randn(B, N, Hq, D, generator=_gen(6)))
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    args = (q, cache, _longer(table, more).to(DEV), i32(ctx), i32(parent), D ** -0.5)
+    masks, bad = [], []
+    for b in range(B):
+        mask = torch.ones(N, ctx[b] + N, dtype=torch.bool)
+        mask[:, ctx[b]:] = ref.ancestors(parent[b])
+        masks.append(mask)
+        bad.append([ctx[b] + 3 + b % 3, ctx[b] + N - 1])
+    _check_seen(lambda: cs.tree_attention(*args), cache, table, masks, bad, side, what)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("D,P", [(128, 32), (64, 16), (128, 128)])
+@pytest.mark.parametrize("B,Hq,H,times,more", _ROWS)
+@pytest.mark.parametrize("side,what", _SEEN)
+def test_hybrid_bad_positions_show(dtype, D, P, B, Hq, H, times, more, side, what):
+    # context queries on both sides of a bad position, and padding
+    n_q, K = 20 * times + 25, 3
+    ctx = [2 * P + 20 * times] * B
+    lengths = [c + 2 * K + 3 for c in ctx]
+    table, n_pages = ref.make_table(B, (lengths[0] + P - 1) // P, 7)
+    cache = _filled(table, n_pages, H, D, P, dtype, lengths, 7)
+    start = [2 * P - 3] * B
+    q = _positive_there(torch.randn(B, n_q, Hq, D, generator=_gen(8)))
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    args = (q, cache, _longer(table, more).to(DEV), i32(ctx), i32(start), K, D ** -0.5)
+    sees = torch.tensor(ref.hybrid_sees(ctx[0], start[0], n_q, K, lengths[0]))
+    masks = [torch.arange(lengths[0]) < sees[:, None]] * B
+    bad = [[2 * P + 2 + b % 7] for b in range(B)]
+    _check_seen(lambda: cs.hybrid_attention_paged(*args), cache, table, masks, bad, side, what)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("more", [0, 3000])
+def test_bad_values_show_where_pages_are_looked_up_anew(dtype, more):
+    # in the last turn before the 253rd page and the first one behind it, which waves share (52 rows a group) or
+    # not; one row in turns that others see in part, and several segments after one another
+    for B, n_q, Hq in ((1, 13, 32), (32, 13, 32), (4, 70, 32)):
+        for at in (252 * 16 - 2, 252 * 16, 252 * 16 + 70):
+            ctx, K, P = [252 * 16 + 90] * B, 2, 16
+            lengths = [c + 2 * K + 3 for c in ctx]
+            table, n_pages = ref.make_table(B, (lengths[0] + P - 1) // P, 9)
+            cache = _filled(table, n_pages, 8, 64, P, dtype, lengths, 9)
+            q = torch.randn(B, n_q, Hq, 64, generator=_gen(10)).to(BF16).to(DEV)
+            start = [at - 6] * B
+            i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+            args = (q, cache, _longer(table, more).to(DEV), i32(ctx), i32(start), K, 0.125)
+            sees = torch.tensor(ref.hybrid_sees(ctx[0], start[0], n_q, K, lengths[0]))
+            masks = [torch.arange(lengths[0]) < sees[:, None]] * B
+            _check_seen(lambda: cs.hybrid_attention_paged(*args), cache, table, masks, [[at]] * B, "v", math.nan)
+
+
 def _check_keep(dtype, D, P, H, ctx, path, N, T=None, seed=0):
     B = len(ctx)
     T = T or (max(max(c, 0) for c in ctx) + N + P - 1) // P
