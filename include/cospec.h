@@ -558,7 +558,8 @@ cospec_status cospec_cache_keep(const cospec_cache *cache, const int32_t *ctx_le
  *       outside [0, l), or that sees only positions on no page, gets zeros.
  * fp32 sums; the attention weights enter the second product, and their sum, rounded to bf16;
  * e4m3 keys and values times their scale are taken exactly (scales by their power of two, of
- * more than 2^119 as 2^119).
+ * more than 2^120, which cospec_cache_append does not write, as 2^120; above 240 * 2^120 they
+ * are infinite).
  *  workspace  256-byte aligned, at least cospec_paged_attention_workspace_size(cache, B, n_q,
  *             Hq) bytes (0: none is needed, and NULL will do): few query groups are
  *             cut into pieces of their keys, by each sequence's own length, and merged by

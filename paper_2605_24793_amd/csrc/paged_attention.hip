@@ -123,11 +123,14 @@ __device__ inline int seen_by_all(const PagedArgs &a, const Seq &s, int q0, int 
 
 // Values that are not finite, among keys that some rows see and others do not.  A weight of zero would not keep them
 // from the others: they are made zero, and the weights of the rows that do see such a key NaN.
-// not_finite: the highest bit of every such element of four bytes; emptied: the four bytes without these
-// elements; element_bits: one bit per element of not_finite's.
-template <bool F8> __device__ inline uint32_t not_finite(uint32_t x) {
-    return F8 ? ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+// not_finite: the highest bit of every such element of four bytes (e4m3: `carry` is 0x01010101, or at the scale 2^120
+// 0x08080808, as more than 240 times that is not finite in bf16); emptied: the four bytes without these elements;
+// element_bits: one bit per element of not_finite's.
+template <bool F8> __device__ inline uint32_t not_finite(uint32_t x, uint32_t carry) {
+    return F8 ? ((x & 0x7f7f7f7fu) + carry) & 0x80808080u : ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
 }
+
+__device__ inline uint32_t carry_of(float scale) { return scale < 1.329227995784916e36f ? 0x01010101u : 0x08080808u; }
 
 template <bool F8> __device__ inline uint32_t emptied(uint32_t x, uint32_t top) {
     return x & ~(top | (top - (top >> (F8 ? 7 : 15))));
@@ -232,10 +235,9 @@ __device__ inline Place place_of(const PagedArgs &a) {
 typedef uint2 PageEntry;
 constexpr uint32_t kNone = 0x80000000u;
 
-// (448 times 2^119 is still finite as bf16: no scale, of a page in use or not, makes a zero or a finite
-// value anything else)
+// (2^120 is the largest scale that an append writes; no scale, of a page in use or not, makes a zero anything else)
 __device__ inline uint32_t pack_scales(float k, float v) {
-    const uint32_t most = 0x7b000000u;
+    const uint32_t most = 0x7b800000u;
     return min(__float_as_uint(k) & 0x7f800000u, most) | min(__float_as_uint(v) & 0x7f800000u, most) >> 16;
 }
 __device__ inline float key_scale(PageEntry e) { return __uint_as_float(e.y & 0xffff0000u); }
@@ -527,13 +529,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
                     }
                     if (k0 + KS > clear && clear < kend) {          // some rows do not see all of them
                         uint32_t top[VC * 4] = {}, any = 0;
+                        const uint32_t carry = carry_of(vsc);
 #pragma unroll
                         for (int c = 0; c < VC; ++c)
 #pragma unroll
                             for (int t = 0; t < DT; ++t) {
                                 const u32x4 x = values[(t * VC + c) * 64];
 #pragma unroll
-                                for (int w = 0; w < 4; ++w) top[c * 4 + w] |= not_finite<F8>(x[w]);
+                                for (int w = 0; w < 4; ++w) top[c * 4 + w] |= not_finite<F8>(x[w], carry);
                             }
 #pragma unroll
                         for (int i = 0; i < VC * 4; ++i) any |= top[i];
@@ -565,7 +568,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
                                 for (int t = 0; t < DT; ++t) {
                                     u32x4 x = values[(t * VC + c) * 64];
 #pragma unroll
-                                    for (int w = 0; w < 4; ++w) x[w] = emptied<F8>(x[w], not_finite<F8>(x[w]));
+                                    for (int w = 0; w < 4; ++w) x[w] = emptied<F8>(x[w], not_finite<F8>(x[w], carry));
                                     values[(t * VC + c) * 64] = x;
                                 }
 #pragma unroll
@@ -823,7 +826,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && F8 ? 3 : 2) void k_paged_atten
                     const int in = real - x * EW;
                     vr[i][x] &= in >= EW ? 0xffffffffu : in > 0 ? (1u << (in * 8 * EB)) - 1u : 0u;
                     if (!CARE && some_see) {
-                        const uint32_t top = not_finite<F8>(vr[i][x]);
+                        const uint32_t top = not_finite<F8>(vr[i][x], 0x01010101u);
                         met |= top;
                         vr[i][x] = emptied<F8>(vr[i][x], top);
                     }
@@ -834,7 +837,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && F8 ? 3 : 2) void k_paged_atten
                 uint32_t keys = 0;                           // of the piece's, from its first one on
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const uint32_t top = not_finite<F8>(vr[i][x]);
+                    const uint32_t top = not_finite<F8>(vr[i][x], carry_of(scale));
                     keys |= element_bits<F8>(top) << (x * EW);
                     vr[i][x] = emptied<F8>(vr[i][x], top);
                 }
@@ -862,7 +865,10 @@ __global__ __launch_bounds__(kThreads, D == 64 && F8 ? 3 : 2) void k_paged_atten
         if (F8 && in) scales = pack_scales(a.c.k_scale[at], a.c.v_scale[at]);
         any_none = __syncthreads_or(in && none);
         load(from);
-        if (F8 && in) s_page[tid].y = scales;
+        if (F8 && in) {
+            s_page[tid].y = scales;
+            if (carry_of(__uint_as_float(scales << 16)) != 0x01010101u) s_met = 1;   // values over 240 need care
+        }
         __syncthreads();
     };
     if (a.parent) find_ancestors(a, b, s_anc, s_up);

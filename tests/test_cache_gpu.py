@@ -427,6 +427,32 @@ def test_scales_count_by_their_power_of_two():
     assert _same(cs.hybrid_attention_paged(q, cache, table.to(DEV), ctx, ctx, 1, 0.125), want)
 
 
+@pytest.mark.parametrize("B,H,Hq,more", [(1, 2, 4, 0), (32, 8, 416, 40), (1, 1, 256, 3000)])
+def test_the_largest_scale_is_read_as_it_was_written(B, H, Hq, more):
+    """Values that need the scale 2^120: those up to 240 times it are finite in bf16 and come back; one query per
+    head that sees one position, in every kernel, with others behind it that it does not see."""
+    D, P, n = 64, 16, 3
+    table, n_pages = ref.make_table(B, 1, 3)
+    cache = cs.PagedCache.empty(n_pages, H, D, P, F8, DEV)
+    v = torch.tensor([1.796875, 1.875, -1.796875, -1.9296875, 1.75, -1.0, 2.0 ** -8, 0.0]).double() * 2.0 ** 127
+    v = v.to(BF16).repeat(D // 8).expand(B, n, H, D).contiguous()
+    k = torch.zeros(B, n, H, D, dtype=BF16)
+    i32 = lambda x: torch.tensor([x] * B, dtype=torch.int32, device=DEV)  # noqa: E731
+    cs.cache_append(cache, table.to(DEV), i32(0), k.to(DEV), v.to(DEV))
+    assert (cache.v_scale[table[:, 0].long().to(DEV)] == 2.0 ** 120).all()
+    _bits(cache.v)[:, :, :, 2] = 126                        # 448: what nobody sees, were it read
+    q = torch.zeros(B, 1, Hq, D, dtype=BF16, device=DEV)
+    got = cs.hybrid_attention_paged(q, cache, _longer(table, more).to(DEV), i32(1), i32(0), 0, 0.125).cpu().double()
+    want = v[:, :1, :1].double().expand_as(got)
+    # half a step of e4m3 (subnormals: 2^-10 of the scale); what it gives is exact in bf16
+    assert ((got - want).abs() <= torch.maximum(2.0 ** -4 * want.abs(), torch.tensor(2.0 ** 110).double())).all()
+    # two of the three positions seen, by a tree's node, beside another that sees the third
+    parent = torch.tensor([[-1, 0, 0]] * B, dtype=torch.int32, device=DEV)
+    q = torch.zeros(B, n, Hq, D, dtype=BF16, device=DEV)
+    got = cs.tree_attention(q, cache, _longer(table, more).to(DEV), i32(0), parent, 0.125)[:, :1].cpu().double()
+    assert ((got - want).abs() <= torch.maximum(2.0 ** -4 * want.abs(), torch.tensor(2.0 ** 110).double())).all()
+
+
 def _check_tree(dtype, D, P, Hq, H, ctx, parent, T=None, seed=0, more=0, only=None):
     B, N = len(ctx), len(parent[0])
     T = T or (max(max(c, 0) for c in ctx) + N + P - 1) // P
