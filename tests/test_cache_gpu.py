@@ -138,6 +138,15 @@ def test_append_rotations(dtype, rot, interleaved):
 
 
 @pytest.mark.parametrize("dtype", [F8, BF16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rot,P,n,start", [(128, 128, 117, [9, 100]), (64, 128, 130, [0, 77]), (48, 16, 20, [5, 16]),
+                                           (128, 32, 1, [31, 32]), (112, 64, 70, [60, 1])])
+def test_append_rotations_of_wide_heads(dtype, interleaved, rot, P, n, start):
+    # d = 128: eight units a token, up to four of a thread; all of the components rotated, or the first ones
+    _check_append(dtype, 128, P, 2, n, start, rot=rot, interleaved=interleaved, Hq=3, strided=True, seed=rot + n)
+
+
+@pytest.mark.parametrize("dtype", [F8, BF16])
 def test_append_positions_and_counts(dtype):
     # tree nodes rotated to their depth, far positions, counts of nothing, too many, too few
     n, start = 6, [10, 61, 0, 5, 40]
