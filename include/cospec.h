@@ -506,7 +506,7 @@ typedef struct {
 
 /*
  * Appends new positions to the cache: token i < count[b] of sequence b goes to position
- * start[b] + i, its key rotated.  Places it does not write keep what they hold.  Positions
+ * start[b] + i, its key rotated.  Places it does not write keep their bytes.  Positions
  * written before are overwritten (a round's rejected tokens need no removal).
  *  start, count  [B] int32; count NULL: n everywhere (values are clamped to [0, n]).
  *                Positions outside [0, max_pages * page) or on no page are not written.
@@ -522,8 +522,10 @@ typedef struct {
  * COSPEC_F8E4M3: the scale of a page and head becomes the smallest power of two s (at least
  * 2^-100) with |x| <= 448 s for the finite new values x that go there, but not below its
  * present scale when the page holds earlier positions of the sequence (start[b] is not the
- * page's first): then it only grows, and the earlier values are rounded anew (exactly, unless
- * they become subnormal).  Rounding is to nearest even; infinities and NaN become NaN.
+ * page's first; they must have been appended, as that is what gives a page its scale): then it only
+ * grows, and the earlier values are rounded anew (exactly, unless they become subnormal).  Later
+ * positions in the pages written are taken for the sequence's no longer: their bytes stand under the
+ * new scale.  Rounding is to nearest even; infinities and NaN become NaN.
  */
 cospec_status cospec_cache_append(const cospec_cache *cache, const int32_t *start, const int32_t *count,
                                   const void *k, int64_t ld_k, const void *v, int64_t ld_v,
@@ -563,7 +565,9 @@ cospec_status cospec_cache_keep(const cospec_cache *cache, const int32_t *ctx_le
  *  workspace  256-byte aligned, at least cospec_paged_attention_workspace_size(cache, B, n_q,
  *             Hq) bytes (0: none is needed, and NULL will do): few query groups are
  *             cut into pieces of their keys, by each sequence's own length, and merged by
- *             a second kernel.
+ *             a second kernel.  How many pieces a launch has room for, and how few rows a workgroup
+ *             takes, goes by the table: few short sequences are faster with max_pages close to what
+ *             they need.
  */
 size_t cospec_paged_attention_workspace_size(const cospec_cache *cache, int32_t B, int32_t n_q, int32_t Hq);
 

@@ -700,7 +700,8 @@ def _on_current(dev: torch.device):
 class CacheCall:
     """Pre-marshalled arguments of one call on a paged cache: `outputs` and the workspace are
     allocated once, so `launch()` enqueues it, on torch's current stream, with no allocation.  The
-    tensors it was prepared with are kept, and read anew by every launch."""
+    tensors it was prepared with are kept, and read anew by every launch.  Launches that may overlap in
+    time (two streams, two captured graphs) need calls of their own: they would share these."""
 
     def __init__(self, fn, args, outputs, device, keep, workspace=None, ws_bytes=None):
         self._fn, self._device, self._keep = fn, device, keep
@@ -757,7 +758,8 @@ def prepare_cache_append(cache: PagedCache, table, start, k, v, count: Optional[
     """Pre-marshalled cospec_cache_append: tokens k, v [B, n, heads, d] go to positions start[b] ..
     start[b] + count[b] - 1 (int32 [B]; count None: n), keys rotated with inv_freq (f32
     [rot / 2]; None: not rotated) to positions (int32 [B, n]; None: where they go).  q
-    [B, n, Hq, d]: queries to rotate as well, into outputs["q"]."""
+    [B, n, Hq, d]: queries to rotate as well, into outputs["q"].  In float8_e4m3fn pages, positions
+    behind the new ones are no longer the sequence's (their page's scale may change)."""
     if k.dim() != 4:
         raise ValueError("k must be [B, n, heads, d]")
     B, n = int(k.shape[0]), int(k.shape[1])

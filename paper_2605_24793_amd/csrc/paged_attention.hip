@@ -22,6 +22,11 @@
 // second product's operand P^T, and the values it needs for them are 16 keys in a row: with
 // values kept [d][place] they are 16 (e4m3) or 32 (bf16) contiguous bytes.
 //
+// The weights are rounded to bf16 for that product, and l sums the rounded ones (in fp32, by the matrix cores: 16 additions
+// a query and turn less on the vector unit), so that what rounding does to all of them alike leaves the
+// quotient.  Relative error against 64 bits: 0.0017 to 0.0020, with weights and sums of 32 bits 0.0017, which is the
+// output's own rounding.
+//
 // e4m3: v_cvt_scalef32_pk_bf16_fp8 widens two elements and applies the page's power of two;
 // e4m3 has fewer bits than bf16, so nothing is rounded, and one conversion serves all rows.
 #include <algorithm>
@@ -1132,6 +1137,10 @@ PagedPlan paged_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq) {
     PagedPlan p{1, 1, 0, 1, kMinPiece, static_cast<int64_t>(B) * n_q * Hq, 0};
     const int64_t tiles = (static_cast<int64_t>(n_q) * (Hq / c.H) + 15) / 16;
     if (B <= 0 || tiles == 0) return p;
+    // The lengths are on the device: the rules below go by the table's room, so the figures are of tables
+    // cut to the sequences.  With room for 32768 positions few short sequences get larger workgroups, pieces that stay
+    // empty and a join with nothing to join: one sequence of 334 positions 8.2 us and 19.4, a token after
+    // 300 8.5 and 13.9, a tree of 38 nodes after 1000 positions 12.5 and 20.1.
     const int64_t groups = static_cast<int64_t>(B) * c.H, room = static_cast<int64_t>(c.max_pages) << c.log_page;
     const int64_t pieces = (room + kMinPiece - 1) / kMinPiece;
     int64_t per_block = 0;                                  // row tiles of a workgroup
