@@ -718,8 +718,8 @@ def test_hybrid_bad_positions_show(dtype, D, P, B, Hq, H, times, more, side, wha
 @pytest.mark.parametrize("more", [0, 3000])
 def test_bad_values_show_where_pages_are_looked_up_anew(dtype, more):
     # in the last turn before the 253rd page and the first one behind it, which waves share (52 rows a group) or
-    # not; one row in turns that others see in part, and several segments after one another
-    for B, n_q, Hq in ((1, 13, 32), (32, 13, 32), (4, 70, 32)):
+    # not; many rows, cut over the keys and not
+    for B, n_q, Hq in ((1, 13, 32), (32, 13, 32), (4, 70, 32), (8, 70, 32)):
         for at in (252 * 16 - 2, 252 * 16, 252 * 16 + 70):
             ctx, K, P = [252 * 16 + 90] * B, 2, 16
             lengths = [c + 2 * K + 3 for c in ctx]
