@@ -21,8 +21,8 @@
  * This library computes that step on the GPU from logits, draft tokens,
  * arbitrator hidden states and head weights, and returns accept lengths and the
  * emitted tokens, plus optional per-row and per-decision features.  The attentions around
- * it (the arbitrator's, and a token tree's under the target model) and the paged cache
- * they read follow after it.
+ * it (the arbitrator's, and a token tree's under the target model) and the paged caches
+ * they read (keys and values, or latent vectors) follow after it.
  *
  * Conventions shared by every entry point
  *  - Array arguments are DEVICE pointers on the current HIP device, owned by the
@@ -56,7 +56,7 @@
 extern "C" {
 #endif
 
-#define COSPEC_ABI_VERSION 5
+#define COSPEC_ABI_VERSION 6
 #define COSPEC_MAX_K 64      /* chain: draft tokens per block              */
 #define COSPEC_MAX_N 256     /* tree: nodes per tree, root included        */
 #define COSPEC_MAX_SPLITS 64 /* workgroups per logit row (tuning override) */
@@ -80,7 +80,7 @@ typedef enum {
     COSPEC_F32 = 0,
     COSPEC_BF16 = 1,
     COSPEC_F8E4M3 = 2 /* 8 bits: 1 sign, 4 exponent, 3 mantissa bits, no infinity; pages of a
-                         cospec_cache only */
+                         cospec_cache or cospec_latent_cache only */
 } cospec_dtype;
 
 /*
@@ -589,6 +589,177 @@ cospec_status cospec_hybrid_attention_paged(const void *q, const cospec_cache *c
 cospec_status cospec_tree_attention(const void *q, const cospec_cache *cache, const int32_t *ctx_len,
                                     const int32_t *parent, int32_t B, int32_t N, int32_t Hq, float scale, void *out,
                                     void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Paged cache of latent vectors, for attention layers whose heads share one vector a token: keys and
+ * values of every head are linear in it (k_h = U_h c, v_h = W_h c), beside a short key that all heads
+ * share and that is rotated to its position.  Positions lie in pages as in a cospec_cache.
+ *  dtype      of c: COSPEC_BF16 or COSPEC_F8E4M3.
+ *  page       16, 32, 64 or 128;  d_c 256 or 512, the latents' components;  the rotated keys have 64.
+ *  c          [n_pages][page][d_c], r [n_pages][page][64] bf16; 16-byte aligned.
+ *  scale      [n_pages][page] f32, COSPEC_F8E4M3 only (else ignored): element x of a position's
+ *             latent stands for x * scale (finite; cospec_latent_append sets powers of two).  4-byte aligned.
+ *  table      [B][max_pages] int32, as in a cospec_cache.
+ */
+#define COSPEC_LATENT_ROT 64
+
+typedef struct {
+    cospec_dtype dtype;
+    int32_t page;
+    int32_t d_c;
+    int64_t n_pages;
+    void *c;
+    void *r;
+    float *scale;
+    const int32_t *table;
+    int32_t max_pages;
+} cospec_latent_cache;
+
+/*
+ * Appends new positions to a latent cache: token i < count[b] of sequence b goes to position
+ * start[b] + i, its latent normalised and its key rotated.  Places it does not write keep their bytes.
+ *  start, count, positions, rope  as in cospec_cache_append; rope->rot at most 64.
+ *  c          bf16, token i of sequence b at element (b * n + i) * ld_c; ld_c a multiple of 8, at
+ *             least d_c.
+ *  k_r        bf16, 64 components at element (b * n + i) * ld_r; ld_r a multiple of 8, at least 64
+ *             (c and k_r may be slices of one projection's output).
+ *  weight     [d_c] bf16: the latent becomes c / sqrt(mean(c^2) + eps) * weight; NULL: as it is.  eps >= 0.
+ *  q          queries' rotated part, or NULL: bf16, head h of a token at element (b * n + i) * ld_q +
+ *             h * head_q, 64 components there, rotated to q_out, where token and head lie at
+ *             ((b * n + i) * Hq + h) * head_out.  ld_q, head_q, head_out multiples of 8; head_q
+ *             and head_out at least 64.  (With head_out = d_c + 64 and q_out 64 from the end of
+ *             a head, this fills the last part of cospec_latent_attention's queries.)
+ *  c_out      [B][n][d_c] bf16, or NULL: the normalised latents;  k_out [B][n][64] bf16, or NULL: the
+ *             rotated keys (for an expanded form of the same tokens).
+ * q_out, c_out and k_out are written for all n tokens, whatever count says.  COSPEC_F8E4M3: a
+ * position's scale becomes the smallest power of two s (at least 2^-100) with |x| <= 448 s for its
+ * finite values x.  Rounding is to nearest even; in 8 bits infinities and NaN become NaN.
+ */
+cospec_status cospec_latent_append(const cospec_latent_cache *cache, const int32_t *start, const int32_t *count,
+                                   const void *c, int64_t ld_c, const void *k_r, int64_t ld_r, const void *weight,
+                                   float eps, const cospec_rope *rope, const int32_t *positions, int32_t B, int32_t n,
+                                   const void *q, int64_t ld_q, int64_t head_q, int32_t Hq, void *q_out,
+                                   int64_t head_out, void *c_out, void *k_out, hipStream_t stream);
+
+/* cospec_cache_keep for a latent cache; bytes and scales move as they are. */
+cospec_status cospec_latent_keep(const cospec_latent_cache *cache, const int32_t *ctx_len, const int32_t *path,
+                                 int32_t B, int32_t N, hipStream_t stream);
+
+/*
+ * Attention over a latent cache in the absorbed form: query head h, taken through U_h beforehand, meets
+ * the latents themselves, and its result is a mean of latents, which the caller takes through W_h:
+ *   score_j = scale * (q[0 .. d_c) . c_j + q[d_c .. d_c + 64) . r_j),  out = sum_j softmax(score)_j c_j
+ *  q    [B][n_q][Hq][d_c + 64] bf16, any Hq >= 1;  out [B][n_q][Hq][d_c] bf16.  16-byte aligned.
+ * cospec_latent_attention sees the keys of cospec_hybrid_attention_paged (n_q = 1, q_start = l_c - 1: plain
+ * decoding; q_start = l_c - n_q: the last n_q positions of a context; q_start = l_c: the region),
+ * cospec_latent_tree_attention those of cospec_tree_attention; queries outside, or that see only positions on no
+ * page, get zeros.  What a query does not see does not reach it, whatever it holds; a position
+ * that it sees makes some or all of its result NaN or infinite if its latent or scale is not finite, or if
+ * its score is NaN or plus infinity.
+ * fp32 sums; the weights enter the second product rounded to bf16, e4m3 latents are taken exactly.  Latents of
+ * more than 2^60 may overflow.
+ *  workspace  as in cospec_hybrid_attention_paged, of cospec_latent_attention_workspace_size(cache, B, n_q, Hq)
+ *             bytes.
+ */
+size_t cospec_latent_attention_workspace_size(const cospec_latent_cache *cache, int32_t B, int32_t n_q, int32_t Hq);
+
+cospec_status cospec_latent_attention(const void *q, const cospec_latent_cache *cache, const int32_t *ctx_len,
+                                      const int32_t *q_start, int32_t B, int32_t n_q, int32_t Hq, int32_t K, float scale,
+                                      void *out, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+cospec_status cospec_latent_tree_attention(const void *q, const cospec_latent_cache *cache, const int32_t *ctx_len,
+                                           const int32_t *parent, int32_t B, int32_t N, int32_t Hq, float scale,
+                                           void *out, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * The same attention in the expanded form, for whole inputs: every head has keys and values of its own,
+ * expanded from the latents, beside the shared rotated key; not paged.
+ *   score_j = scale * (q[0 .. d) . k_j^h + q[d .. d + 64) . r_j),  out = sum_j softmax(score)_j v_j^h
+ *  q      [B][n_q][H][d + 64] bf16;  out [B][n_q][H][d] bf16;  d 64 or 128.
+ *  k, v   bf16: position j of sequence b and head h at element (b * L + j) * ld_k + h * head_k (ld_v, head_v), d
+ *         components there, so the two halves of one projection's heads are taken as they are.
+ *  k_r    bf16: 64 components at element (b * L + j) * ld_r.
+ *         Strides are multiples of 8, head strides at least d, ld_r at least 64.  Arrays 16-byte aligned.
+ * Masks, padding queries, keys past L and values that are not finite as in cospec_hybrid_attention_paged.
+ */
+cospec_status cospec_expanded_attention(const void *q, const void *k, int64_t ld_k, int64_t head_k, const void *v,
+                                        int64_t ld_v, int64_t head_v, const void *k_r, int64_t ld_r,
+                                        const int32_t *ctx_len, const int32_t *q_start, int32_t B, int32_t n_q,
+                                        int32_t L, int32_t H, int32_t d, int32_t K, float scale, void *out,
+                                        hipStream_t stream);
+
+/*
+ * The pages under the caches of a model's layers.  One table serves all layers, and a pool counts for
+ * each page how many table entries name it (0: free), so that sequences can share the pages of a common
+ * beginning.  All of it lives on the device; nothing is read back.  Entries outside [0, n_pages) name no
+ * page.  The results are the same every time: which page is taken follows from the counts alone.
+ *  refs   [n_pages] int32;  page 16, 32, 64 or 128, as the caches'.
+ * Every entry of the tables in use is counted once (fork, reserve, release and compact keep it so); calls on one
+ * pool must not overlap in time.
+ */
+typedef struct {
+    int32_t *refs;
+    int64_t n_pages;
+    int32_t page;
+} cospec_page_pool;
+
+/*
+ * Sequences that go on from others: row b of table_to ([B][max_pages], not overlapping table) becomes the
+ * entries of row row[b] of table ([rows][max_pages]) for its first len[b] positions, which both then
+ * share, and -1 behind them.  row[b] outside [0, rows) gives a row of -1; len is clamped to
+ * [0, max_pages * page].  What the row held before is not released.
+ */
+cospec_status cospec_pages_fork(const cospec_page_pool *pool, const int32_t *table, int32_t rows, const int32_t *row,
+                                const int32_t *len, int32_t B, int32_t max_pages, int32_t *table_to,
+                                hipStream_t stream);
+
+/*
+ * Room for new positions: afterwards positions start[b] .. start[b] + count[b] - 1 of every sequence lie on
+ * pages of its own.  (start, count as in cospec_cache_append; positions outside the table are left out.)
+ * An entry that names no page gets one, and an entry whose page others hold too gets another one instead; pages
+ * are the free ones of lowest number, in the order of the sequences and their positions.
+ *  copies  [B][2] out: {from, to} where the sequence's first new position lies inside a page that was shared, whose
+ *          earlier positions it needs a copy of (cospec_pages_copy), else {-1, -1}.
+ *  lacking [1] out: 0, or how many pages are missing; then nothing is changed, and copies are -1.
+ *  workspace 256-byte aligned, cospec_pages_reserve_workspace_size(pool, B, n) bytes.
+ */
+size_t cospec_pages_reserve_workspace_size(const cospec_page_pool *pool, int32_t B, int32_t n);
+
+cospec_status cospec_pages_reserve(const cospec_page_pool *pool, int32_t *table, int32_t max_pages, const int32_t *start,
+                                   const int32_t *count, int32_t B, int32_t n, int32_t *copies, int32_t *lacking,
+                                   void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Gives back the pages behind each sequence's first keep[b] positions (negative values act as 0): their
+ * entries become -1, and pages that no entry names any more are free. */
+cospec_status cospec_pages_release(const cospec_page_pool *pool, int32_t *table, int32_t max_pages, const int32_t *keep,
+                                   int32_t B, hipStream_t stream);
+
+/*
+ * Moves the pages in use to the front: with U of them, those numbered U and above take, in order, the free numbers
+ * below U.  table must hold every entry that names a page of the pool.
+ *  moves    [max(n_pages / 2, 1)][2] out: {from, to}, then {-1, -1};  n_moves [1] out.  (cospec_pages_copy moves
+ *           what the pages hold.)
+ *  workspace 256-byte aligned, cospec_pages_compact_workspace_size(pool) bytes.
+ */
+size_t cospec_pages_compact_workspace_size(const cospec_page_pool *pool);
+
+cospec_status cospec_pages_compact(const cospec_page_pool *pool, int32_t *table, int32_t max_pages, int32_t B,
+                                   int32_t *moves, int32_t *n_moves, void *workspace, size_t workspace_bytes,
+                                   hipStream_t stream);
+
+/*
+ * Copies pages from[i] -> to[i] (pairs [n_pairs][2]; the first *count of them when count is not NULL, device) in
+ * every plane: an array of n_pages pages of page_bytes each (a multiple of 4; data 4-byte aligned), such as the
+ * keys, the values or the scales of one layer's cache.  A pair with a page outside [0, n_pages), or of a page and
+ * itself, is left out.  A page that is copied to must not be in another pair.
+ */
+typedef struct {
+    void *data;
+    int64_t page_bytes;
+} cospec_page_plane;
+
+cospec_status cospec_pages_copy(const cospec_page_plane *planes, int32_t n_planes, int64_t n_pages,
+                                const int32_t *pairs, int32_t n_pairs, const int32_t *count, hipStream_t stream);
 
 /*
  * How a whole step of these sizes runs its head's first layer (n: draft tokens K of a chain,

@@ -12,7 +12,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libcospec.so")
 SOURCES = ["cospec_api.hip", "reduce.hip", "sample.hip", "head.hip", "scan.hip", "sps.hip", "attention.hip",
-           "cache.hip", "paged_attention.hip", "cache_api.hip"]
+           "cache.hip", "paged_attention.hip", "cache_api.hip", "latent.hip", "latent_attention.hip", "expanded_attention.hip",
+           "pages.hip", "latent_api.hip"]
 HEADERS = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")) + \
     [os.path.join(INCLUDE, "cospec.h")]
 

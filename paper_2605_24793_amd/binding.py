@@ -19,7 +19,12 @@ __all__ = ["lib", "verify_block", "verify_block_static", "verify_tree", "arbitra
            "prepare_block", "prepare_tree", "prepare_sps", "SplitBlock", "sps_block", "hybrid_mask",
            "hybrid_attention", "PagedCache", "CacheCall", "prepare_cache_append", "cache_append",
            "prepare_cache_keep", "cache_keep", "prepare_hybrid_attention_paged", "hybrid_attention_paged",
-           "prepare_tree_attention", "tree_attention", "status_string", "MAX_K",
+           "prepare_tree_attention", "tree_attention", "LatentCache", "prepare_latent_append", "latent_append",
+           "prepare_latent_keep", "latent_keep", "prepare_latent_attention", "latent_attention",
+           "prepare_latent_tree_attention", "latent_tree_attention", "prepare_expanded_attention",
+           "expanded_attention", "PagePool", "PoolCall", "prepare_pages_fork", "pages_fork", "prepare_pages_reserve",
+           "pages_reserve", "prepare_pages_release", "pages_release", "prepare_pages_compact", "pages_compact",
+           "prepare_pages_copy", "pages_copy", "status_string", "MAX_K",
            "MAX_N", "MAX_SPLITS"]
 
 MAX_K, MAX_N, MAX_SPLITS = 64, 256, 64
@@ -68,6 +73,20 @@ class _Cache(ctypes.Structure):
                 ("d", ctypes.c_int32), ("n_pages", ctypes.c_int64), ("k", ctypes.c_void_p),
                 ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("table", ctypes.c_void_p), ("max_pages", ctypes.c_int32)]
+
+
+class _LatentCache(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("page", ctypes.c_int32), ("d_c", ctypes.c_int32),
+                ("n_pages", ctypes.c_int64), ("c", ctypes.c_void_p), ("r", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p), ("table", ctypes.c_void_p), ("max_pages", ctypes.c_int32)]
+
+
+class _Pool(ctypes.Structure):
+    _fields_ = [("refs", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page", ctypes.c_int32)]
+
+
+class _Plane(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("page_bytes", ctypes.c_int64)]
 
 
 class _Rope(ctypes.Structure):
@@ -159,6 +178,36 @@ def lib():
         L.cospec_hybrid_attention_paged.argtypes = [P, CP, P, P, I32, I32, I32, I32, ctypes.c_float, P, P, SZ, P]
         L.cospec_tree_attention.restype = I32
         L.cospec_tree_attention.argtypes = [P, CP, P, P, I32, I32, I32, ctypes.c_float, P, P, SZ, P]
+        LP, F32 = ctypes.POINTER(_LatentCache), ctypes.c_float
+        L.cospec_latent_append.restype = I32
+        L.cospec_latent_append.argtypes = [LP, P, P, P, I64, P, I64, P, F32, ctypes.POINTER(_Rope), P, I32, I32, P, I64,
+                                           I64, I32, P, I64, P, P, P]
+        L.cospec_latent_keep.restype = I32
+        L.cospec_latent_keep.argtypes = [LP, P, P, I32, I32, P]
+        L.cospec_latent_attention_workspace_size.restype = SZ
+        L.cospec_latent_attention_workspace_size.argtypes = [LP, I32, I32, I32]
+        L.cospec_latent_attention.restype = I32
+        L.cospec_latent_attention.argtypes = [P, LP, P, P, I32, I32, I32, I32, F32, P, P, SZ, P]
+        L.cospec_latent_tree_attention.restype = I32
+        L.cospec_latent_tree_attention.argtypes = [P, LP, P, P, I32, I32, I32, F32, P, P, SZ, P]
+        L.cospec_expanded_attention.restype = I32
+        L.cospec_expanded_attention.argtypes = [P, P, I64, I64, P, I64, I64, P, I64, P, P, I32, I32, I32, I32, I32, I32,
+                                                F32, P, P]
+        OP = ctypes.POINTER(_Pool)
+        L.cospec_pages_fork.restype = I32
+        L.cospec_pages_fork.argtypes = [OP, P, I32, P, P, I32, I32, P, P]
+        L.cospec_pages_reserve_workspace_size.restype = SZ
+        L.cospec_pages_reserve_workspace_size.argtypes = [OP, I32, I32]
+        L.cospec_pages_reserve.restype = I32
+        L.cospec_pages_reserve.argtypes = [OP, P, I32, P, P, I32, I32, P, P, P, SZ, P]
+        L.cospec_pages_release.restype = I32
+        L.cospec_pages_release.argtypes = [OP, P, I32, P, I32, P]
+        L.cospec_pages_compact_workspace_size.restype = SZ
+        L.cospec_pages_compact_workspace_size.argtypes = [OP]
+        L.cospec_pages_compact.restype = I32
+        L.cospec_pages_compact.argtypes = [OP, P, I32, I32, P, P, P, SZ, P]
+        L.cospec_pages_copy.restype = I32
+        L.cospec_pages_copy.argtypes = [ctypes.POINTER(_Plane), I32, I64, P, I32, P, P]
         _lib = L
     return _lib
 
@@ -678,6 +727,9 @@ class PagedCache:
             scales = [torch.empty((n_pages, heads), dtype=torch.float32, device=device) for _ in range(2)]
         return cls(k, v, *scales)
 
+    def _planes(self):
+        return [self.k, self.v] + ([] if self.k_scale is None else [self.k_scale, self.v_scale])
+
     def _struct(self, table: torch.Tensor, B: int) -> _Cache:
         if table.dim() != 2 or table.shape[0] != B or table.dtype != torch.int32 or not table.is_contiguous():
             raise ValueError("table must be contiguous int32 [B, pages of a sequence]")
@@ -859,3 +911,410 @@ def tree_attention(q, cache: PagedCache, table, ctx_len, parent, scale: float) -
     p = prepare_tree_attention(q, cache, table, ctx_len, parent, scale)
     p.launch()
     return p.outputs["out"]
+
+
+# ------------------------------------------------------------------ latent vectors
+
+_ROT = 64       # components of a latent cache's rotated keys
+
+
+class LatentCache:
+    """Pages of latent vectors of one attention layer (cospec_latent_cache): c [n_pages, page, d_c], bf16 or
+    float8_e4m3fn with f32 scales [n_pages, page] (one a position), and r [n_pages, page, 64] bf16, the rotated
+    keys.  page is 16, 32, 64 or 128, d_c 256 or 512."""
+
+    def __init__(self, c, r, scale: Optional[torch.Tensor] = None):
+        if c.dim() != 3:
+            raise ValueError("c must be [n_pages, page, d_c]")
+        n, page, d_c = c.shape
+        if tuple(r.shape) != (n, page, _ROT) or r.dtype != torch.bfloat16:
+            raise ValueError(f"r must be bf16 [n_pages, page, {_ROT}]")
+        if c.dtype == torch.float8_e4m3fn:
+            self.dtype = _F8E4M3
+            if scale is None or tuple(scale.shape) != (n, page) or scale.dtype != torch.float32:
+                raise ValueError("float8_e4m3fn latents need float32 scales [n_pages, page]")
+        elif c.dtype == torch.bfloat16:
+            self.dtype = _BF16
+            if scale is not None:
+                raise ValueError("bf16 latents have no scales")
+        else:
+            raise TypeError(f"latents are bf16 or float8_e4m3fn, got {c.dtype}")
+        for t in (c, r, scale):
+            if t is not None and (not t.is_cuda or not t.is_contiguous() or t.device != c.device):
+                raise ValueError("latents, rotated keys and scales must be contiguous tensors of one device")
+        self.c, self.r, self.scale = c, r, scale
+        self.n_pages, self.page, self.d_c = int(n), int(page), int(d_c)
+
+    @classmethod
+    def empty(cls, n_pages: int, d_c: int, page: int = 64, dtype: torch.dtype = torch.bfloat16,
+              device="cuda") -> "LatentCache":
+        """A cache with nothing in it (its memory is not cleared: every place is written before
+        it is read)."""
+        c = torch.empty((n_pages, page, d_c), dtype=dtype, device=device)
+        r = torch.empty((n_pages, page, _ROT), dtype=torch.bfloat16, device=device)
+        scale = torch.empty((n_pages, page), dtype=torch.float32, device=device) if dtype == torch.float8_e4m3fn else None
+        return cls(c, r, scale)
+
+    def _struct(self, table: torch.Tensor, B: int) -> _LatentCache:
+        if table.dim() != 2 or table.shape[0] != B or table.dtype != torch.int32 or not table.is_contiguous():
+            raise ValueError("table must be contiguous int32 [B, pages of a sequence]")
+        _same_device(self.c, table)
+        return _LatentCache(self.dtype, self.page, self.d_c, self.n_pages, _ptr(self.c), _ptr(self.r),
+                            _ptr(self.scale), _ptr(table), int(table.shape[1]))
+
+    def _planes(self):
+        return [self.c, self.r] + ([] if self.scale is None else [self.scale])
+
+
+def _token_stride(t: torch.Tensor, what: str) -> int:
+    """Distance in elements between the tokens of t [B, n, ...], evenly spaced."""
+    B, n = t.shape[0], t.shape[1]
+    if B * n <= 1:
+        return -1                                           # one token, or none: no distance
+    ld = t.stride(1) if n > 1 else t.stride(0)
+    if B > 1 and n > 1 and t.stride(0) != n * ld:
+        raise ValueError(f"the tokens of {what} must be evenly spaced: stride(0) == n * stride(1)")
+    return int(ld)
+
+
+def _token_rows(t: torch.Tensor, B: int, n: int, d: int, what: str) -> int:
+    """Distance in elements between tokens of a [B, n, d] bf16 tensor."""
+    if tuple(t.shape) != (B, n, d) or t.dtype != torch.bfloat16 or not t.is_cuda or t.stride(2) != 1:
+        raise ValueError(f"{what} must be a bf16 device tensor [B, n, {d}] with unit element stride")
+    ld = _token_stride(t, what)
+    return d if ld < 0 else ld
+
+
+def _head_rows(t: torch.Tensor, B: int, n: int, d: int, what: str):
+    """Distances in elements between tokens, and between heads, of a [B, n, heads, d] bf16 tensor."""
+    if t.dim() != 4 or tuple(t.shape[:2]) != (B, n) or t.shape[3] != d or t.dtype != torch.bfloat16 or not t.is_cuda \
+            or t.stride(3) != 1:
+        raise ValueError(f"{what} must be a bf16 device tensor [B, n, heads, {d}] with unit element stride")
+    head = int(t.stride(2)) if t.shape[2] > 1 else d
+    ld = _token_stride(t, what)
+    return (head * int(t.shape[2]) if ld < 0 else ld), head
+
+
+def prepare_latent_append(cache: LatentCache, table, start, c, k_r, weight: Optional[torch.Tensor] = None,
+                          eps: float = 1e-6, count: Optional[torch.Tensor] = None,
+                          inv_freq: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                          interleaved: bool = False, q: Optional[torch.Tensor] = None,
+                          q_out: Optional[torch.Tensor] = None, dense: bool = False) -> CacheCall:
+    """Pre-marshalled cospec_latent_append: tokens c [B, n, d_c] (bf16; normalised and taken times weight
+    [d_c] unless that is None) and k_r [B, n, 64] go to positions start[b] .. start[b] + count[b] - 1 (int32
+    [B]; count None: n), k_r rotated with inv_freq (f32 [rot / 2]; None: not rotated) to positions (int32
+    [B, n]; None: where they go).  q [B, n, Hq, 64]: queries' rotated part, into outputs["q"]: q_out
+    [B, n, Hq, 64] (such as the last components of the attention's queries), or a new tensor.  dense: outputs["c"]
+    [B, n, d_c] and outputs["k_r"] [B, n, 64] hold the same latents and keys side by side, bf16."""
+    if c.dim() != 3:
+        raise ValueError("c must be [B, n, d_c]")
+    B, n = int(c.shape[0]), int(c.shape[1])
+    ld_c, ld_r = _token_rows(c, B, n, cache.d_c, "c"), _token_rows(k_r, B, n, _ROT, "k_r")
+    cs = cache._struct(table, B)
+    start = _i32_kept(start, B, "start")
+    if count is not None:
+        count = _i32_kept(count, B, "count")
+    if positions is not None and (tuple(positions.shape) != (B, n) or positions.dtype != torch.int32
+                                  or not positions.is_contiguous()):
+        raise ValueError("positions must be contiguous int32 [B, n]")
+    if weight is not None and (tuple(weight.shape) != (cache.d_c,) or weight.dtype != torch.bfloat16
+                               or not weight.is_contiguous()):
+        raise ValueError("weight must be contiguous bf16 [d_c]")
+    rope = None
+    if inv_freq is not None:
+        if inv_freq.dim() != 1 or inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be contiguous float32 [rot / 2]")
+        rope = _Rope(2 * int(inv_freq.shape[0]), int(bool(interleaved)), _ptr(inv_freq))
+    ld_q = head_q = Hq = head_out = 0
+    outputs = {}
+    if q is not None:
+        Hq = int(q.shape[2]) if q.dim() == 4 else 0
+        ld_q, head_q = _head_rows(q, B, n, _ROT, "q")
+        if q_out is None:
+            q_out = torch.empty((B, n, Hq, _ROT), dtype=torch.bfloat16, device=c.device)
+        if tuple(q_out.shape) != (B, n, Hq, _ROT):
+            raise ValueError("q_out must have q's shape")
+        ld_out, head_out = _head_rows(q_out, B, n, _ROT, "q_out")
+        if B * n > 1 and ld_out != Hq * head_out:
+            raise ValueError("q_out's tokens must lie one after the other")
+        outputs["q"] = q_out
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if dense:
+        outputs["c"] = torch.empty((B, n, cache.d_c), dtype=torch.bfloat16, device=c.device)
+        outputs["k_r"] = torch.empty((B, n, _ROT), dtype=torch.bfloat16, device=c.device)
+    _same_device(cache.c, c, k_r, weight, start, count, positions, inv_freq, q, q_out)
+    args = (ctypes.byref(cs), _ptr(start), _ptr(count), _ptr(c), ld_c, _ptr(k_r), ld_r, _ptr(weight), float(eps),
+            None if rope is None else ctypes.byref(rope), _ptr(positions), B, n, _ptr(q), ld_q, head_q, Hq, _ptr(q_out),
+            head_out, _ptr(outputs.get("c")), _ptr(outputs.get("k_r")))
+    return CacheCall(lib().cospec_latent_append, args, outputs, cache.c.device,
+                     [cache, table, start, count, c, k_r, weight, inv_freq, positions, q, q_out, cs, rope])
+
+
+def latent_append(cache: LatentCache, table, start, c, k_r, weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  count: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None,
+                  positions: Optional[torch.Tensor] = None, interleaved: bool = False,
+                  q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, dense: bool = False) -> dict:
+    """cospec_latent_append (see prepare_latent_append); returns its outputs: "q", "c" and "k_r", as far as they
+    were asked for."""
+    p = prepare_latent_append(cache, table, start, c, k_r, weight, eps, count, inv_freq, positions, interleaved, q, q_out,
+                              dense)
+    p.launch()
+    return p.outputs
+
+
+def prepare_latent_keep(cache: LatentCache, table, ctx_len, path) -> CacheCall:
+    """Pre-marshalled cospec_latent_keep: the nodes path [B, N] (int32, as verify_tree returns
+    it) of each tree at positions ctx_len[b] .. move to its front."""
+    if path.dim() != 2 or path.dtype != torch.int32 or not path.is_contiguous():
+        raise ValueError("path must be contiguous int32 [B, N]")
+    B, N = int(path.shape[0]), int(path.shape[1])
+    cs = cache._struct(table, B)
+    ctx = _i32_kept(ctx_len, B, "ctx_len")
+    _same_device(cache.c, ctx, path)
+    return CacheCall(lib().cospec_latent_keep, (ctypes.byref(cs), _ptr(ctx), _ptr(path), B, N), {}, cache.c.device,
+                     [cache, table, ctx, path, cs])
+
+
+def latent_keep(cache: LatentCache, table, ctx_len, path) -> None:
+    """cospec_latent_keep (see prepare_latent_keep)."""
+    prepare_latent_keep(cache, table, ctx_len, path).launch()
+
+
+def _latent_call(fn, q, cache, table, ctx_len, more, K, scale) -> CacheCall:
+    if q.dim() != 4 or q.shape[3] != cache.d_c + _ROT or q.dtype != torch.bfloat16 or not q.is_contiguous():
+        raise ValueError(f"q must be contiguous bf16 [B, n, Hq, {cache.d_c + _ROT}]")
+    B, n, Hq = int(q.shape[0]), int(q.shape[1]), int(q.shape[2])
+    cs = cache._struct(table, B)
+    ctx = _i32_kept(ctx_len, B, "ctx_len")
+    _same_device(cache.c, q, ctx, more)
+    out = torch.empty((B, n, Hq, cache.d_c), dtype=torch.bfloat16, device=q.device)
+    ws_bytes = lib().cospec_latent_attention_workspace_size(ctypes.byref(cs), B, n, Hq)
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device) if ws_bytes else None
+    args = (_ptr(q), ctypes.byref(cs), _ptr(ctx), _ptr(more), B, n, Hq) + K + (float(scale), _ptr(out))
+    return CacheCall(fn, args, dict(out=out), q.device, [q, cache, table, ctx, more, cs], ws, ws_bytes)
+
+
+def prepare_latent_attention(q, cache: LatentCache, table, ctx_len, q_start, K: int, scale: float) -> CacheCall:
+    """Pre-marshalled cospec_latent_attention: q [B, n_q, Hq, d_c + 64] (bf16, contiguous) at positions
+    q_start[b] .. q_start[b] + n_q - 1 against the latents, under the arbitrator's hybrid mask;
+    outputs["out"] is [B, n_q, Hq, d_c] bf16."""
+    return _latent_call(lib().cospec_latent_attention, q, cache, table, ctx_len,
+                        _i32_kept(q_start, int(q.shape[0]), "q_start"), (int(K),), scale)
+
+
+def latent_attention(q, cache: LatentCache, table, ctx_len, q_start, K: int, scale: float) -> torch.Tensor:
+    """cospec_latent_attention (see prepare_latent_attention) -> [B, n_q, Hq, d_c] bf16."""
+    p = prepare_latent_attention(q, cache, table, ctx_len, q_start, K, scale)
+    p.launch()
+    return p.outputs["out"]
+
+
+def prepare_latent_tree_attention(q, cache: LatentCache, table, ctx_len, parent, scale: float) -> CacheCall:
+    """Pre-marshalled cospec_latent_tree_attention: q [B, N, Hq, d_c + 64] (bf16, contiguous) of the nodes kept
+    at positions ctx_len[b] .. ctx_len[b] + N - 1, parent [B, N] as verify_tree takes it;
+    outputs["out"] is [B, N, Hq, d_c] bf16."""
+    if tuple(parent.shape) != tuple(q.shape[:2]) or parent.dtype != torch.int32 or not parent.is_contiguous():
+        raise ValueError("parent must be contiguous int32 [B, N]")
+    return _latent_call(lib().cospec_latent_tree_attention, q, cache, table, ctx_len, parent, (), scale)
+
+
+def latent_tree_attention(q, cache: LatentCache, table, ctx_len, parent, scale: float) -> torch.Tensor:
+    """cospec_latent_tree_attention (see prepare_latent_tree_attention) -> [B, N, Hq, d_c] bf16."""
+    p = prepare_latent_tree_attention(q, cache, table, ctx_len, parent, scale)
+    p.launch()
+    return p.outputs["out"]
+
+
+def prepare_expanded_attention(q, k, v, k_r, ctx_len, q_start, K: int, scale: float) -> CacheCall:
+    """Pre-marshalled cospec_expanded_attention: q [B, n_q, H, d + 64] (bf16, contiguous), k and v [B, L, H, d]
+    (bf16; halves of one projection's heads will do) and the heads' shared rotated key k_r [B, L, 64], under the
+    arbitrator's hybrid mask; outputs["out"] is [B, n_q, H, d] bf16."""
+    if k.dim() != 4 or q.dim() != 4 or q.dtype != torch.bfloat16 or not q.is_contiguous() or not q.is_cuda:
+        raise ValueError("q must be contiguous bf16 [B, n_q, H, d + 64] on the device, k [B, L, H, d]")
+    B, n, H, L, d = int(q.shape[0]), int(q.shape[1]), int(q.shape[2]), int(k.shape[1]), int(k.shape[3])
+    if q.shape[3] != d + _ROT or k.shape[2] != H or tuple(v.shape) != tuple(k.shape):
+        raise ValueError("q must be [B, n_q, H, d + 64], k and v [B, L, H, d]")
+    ld_k, head_k = _head_rows(k, B, L, d, "k")
+    ld_v, head_v = _head_rows(v, B, L, d, "v")
+    ld_r = _token_rows(k_r, B, L, _ROT, "k_r")
+    ctx, qs = _i32_kept(ctx_len, B, "ctx_len"), _i32_kept(q_start, B, "q_start")
+    _same_device(q, k, v, k_r, ctx, qs)
+    out = torch.empty((B, n, H, d), dtype=torch.bfloat16, device=q.device)
+    args = (_ptr(q), _ptr(k), ld_k, head_k, _ptr(v), ld_v, head_v, _ptr(k_r), ld_r, _ptr(ctx), _ptr(qs), B, n, L, H, d,
+            int(K), float(scale), _ptr(out))
+    return CacheCall(lib().cospec_expanded_attention, args, dict(out=out), q.device, [q, k, v, k_r, ctx, qs])
+
+
+def expanded_attention(q, k, v, k_r, ctx_len, q_start, K: int, scale: float) -> torch.Tensor:
+    """cospec_expanded_attention (see prepare_expanded_attention) -> [B, n_q, H, d] bf16."""
+    p = prepare_expanded_attention(q, k, v, k_r, ctx_len, q_start, K, scale)
+    p.launch()
+    return p.outputs["out"]
+
+
+# ------------------------------------------------------------------ the pages under the caches
+
+class PagePool:
+    """Which pages of the caches of a model's layers are in use (cospec_page_pool): refs [n_pages] int32 counts for
+    each page the table entries that name it, 0: free.  One table serves all layers."""
+
+    def __init__(self, refs: torch.Tensor, page: int):
+        if refs.dim() != 1 or refs.dtype != torch.int32 or not refs.is_cuda or not refs.is_contiguous():
+            raise ValueError("refs must be a contiguous int32 device tensor [n_pages]")
+        self.refs, self.n_pages, self.page = refs, int(refs.shape[0]), int(page)
+        self._struct = _Pool(_ptr(refs), self.n_pages, self.page)
+
+    @classmethod
+    def empty(cls, n_pages: int, page: int = 64, device="cuda") -> "PagePool":
+        """A pool of free pages."""
+        return cls(torch.zeros(n_pages, dtype=torch.int32, device=device), page)
+
+    def _table(self, table: torch.Tensor, rows: Optional[int] = None):
+        if table.dim() != 2 or table.dtype != torch.int32 or not table.is_contiguous() \
+                or (rows is not None and table.shape[0] != rows):
+            raise ValueError("table must be contiguous int32 [rows, pages of a sequence]")
+        _same_device(self.refs, table)
+        return int(table.shape[0]), int(table.shape[1])
+
+
+class PoolCall(CacheCall):
+    """Calls on a pool's pages, launched one after the other as one CacheCall."""
+
+    def __init__(self, fn, args, outputs, device, keep, workspace=None, ws_bytes=None, then=None):
+        super().__init__(fn, args, outputs, device, keep, workspace, ws_bytes)
+        self._then = then
+
+    def launch(self):
+        super().launch()
+        if self._then is not None:
+            fn, args = self._then
+            code = fn(*args, _stream())
+            if code:
+                _check(code, fn.__name__)
+
+
+def _planes_of(pool_pages: int, page: int, caches, device):
+    """The planes of the caches' pages, as the library takes them, and how many."""
+    tensors = []
+    for cache in caches:
+        if cache.n_pages != pool_pages or cache.page != page:
+            raise ValueError("every cache must have the pool's pages")
+        tensors += cache._planes()
+    for t in tensors:
+        if t.device != device:
+            raise ValueError("every tensor of a call must be on one device")
+    planes = (_Plane * max(len(tensors), 1))()
+    for p, t in zip(planes, tensors):
+        p.data, p.page_bytes = t.data_ptr(), t[0].numel() * t.element_size()
+    return planes, len(tensors)
+
+
+def _copy_args(pool: PagePool, caches, pairs, count):
+    planes, n = _planes_of(pool.n_pages, pool.page, caches, pool.refs.device)
+    return (planes, n, pool.n_pages, _ptr(pairs), int(pairs.shape[0]), _ptr(count))
+
+
+def prepare_pages_copy(pool: PagePool, caches, pairs, count: Optional[torch.Tensor] = None) -> CacheCall:
+    """Pre-marshalled cospec_pages_copy: pages pairs[i, 0] -> pairs[i, 1] (int32 [n, 2]; the first count[0] of
+    them if count, int32 [1], is given) in all of the caches."""
+    if pairs.dim() != 2 or pairs.shape[1] != 2 or pairs.dtype != torch.int32 or not pairs.is_contiguous():
+        raise ValueError("pairs must be contiguous int32 [n, 2]")
+    if count is not None:
+        count = _i32_kept(count, 1, "count")
+    caches = list(caches)
+    _same_device(pool.refs, pairs, count)
+    args = _copy_args(pool, caches, pairs, count)
+    return CacheCall(lib().cospec_pages_copy, args, {}, pool.refs.device, [pool, caches, pairs, count])
+
+
+def pages_copy(pool: PagePool, caches, pairs, count: Optional[torch.Tensor] = None) -> None:
+    """cospec_pages_copy (see prepare_pages_copy)."""
+    prepare_pages_copy(pool, caches, pairs, count).launch()
+
+
+def prepare_pages_fork(pool: PagePool, table, row, length) -> CacheCall:
+    """Pre-marshalled cospec_pages_fork: outputs["table"] [B, pages] shares the pages of the first length[b]
+    positions of row row[b] of table (int32 [B] both)."""
+    rows, T = pool._table(table)
+    B = int(row.shape[0])
+    row, length = _i32_kept(row, B, "row"), _i32_kept(length, B, "length")
+    _same_device(pool.refs, row, length)
+    out = torch.empty((B, T), dtype=torch.int32, device=table.device)
+    args = (ctypes.byref(pool._struct), _ptr(table), rows, _ptr(row), _ptr(length), B, T, _ptr(out))
+    return CacheCall(lib().cospec_pages_fork, args, dict(table=out), pool.refs.device, [pool, table, row, length])
+
+
+def pages_fork(pool: PagePool, table, row, length) -> torch.Tensor:
+    """cospec_pages_fork (see prepare_pages_fork); returns the new table."""
+    p = prepare_pages_fork(pool, table, row, length)
+    p.launch()
+    return p.outputs["table"]
+
+
+def prepare_pages_reserve(pool: PagePool, table, start, n: int, count: Optional[torch.Tensor] = None,
+                          caches=()) -> PoolCall:
+    """Pre-marshalled cospec_pages_reserve: positions start[b] .. start[b] + count[b] - 1 (int32 [B]; count
+    None: n) get pages of their sequence's own in table, and the caches' pages are copied where a sequence leaves a
+    page that others share inside it.  outputs: copies [B, 2], lacking [1] (0: done; else nothing was)."""
+    B, T = pool._table(table)
+    start = _i32_kept(start, B, "start")
+    if count is not None:
+        count = _i32_kept(count, B, "count")
+    _same_device(pool.refs, start, count)
+    caches = list(caches)
+    dev = pool.refs.device
+    copies = torch.empty((B, 2), dtype=torch.int32, device=dev)
+    lacking = torch.empty(1, dtype=torch.int32, device=dev)
+    L = lib()
+    ws_bytes = L.cospec_pages_reserve_workspace_size(ctypes.byref(pool._struct), B, int(n))
+    ws = torch.empty(max(ws_bytes, 256), dtype=torch.uint8, device=dev)
+    args = (ctypes.byref(pool._struct), _ptr(table), T, _ptr(start), _ptr(count), B, int(n), _ptr(copies), _ptr(lacking))
+    then = (L.cospec_pages_copy, _copy_args(pool, caches, copies, None)) if caches else None
+    return PoolCall(L.cospec_pages_reserve, args, dict(copies=copies, lacking=lacking), dev,
+                    [pool, table, start, count, caches], ws, ws.numel(), then)
+
+
+def pages_reserve(pool: PagePool, table, start, n: int, count: Optional[torch.Tensor] = None, caches=()) -> dict:
+    """cospec_pages_reserve and, for the caches, cospec_pages_copy (see prepare_pages_reserve)."""
+    p = prepare_pages_reserve(pool, table, start, n, count, caches)
+    p.launch()
+    return p.outputs
+
+
+def prepare_pages_release(pool: PagePool, table, keep) -> CacheCall:
+    """Pre-marshalled cospec_pages_release: gives back the pages behind each row's first keep[b] positions."""
+    B, T = pool._table(table)
+    keep = _i32_kept(keep, B, "keep")
+    _same_device(pool.refs, keep)
+    args = (ctypes.byref(pool._struct), _ptr(table), T, _ptr(keep), B)
+    return CacheCall(lib().cospec_pages_release, args, {}, pool.refs.device, [pool, table, keep])
+
+
+def pages_release(pool: PagePool, table, keep) -> None:
+    """cospec_pages_release (see prepare_pages_release)."""
+    prepare_pages_release(pool, table, keep).launch()
+
+
+def prepare_pages_compact(pool: PagePool, table, caches=()) -> PoolCall:
+    """Pre-marshalled cospec_pages_compact: the pages in use move to the pool's front, in table (which must hold
+    every entry that names one) and in the caches.  outputs: moves [n_pages // 2, 2] and n_moves [1]."""
+    B, T = pool._table(table)
+    caches = list(caches)
+    dev = pool.refs.device
+    moves = torch.empty((max(pool.n_pages // 2, 1), 2), dtype=torch.int32, device=dev)
+    n_moves = torch.empty(1, dtype=torch.int32, device=dev)
+    L = lib()
+    ws_bytes = L.cospec_pages_compact_workspace_size(ctypes.byref(pool._struct))
+    ws = torch.empty(max(ws_bytes, 256), dtype=torch.uint8, device=dev)
+    args = (ctypes.byref(pool._struct), _ptr(table), T, B, _ptr(moves), _ptr(n_moves))
+    then = (L.cospec_pages_copy, _copy_args(pool, caches, moves, n_moves)) if caches else None
+    return PoolCall(L.cospec_pages_compact, args, dict(moves=moves, n_moves=n_moves), dev, [pool, table, caches], ws,
+                    ws.numel(), then)
+
+
+def pages_compact(pool: PagePool, table, caches=()) -> dict:
+    """cospec_pages_compact and, for the caches, cospec_pages_copy (see prepare_pages_compact)."""
+    p = prepare_pages_compact(pool, table, caches)
+    p.launch()
+    return p.outputs

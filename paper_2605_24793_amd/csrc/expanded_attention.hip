@@ -1,0 +1,261 @@
+// The latent cache's attention in the expanded form: every head has keys and values of its own beside
+// the rotated key that all heads share, for whole inputs, not paged.
+//
+// One pass over the keys with a running maximum, as in paged_attention.hip.  A workgroup takes rows of one
+// head and sequence, 32 a wave, and its waves share the keys, in turns of 64 that are on their way into LDS
+// while the turn before is worked on.
+//
+// S^T = K Q^T and O^T = V^T P^T with 32 x 32 products: a lane holds query l % 32 and the keys 8 (i / 4) +
+// 4 (l / 32) + i % 4 of a tile, whose rounded weights are the second product's operand as they
+// stand; the values are turned while they are read from LDS (ds_read_b64_tr).
+#include <algorithm>
+
+#include "attend.h"
+#include "latent.h"
+
+namespace cospec {
+namespace {
+
+constexpr int kKeys = 64;             // of a turn
+
+// Row `key` of a turn holds its sixteen-byte pieces at place i ^ turned(key): eight rows' same piece, and four
+// rows' two pieces, lie in different banks.
+__device__ inline int turned(int key) { return (key & 3) << 1 | (key >> 2 & 1); }
+
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void k_expanded_attention(ExpandedArgs a) {
+    constexpr int RB = D * 2, DR = kRotated;
+    constexpr int CS = D / 16, RS = DR / 16, DT = D / 32, KT = kKeys / 32;
+    constexpr int kRotAt = kKeys * RB, kValuesAt = kRotAt + kKeys * DR * 2, kStage = kValuesAt + kKeys * RB;
+    constexpr int PPR = RB / 16;                            // pieces of a row
+    constexpr int ROWS = 32 * NW;
+    __shared__ __attribute__((aligned(128))) char s_ring[2 * kStage];
+    __shared__ uint32_t s_bad[2];                           // keys whose values are not finite
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int gh = lane >> 5, l32 = lane & 31;
+    // the row blocks of a head follow each other on one XCD, whose L2 then serves all but the first; the last
+    // rows, which see the most keys, come first
+    const uint32_t slot = blockIdx.x / kXcds, round = quot(a.by_blocks, slot);
+    const int block = a.by_blocks.d - 1 - (slot - round * a.by_blocks.d);
+    const uint32_t bh = round * kXcds + blockIdx.x % kXcds;
+    const int b = quot(a.by_heads, bh), h = static_cast<int>(bh - b * a.by_heads.d);
+    if (b >= a.B) return;
+    const int q0 = block * ROWS, q1 = min(q0 + ROWS, a.n_q);
+    const int qi = q0 + wave * 32 + l32;
+    const bool valid = qi < q1;
+    const int64_t R = (static_cast<int64_t>(b) * a.n_q + min(qi, q1 - 1)) * a.H + h;
+    const char *qrow = a.q + R * ((D + DR) * 2);
+    u32x4 qf[CS + RS];
+#pragma unroll
+    for (int c = 0; c < CS + RS; ++c) qf[c] = *reinterpret_cast<const u32x4 *>(qrow + (c * 16 + gh * 8) * 2);
+    const int64_t lc0 = max(scalar_load(a.ctx_len + b), 0);
+    const int end = static_cast<int>(min(lc0 + 2 * static_cast<int64_t>(a.K) + 3, static_cast<int64_t>(a.L)));
+    const int lc = static_cast<int>(min(lc0, static_cast<int64_t>(end)));
+    const int64_t qs = scalar_load(a.q_start + b);
+    // keys [0, kend) that some row sees, [0, all_see) that every row sees that sees any
+    const int64_t p_lo = qs + q0, p_hi = qs + q1 - 1;
+    int kend = p_lo >= end ? 0 : p_hi < lc ? max(static_cast<int>(p_hi) + 1, 0) : end;
+    const int64_t p_first = max(p_lo, static_cast<int64_t>(0));
+    const int all_see = p_first >= lc ? kend : min(static_cast<int>(p_first) + 1, kend);
+
+    const int64_t p_q = qs + qi;
+    const bool live = valid && p_q >= 0 && p_q < end;
+    const int vis = !live ? 0 : p_q >= lc ? end : static_cast<int>(p_q) + 1;
+    int most = vis;                                         // of the wave's rows
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) most = max(most, __shfl_xor(most, off));
+    most = uniform(most);
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int c = 0; c < CS + RS; ++c)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) qf[c][x] = live ? qf[c][x] ^ flip : 0u;
+    const float sc = fmaxf(fabsf(a.scale) * kLog2eP, 1.17549435e-38f);
+
+    const uint32_t ring = uniform(lds_address(s_ring));
+    const char *const kb = a.k + (static_cast<int64_t>(b) * a.L * a.ld_k + h * a.head_k) * 2;
+    const char *const vb = a.v + (static_cast<int64_t>(b) * a.L * a.ld_v + h * a.head_v) * 2;
+    const char *const rb = a.k_r + static_cast<int64_t>(b) * a.L * a.ld_r * 2;
+    // a turn's keys, values and rotated keys; keys past the last one are read as the last one
+    auto load = [&](int k0, uint32_t stage) {
+        constexpr int NI = kKeys * RB / 1024, NR = kKeys * DR * 2 / 1024;   // loads of the keys, and of the rotated ones
+#pragma unroll
+        for (int i = 0; i < NI / NW; ++i) {
+            const int e = wave * (NI / NW) + i, row = e * (1024 / RB) + lane / PPR;
+            const int piece = (lane % PPR) ^ turned(row);
+            const int64_t key = min(k0 + row, kend - 1);
+            load_lds16<false>(kb + key * a.ld_k * 2 + piece * 16, stage + e * 1024);
+            load_lds16<false>(vb + key * a.ld_v * 2 + piece * 16, stage + kValuesAt + e * 1024);
+        }
+        if (NR >= NW || wave < NR) {
+#pragma unroll
+            for (int i = 0; i < (NR + NW - 1) / NW; ++i) {
+                const int e = wave * ((NR + NW - 1) / NW) + i, row = e * 8 + lane / 8;
+                const int64_t key = min(k0 + row, kend - 1);
+                load_lds16<false>(rb + key * a.ld_r * 2 + ((lane % 8) ^ (row & 7)) * 16, stage + kRotAt + e * 1024);
+            }
+        }
+    };
+
+    floatx16 o[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+    float m = -INFINITY, l = 0.f;                           // l: of this lane's keys alone
+    const uint32_t k_at = l32 * RB + ((gh ^ turned(l32)) & 7) * 16;
+    const uint32_t r_at = kRotAt + l32 * (DR * 2) + ((gh ^ l32) & 7) * 16;
+    const int vj = lane & 15, vrow = 4 * gh + (vj >> 2);
+    const uint32_t v_at = kValuesAt + vrow * RB + (((2 * (lane >> 4 & 1) + (vj >> 1 & 1)) ^ turned(vrow)) & 7) * 16 + (vj & 1) * 8;
+
+    if (kend > 0) load(0, ring);
+    for (int k0 = 0, buf = 0; k0 < kend; k0 += kKeys, buf ^= 1) {
+        wait_vm<0>();                                       // this wave's part of the turn
+        lds_barrier();                                      // ... and the others'; the turn before is used up
+        if (k0 + kKeys < kend) load(k0 + kKeys, ring + (buf ^ 1) * kStage);
+        char *const stage = s_ring + buf * kStage;
+        const bool masked = k0 + kKeys > all_see;           // the same in the whole workgroup
+        if (masked) {
+            // values that are not finite become zeros (a weight of zero would not keep them from the rows that
+            // do not see them), and their keys are marked
+            if (tid < 2) s_bad[tid] = 0;
+            lds_barrier();
+            constexpr int PT = NW;                          // threads of a key
+            const int key = tid / PT;
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < (PPR + PT - 1) / PT; ++i) {
+                const int piece = tid % PT + PT * i;
+                u32x4 *at = reinterpret_cast<u32x4 *>(stage + kValuesAt + key * RB + piece * 16);
+                u32x4 x = *at;
+                uint32_t any = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t t = not_finite<false>(x[e], 0u);
+                    any |= t;
+                    x[e] &= ~(t | (t - (t >> 15)));
+                }
+                if (any) *at = x;
+                top |= any;
+            }
+            if (top) atomicOr(&s_bad[key >> 5], 1u << (key & 31));
+            lds_barrier();
+        }
+        if (k0 < most) {
+            floatx16 st[KT];
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) st[t][i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < CS; ++c)
+#pragma unroll
+                for (int t = 0; t < KT; ++t)
+                    st[t] = mfma32(*reinterpret_cast<const u32x4 *>(stage + t * (32 * RB) + (k_at ^ (c % 4 * 32)) + c / 4 * 128), qf[c], st[t]);
+#pragma unroll
+            for (int c = 0; c < RS; ++c)
+#pragma unroll
+                for (int t = 0; t < KT; ++t)
+                    st[t] = mfma32(*reinterpret_cast<const u32x4 *>(stage + t * (32 * DR * 2) + (r_at ^ (c * 32))), qf[CS + c], st[t]);
+            if (masked) {
+#pragma unroll
+                for (int t = 0; t < KT; ++t) {
+                    const uint32_t see = low_bits(vis - (k0 + 32 * t)) >> (4 * gh), bad = s_bad[t] >> (4 * gh);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int bit = 8 * (i / 4) + i % 4;
+                        if (!(see >> bit & 1)) st[t][i] = -INFINITY;
+                        else if (bad >> bit & 1) st[t][i] = NAN;
+                    }
+                }
+            }
+            float bm = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) bm = fmaxf(bm, st[t][i]);
+            {
+                const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
+                bm = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * sc;
+            }
+            const bool raise = bm > m + kLazyRescale;       // always when m is still -inf
+            if (__builtin_expect(__ballot(raise) != 0, 0)) {
+                const float alpha = raise ? __builtin_amdgcn_exp2f(m - bm) : 1.f;   // 0 from -inf
+                if (raise) m = bm;
+                l *= alpha;
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[t][i] *= alpha;
+            }
+            // a query that has seen nothing yet keeps m = -inf and adds nothing
+            const float mm = m == -INFINITY ? INFINITY : m;
+            u32x4 pb[KT][2];
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int v = 0; v < 2; ++v)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int e = 8 * v + 2 * i;
+                        const float p0 = __builtin_amdgcn_exp2f(fmaf(st[t][e], sc, -mm)), p1 = __builtin_amdgcn_exp2f(fmaf(st[t][e + 1], sc, -mm));
+                        l += p0 + p1;
+                        pb[t][v][i] = bf16_pair(p0, p1);
+                    }
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int v = 0; v < 2; ++v)
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        const char *at = stage + (t * 32 + v * 16) * RB + (v_at ^ (dt % 2 * 64)) + dt / 2 * 128;
+                        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at));
+                        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * RB)));
+                        o[dt] = mfma32(u32x4{lo[0], lo[1], hi[0], hi[1]}, pb[t][v], o[dt]);
+                    }
+        }
+    }
+    l += __shfl_xor(l, 32);
+    if (!valid) return;
+    // O^T tile t, elements 4e .. 4e + 3: components 32 t + 8 e + 4 gh + 0..3 of this lane's row
+    if (!live) l = 0.f;                                     // (unmasked turns gave it some weights)
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;   // NaN stays
+    char *dst = a.out + (R * D + 4 * gh) * 2;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            floatx4 x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = l == 0.f ? 0.f : o[t][4 * e + i] * inv;
+            *reinterpret_cast<u32x2 *>(dst + (32 * t + 8 * e) * 2) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+        }
+}
+
+// Waves of a workgroup: rows beyond 128 fill eight.
+int waves_of(int32_t n_q) { return n_q > 128 ? 8 : 4; }
+
+template <int D> void run_expanded(const ExpandedArgs &a, unsigned grid, hipStream_t s) {
+    if (waves_of(a.n_q) == 8) hipLaunchKernelGGL((k_expanded_attention<D, 8>), dim3(grid), dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((k_expanded_attention<D, 4>), dim3(grid), dim3(256), 0, s, a);
+}
+
+int64_t row_blocks(int32_t n_q) { return (static_cast<int64_t>(n_q) + 32 * waves_of(n_q) - 1) / (32 * waves_of(n_q)); }
+
+}  // namespace
+
+int64_t expanded_workgroups(int32_t B, int32_t n_q, int32_t H) {
+    return (static_cast<int64_t>(B) * H + kXcds - 1) / kXcds * kXcds * row_blocks(n_q);
+}
+
+hipError_t launch_expanded_attention(ExpandedArgs a, hipStream_t s) {
+    a.by_blocks = fast_div(static_cast<uint32_t>(row_blocks(a.n_q)));
+    a.by_heads = fast_div(a.H);
+    const unsigned grid = static_cast<unsigned>(expanded_workgroups(a.B, a.n_q, a.H));
+    if (a.d == 128) run_expanded<128>(a, grid, s);
+    else run_expanded<64>(a, grid, s);
+    return hipGetLastError();
+}
+
+}  // namespace cospec

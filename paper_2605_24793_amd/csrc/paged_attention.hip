@@ -32,109 +32,23 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "paged.h"
+#include "attend.h"
 
 namespace cospec {
 namespace {
 
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(4))) float floatx4;
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-
-constexpr int kWaves = 4;             // of a workgroup
-constexpr int kThreads = 64 * kWaves;
-constexpr int kSegment = 252;         // pages looked up at a time: with one more, at most one a thread; whole turns
-constexpr int kStep = 64;             // keys of a wave's turn, at most
 // 16-row tiles of a workgroup, at most: what the registers hold of queries, scores and sums
 constexpr int kMaxRowTiles = 3;
 // Keys of a piece, at least.  One token at 15000 positions: pieces of 256 17.6 us, 512 15.0, 1024 17.0; with many rows
 // (196 of a group at 4687) 25.7, 24.3 and 33.5.
 constexpr int kMinPiece = 512;
 constexpr int kMinPieceWide = 256;
-constexpr int64_t kMaxPieces = 64;    // of a group's keys (the join weighs them in one wave)
-constexpr float kLog2eP = 1.4426950408889634f;
-constexpr float kLazyRescale = 8.0f;  // log2 units a block's max may exceed the running max by
-
-__device__ inline uint32_t bf16_pair(float lo, float hi) {
-    return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(lo), static_cast<__bf16>(hi)});
-}
-
-__device__ inline floatx4 mfma(u32x4 a, u32x4 b, floatx4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
-                                                   0, 0);
-}
-
-// max over the four lanes that share a query column (l % 16)
-__device__ inline float max_rows(float x) {
-    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
-    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
-}
-
-// Eight e4m3 bytes (two words) times a power of two, as four words of two bf16.
-__device__ inline u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
-    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
-}
-
-// A value that is the same in every lane, for the scalar registers.
-__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-// A load through the scalar cache, of what no kernel writes while this one runs.
-typedef __attribute__((address_space(4))) const int const_int;
-__device__ inline int scalar_load(const int32_t *p) { return *(const_int *)reinterpret_cast<uintptr_t>(p); }
-
-// What the queries of sequence b see.  Hybrid: position p < lc sees [0, p], lc <= p < end sees
-// [0, end).  Tree: node r sees [0, lc) and its ancestors among lc .. end - 1.
-struct Seq {
-    int lc, end;
-    int64_t qs;
-};
-
-__device__ inline Seq sequence_of(const PagedArgs &a, int b) {
-    const int64_t room = static_cast<int64_t>(a.c.max_pages) << a.c.log_page;
-    const int64_t lc = max(scalar_load(a.ctx_len + b), 0);
-    const int64_t more = a.parent ? a.n_q : 2 * static_cast<int64_t>(a.K) + 3;
-    const int end = static_cast<int>(min(lc + more, room));
-    return Seq{static_cast<int>(min(lc, static_cast<int64_t>(end))), end, a.parent ? lc : static_cast<int64_t>(scalar_load(a.q_start + b))};
-}
-
-// Keys [0, kend) that the rows [q0, q1) of a group see, and how they are cut.
-struct Cut {
-    int kend, chunk;
-    int pieces;                // at least 1
-};
-
-__device__ inline Cut cut_of(const PagedArgs &a, const Seq &s, int q0, int q1) {
-    const int64_t p_lo = s.qs + quot(a.by_grp, q0), p_hi = s.qs + quot(a.by_grp, q1 - 1);
-    int kend = s.end;
-    if (p_lo >= s.end) kend = 0;                            // all padding: no key
-    else if (!a.parent && p_hi < s.lc) kend = max(static_cast<int>(p_hi) + 1, 0);
-    const Pieces p = pieces_of(kend, quot(a.by_splits, kend + a.splits - 1), kStep, a.min_piece);
-    return Cut{kend, p.chunk, p.count};
-}
-
-// Keys [0, result) of a piece's [.., kend) are seen by every row of [q0, q1) that sees any.
-__device__ inline int seen_by_all(const PagedArgs &a, const Seq &s, int q0, int kend) {
-    if (a.parent) return min(s.lc, kend);
-    const int64_t p = max(s.qs + quot(a.by_grp, q0), static_cast<int64_t>(0));
-    return p >= s.lc ? kend : min(static_cast<int>(p) + 1, kend);
-}
 
 // Values that are not finite, among keys that some rows see and others do not.  A weight of zero would not keep them
 // from the others: they are made zero, and the weights of the rows that do see such a key NaN.
-// not_finite: the highest bit of every such element of four bytes (e4m3: `carry` is 0x01010101, or at the scale 2^120
-// 0x08080808, as more than 240 times that is not finite in bf16); emptied: the four bytes without these elements;
+// (not_finite: e4m3's `carry` is 0x01010101, or at the scale 2^120 0x08080808, as more than 240 times that is not finite
+// in bf16); emptied: the four bytes without these elements;
 // element_bits: one bit per element of not_finite's.
-template <bool F8> __device__ inline uint32_t not_finite(uint32_t x, uint32_t carry) {
-    return F8 ? ((x & 0x7f7f7f7fu) + carry) & 0x80808080u : ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-}
-
 __device__ inline uint32_t carry_of(float scale) { return scale < 1.329227995784916e36f ? 0x01010101u : 0x08080808u; }
 
 template <bool F8> __device__ inline uint32_t emptied(uint32_t x, uint32_t top) {
@@ -148,97 +62,10 @@ template <bool F8> __device__ inline uint32_t element_bits(uint32_t top) {
     return bits;
 }
 
-// The sixteen bits from bit `at` (may be negative) of a set of 256.
-__device__ inline uint32_t window16(const uint32_t *set, int at) {
-    if (at <= -16 || at >= 256) return 0;
-    if (at < 0) return (set[0] << -at) & 0xffffu;
-    const int w = at >> 5;
-    const uint64_t two = set[w] | static_cast<uint64_t>(w < 7 ? set[w + 1] : 0u) << 32;
-    return static_cast<uint32_t>(two >> (at & 31)) & 0xffffu;
-}
-
-// 16 bytes per lane from global memory into LDS at byte lds + 16 * lane, lds the same in every
-// lane.  Written as assembly, so that the compiler, which knows nothing of these loads, places no
-// wait for them before LDS reads; the kernel's own waits order them.  ONCE: read once, not to be kept in
-// the caches.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-template <bool ONCE> __device__ inline void load_lds16(const char *src, uint32_t lds) {
-    if constexpr (ONCE)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" : : "s"(lds), "v"(src) : "memory", "m0");
-    else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(src) : "memory", "m0");
-}
-#pragma clang diagnostic pop
-
-// Waits until at most N vector-memory operations of this wave are outstanding.
-template <int N> __device__ inline void wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
-
-// Waits for this wave's LDS reads.
-__device__ inline void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-
-typedef __attribute__((address_space(3))) const char lds_cchar;
-
-// Workgroup barrier that does not wait for the loads still in flight (as the fence of
-// __syncthreads would); the compiler may not move memory accesses across it.
-__device__ inline void lds_barrier() {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
-// Ancestors of every node, as sets of 256 bits in LDS, by all threads: each round joins the set
-// of the node `up`, twice as far up as the round before.
-__device__ inline void find_ancestors(const PagedArgs &a, int b, uint32_t (*s_anc)[8], int *s_up) {
-    const int tid = threadIdx.x;
-    const int n = a.n_q;
-    int up = -1;
-    if (tid < n) {
-        const int p = a.parent[static_cast<int64_t>(b) * n + tid];
-        up = p >= 0 && p < tid ? p : -1;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) s_anc[tid][w] = w == tid >> 5 ? 1u << (tid & 31) : 0u;
-        s_up[tid] = up;
-    }
-    for (int far = 1; far < n; far *= 2) {
-        __syncthreads();
-        uint32_t set[8];
-        int next_up = -1;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) set[w] = up >= 0 ? s_anc[up][w] : 0u;
-        if (up >= 0) next_up = s_up[up];
-        __syncthreads();
-        if (tid < n) {
-#pragma unroll
-            for (int w = 0; w < 8; ++w) s_anc[tid][w] |= set[w];
-            s_up[tid] = up = next_up;
-        }
-    }
-    __syncthreads();
-}
-
-// Which rows, keys and group a workgroup takes.  Workgroups are dealt to the XCDs round-robin: those
-// that read the same keys (the row blocks of a piece of a group) follow each other on one XCD,
-// whose L2 then serves all but the first; the last rows, which see the most keys, come first.
-struct Place {
-    int b, h, block, piece;
-};
-
-__device__ inline Place place_of(const PagedArgs &a) {
-    const uint32_t slot = blockIdx.x / kXcds;
-    const uint32_t round = quot(a.by_blocks, slot);
-    const int block = a.by_blocks.d - 1 - (slot - round * a.by_blocks.d);
-    const uint32_t unit = round * kXcds + blockIdx.x % kXcds;
-    const uint32_t bh = quot(a.by_splits, unit);
-    const int b = quot(a.by_heads, bh);
-    return Place{b, static_cast<int>(bh - b * a.by_heads.d), block, static_cast<int>(unit - bh * a.by_splits.d)};
-}
-
 // What a workgroup keeps in LDS of each page of its keys, up to kThreads of them at a time, one looked
 // up by each thread: {page * heads + head, with kNone for a page that is none (it is read as page
 // 0, and not used); the upper halves of the scales of keys and of values (e4m3)}.
 typedef uint2 PageEntry;
-constexpr uint32_t kNone = 0x80000000u;
 
 // (2^120 is the largest scale that an append writes; no scale, of a page in use or not, makes a zero anything else)
 __device__ inline uint32_t pack_scales(float k, float v) {
@@ -247,12 +74,6 @@ __device__ inline uint32_t pack_scales(float k, float v) {
 }
 __device__ inline float key_scale(PageEntry e) { return __uint_as_float(e.y & 0xffff0000u); }
 __device__ inline float value_scale(PageEntry e) { return __uint_as_float(e.y << 16); }
-
-// This thread's entry of sequence b's table, from entry `first` on (clamped to the table).
-__device__ inline uint32_t table_entry(const PagedArgs &a, int b, int first) {
-    const int at = min(first + static_cast<int>(threadIdx.x), a.c.max_pages - 1);
-    return a.c.table[static_cast<int64_t>(b) * a.c.max_pages + at];
-}
 
 // RW waves of the four share the keys, each with RT row tiles of its own; the 4 / RW sets of them
 // take turns at the keys.
@@ -698,14 +519,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_paged_attention(PagedArgs a) {
 
 // ---------------------------------------------------------------- many query rows
 
-typedef __attribute__((ext_vector_type(16))) float floatx16;
-
 constexpr int kWideRows = 32 * kWaves;
-
-__device__ inline floatx16 mfma32(u32x4 a, u32x4 b, floatx16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
-                                                   0, 0);
-}
 
 // The same attention where a group has many query rows.  There the vector unit bounds it: every
 // instruction, a matrix one too, takes it for 4 to 5 cycles.  So each wave takes 32 rows with 32 x 32
@@ -1129,7 +943,6 @@ void run_attention(const PagedArgs &a, unsigned grid, hipStream_t s) {
     else hipLaunchKernelGGL((k_paged_attention<D, F8, 1, 1>), g, t, 0, s, a);
 }
 
-constexpr int64_t kCus = 256;         // compute units of an MI355X
 
 }  // namespace
 
