@@ -555,6 +555,8 @@ def run(state):
             out.update(call.outputs)
         if kind == "append":
             out = dict(q=out["q"], dense_c=out["c"], dense_r=out["k_r"])
+        elif kind == "fork":
+            out["short"] = out.pop("lacking")
     elif kind == "append":
         out = _plain_append(s)
     elif kind == "attend":
