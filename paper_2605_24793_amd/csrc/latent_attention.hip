@@ -16,6 +16,7 @@ namespace cospec {
 namespace {
 
 constexpr int kKeys = 64;             // of a turn
+constexpr int kFewRows = 32, kManyRows = 64;   // of a workgroup
 constexpr int kRotBytes = kRotated * 2;
 constexpr int kMinPieceLatent = 256;  // keys of a piece, at least
 constexpr float kFar = 60.f;          // log2 units a score may exceed a row's m by (weights and sums are floats)
@@ -33,14 +34,72 @@ __device__ inline void load_lds4(const char *src, uint32_t lds) {
 // which read four rows (bf16) or eight (e4m3) of sixteen components.
 template <bool F8> __device__ inline int turned(int key) { return F8 ? key & 7 : (key & 3) << 1 | (key >> 2 & 1); }
 
-// A workgroup takes RT * 32 rows of a sequence, or a piece of its keys, in turns of 64 keys; the next turn's
-// latents are on their way into LDS while one is worked on.
-//
-// The four waves share both products out differently.  Scores: RT = 2, 32 rows and 32 keys each; RT = 1, all
-// rows and sixteen keys each.  Sums: all rows and a quarter of the components each, so that a latent is
-// read from LDS once or twice for the scores and once for the sums, and a wave holds the queries of 32
-// rows and a quarter of the sums.  The rounded weights go from one to the other through LDS.  (With sums of its
-// own rows, a wave would hold 256 registers of them beside 144 of queries, and every wave read every latent twice.)
+// A lane's part of row R's sums: tile dt, elements 4e .. 4e + 3 are the components d0 + 32 dt + 8 e + 0..3.  Whole
+// rows are divided by the weights' sum L, pieces stored as they are, with {m, L} by one lane (`first`).
+template <int DC, int DT>
+__device__ inline void store_sums(const PagedArgs &a, const floatx16 (&o)[DT], int64_t R, int d0, int pieces, int piece,
+                                  float m, float L, bool first) {
+    if (pieces == 1) {
+        const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;   // NaN stays
+        char *dst = static_cast<char *>(a.out) + (R * DC + d0) * 2;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                floatx4 x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = L == 0.f ? 0.f : o[dt][4 * e + i] * inv;
+                *reinterpret_cast<u32x2 *>(dst + (32 * dt + 8 * e) * 2) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+            }
+    } else {
+        const int64_t at = piece * (static_cast<int64_t>(a.B) * a.n_q * a.Hq) + R;
+        float *po = a.part_o + at * DC + d0;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *reinterpret_cast<floatx4 *>(po + 32 * dt + 8 * e) =
+                    floatx4{o[dt][4 * e], o[dt][4 * e + 1], o[dt][4 * e + 2], o[dt][4 * e + 3]};
+        if (first) a.part_ml[at] = make_float2(m, L);
+    }
+}
+
+// Makes zeros of a staged turn's latents that hold no key of the sequence (such places may hold anything, and a
+// weight of zero does not make a NaN harmless), and of elements that are not finite, whose keys are marked in `bad`.
+// By all T threads, between barriers.
+template <int RB, int KS, int T, bool F8>
+__device__ inline void clean_turn(char *stage, float *scales, uint32_t *bad, int tid, bool real) {
+    constexpr int PT = T / KS;                              // threads of a key, of one wave
+    const int key = tid / PT, part = tid % PT;
+    uint32_t top = 0;
+#pragma unroll 2
+    for (int i = 0; i < RB / 16 / PT; ++i) {
+        u32x4 *at = reinterpret_cast<u32x4 *>(stage + key * RB + (part + PT * i) * 16);
+        u32x4 x = *at;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t t = not_finite<F8>(x[e], 0x01010101u);
+            top |= t;
+            x[e] = real ? x[e] & ~(t | (t - (t >> (F8 ? 7 : 15)))) : 0u;
+        }
+        *at = x;
+    }
+    bool marked = top != 0;
+    if constexpr (F8) {
+        const float sv = scales[key];
+        const bool wild = !(fabsf(sv) < INFINITY);
+        marked |= wild;
+        wait_lds();
+        if (part == 0 && (wild || !real)) scales[key] = 0.f;
+    }
+    if (real && marked) atomicOr(&bad[key >> 5], 1u << (key & 31));
+}
+
+// Up to 32 rows.  A workgroup takes a sequence, or a piece of its keys, in turns of 64 keys; the next turns' latents
+// are on their way into LDS while one is worked on.  Its four waves share both products out differently.  Scores:
+// sixteen of the turn's keys each.  Sums: a quarter of the components each.  So a latent is read from LDS
+// once for either, and a wave holds the queries and a quarter of the sums.  The rounded weights go
+// from one to the other through LDS.
 //
 // S^T = K Q^T and O^T = C^T P^T: the second product's operand C^T has positions where the rows lie; LDS turns
 // them while they are read (ds_read_b64_tr).
@@ -48,21 +107,22 @@ template <bool F8> __device__ inline int turned(int key) { return F8 ? key & 7 :
 // A row's weights are 2^(s - m) with m the maximum of the first turn in which it sees a key: that is as exact as with
 // the running one, as long as no later score is kFar above it.  Then the sums need not be scaled
 // down on the way, and all waves know m.  Where a score is, the piece is taken again: its maxima first, then the
-// sums.
-template <int DC, bool F8, int RT>
-__global__ __launch_bounds__(kThreads, 1) void k_latent_attention(PagedArgs a) {
+// sums (the rest of the pass that finds it is for nothing: nothing else may leave the loop, or the compiler
+// keeps the sums twice).
+template <int DC, bool F8>
+__global__ __launch_bounds__(kThreads, 1) void k_latent_few(PagedArgs a) {
     constexpr int EB = F8 ? 1 : 2, RB = DC * EB;            // bytes of a latent
-    constexpr int ROWS = 32 * RT;
-    constexpr int KP = RT == 2 ? 2 : 4;                     // parts of a turn's keys among the waves
-    constexpr int QT = RT == 2 ? 1 : 2;                     // query tiles of a wave's scores: 32 wide, or 16
-    constexpr int SK = RT == 2 ? 16 : 32;                   // components of a k-step of the first product
-    constexpr int CS = DC / SK, RS = kRotated / SK;         // its k-steps, of latents and of rotated keys
-    constexpr int NS = RT == 2 ? 16 : 4;                    // scores of a lane and query tile
-    constexpr int DT = DC / 4 / 32;                         // component tiles of a wave
+    constexpr int ROWS = kFewRows, NW = kWaves, T = kThreads;
+    constexpr int KP = 4, TK = kKeys / KP;                  // parts of a turn's keys among the waves' scores, and their keys
+    constexpr int CS = DC / 32, RS = kRotated / 32;         // k-steps of the first product, of latents and of rotated keys
+    constexpr int DT = DC / NW / 32;                        // component tiles of a wave
     constexpr int kRotAt = kKeys * RB, kScaleAt = kRotAt + kKeys * kRotBytes, kStage = kScaleAt + (F8 ? kKeys * 4 : 0);
     constexpr int RPI = 1024 / RB, PPR = RB / 16;           // rows of a load, pieces of a row
     constexpr int kWeightRow = kKeys * 2 + 16;              // bytes
-    __shared__ __attribute__((aligned(128))) char s_ring[2 * kStage];
+    constexpr int NB = kStage > 48 * 1024 ? 2 : 3;          // turns in LDS: the one worked on, and those on their way
+    constexpr int SR = kKeys / NW;                          // keys that a wave loads
+    constexpr int LPT = SR / RPI + SR / 8 + (F8 ? 1 : 0);   // loads of a wave's part of a turn
+    __shared__ __attribute__((aligned(128))) char s_ring[NB * kStage];
     __shared__ __attribute__((aligned(16))) char s_weight[ROWS * kWeightRow];
     __shared__ uint32_t s_page[kThreads];
     __shared__ uint32_t s_seen[ROWS][8];                    // ancestors of the rows' nodes
@@ -73,9 +133,8 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_attention(PagedArgs a) {
 
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int gh = lane >> 5, l32 = lane & 31;
-    const int ql = RT == 2 ? l32 : lane & 15, kg = RT == 2 ? gh : lane >> 4;   // of the first product: query, k-piece
-    const int rw = RT == 2 ? wave & 1 : 0, kp = RT == 2 ? wave >> 1 : wave;
-    constexpr int TK = kKeys / KP;                          // keys of a wave's scores
+    const int ql = lane & 15, kg = lane >> 4;               // of the first product: query, k-piece
+    const int kp = wave;
     const int rows = a.n_q * a.Hq;
     const Place w_ = place_of(a);
     const int b = w_.b;
@@ -83,21 +142,21 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_attention(PagedArgs a) {
     const int q0 = w_.block * ROWS, q1 = min(q0 + ROWS, rows);
     uint32_t id = a.splits == 1 ? table_entry(a, b, 0) : 0u;
     const int64_t R0 = static_cast<int64_t>(b) * rows;
-    u32x4 qf[QT][CS + RS];
-    int node[QT];
+    u32x4 qf[2][CS + RS];                                   // of the wave's two query tiles
+    int node[2];
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-        const int qi = min(q0 + rw * 32 + t * 16 + ql, q1 - 1);
+    for (int t = 0; t < 2; ++t) {
+        const int qi = min(q0 + t * 16 + ql, q1 - 1);
         node[t] = quot(a.by_grp, qi);
         const char *qrow = static_cast<const char *>(a.q) + (R0 + qi) * ((DC + kRotated) * 2);
 #pragma unroll
         for (int c = 0; c < CS; ++c) {
             // in the order in which the keys' pieces come: of e4m3 a lane's sixteen bytes are two k-steps
-            const int d = F8 ? c / 2 * (2 * SK) + kg * 16 + c % 2 * 8 : c * SK + kg * 8;
+            const int d = F8 ? c / 2 * 64 + kg * 16 + c % 2 * 8 : c * 32 + kg * 8;
             qf[t][c] = *reinterpret_cast<const u32x4 *>(qrow + d * 2);
         }
 #pragma unroll
-        for (int c = 0; c < RS; ++c) qf[t][CS + c] = *reinterpret_cast<const u32x4 *>(qrow + (DC + c * SK + kg * 8) * 2);
+        for (int c = 0; c < RS; ++c) qf[t][CS + c] = *reinterpret_cast<const u32x4 *>(qrow + (DC + c * 32 + kg * 8) * 2);
     }
     const Seq s = sequence_of(a, b);
     const Cut cut = cut_of(a, s, q0, q1);
@@ -110,28 +169,24 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_attention(PagedArgs a) {
     bool any_none = false;
     const uint32_t ring = uniform(lds_address(s_ring));
     auto page_of = [&](int key) { return s_page[min(key >> a.c.log_page, last_page) - first_page]; };
-    // this wave's sixteen keys of a turn (all of one page), into LDS
+    // this wave's keys of a turn (all of one page), into LDS
     auto load = [&](int k0, uint32_t stage) {
-        const int key = k0 + wave * 16;
+        const int key = k0 + wave * SR;
         const int64_t page = uniform(page_of(key) & ~kNone);
         const int64_t place = (page << a.c.log_page) + (key & P1);
         const char *c = a.c.k + place * RB, *rot = a.c.v + place * kRotBytes;
-        const uint32_t at = stage + wave * (16 * RB);
+        const uint32_t at = stage + wave * (SR * RB);
 #pragma unroll
-        for (int i = 0; i < 16 / RPI; ++i) {
-            const int row = i * RPI + lane / PPR;
+        for (int i = 0; i < SR / RPI; ++i) {
+            const int row = i * RPI + lane / PPR;           // (a wave's first key is a multiple of eight)
             load_lds16<false>(c + row * RB + ((lane % PPR) ^ turned<F8>(row)) * 16, at + i * 1024);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < SR / 8; ++i) {
             const int row = i * 8 + lane / 8;
-            load_lds16<false>(rot + row * kRotBytes + ((lane % 8) ^ (row & 7)) * 16, stage + kRotAt + wave * (16 * kRotBytes) + i * 1024);
+            load_lds16<false>(rot + row * kRotBytes + ((lane % 8) ^ (row & 7)) * 16, stage + kRotAt + wave * (SR * kRotBytes) + i * 1024);
         }
-        if (F8 && wave == 0) {
-            const int mine = k0 + lane;
-            const int64_t p = page_of(mine) & ~kNone;
-            load_lds4(reinterpret_cast<const char *>(a.c.k_scale + (p << a.c.log_page) + (mine & P1)), stage + kScaleAt);
-        }
+        if (F8 && lane < SR) load_lds4(reinterpret_cast<const char *>(a.c.k_scale + place + lane), stage + kScaleAt + wave * (SR * 4));
     };
     auto look_up = [&](int from, int to, uint32_t entry) {  // of keys [from, to), this thread's table entry given
         first_page = from >> a.c.log_page;
@@ -143,17 +198,17 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_attention(PagedArgs a) {
     if (a.parent) {
         uint32_t(*const anc)[8] = reinterpret_cast<uint32_t(*)[8]>(s_ring);
         find_ancestors(a, b, anc, reinterpret_cast<int *>(s_ring + kMaxSeqRows * 32));
-        for (int i = tid; i < ROWS * 8; i += kThreads) s_seen[i / 8][i % 8] = anc[quot(a.by_grp, min(q0 + i / 8, q1 - 1))][i % 8];
+        for (int i = tid; i < ROWS * 8; i += T) s_seen[i / 8][i % 8] = anc[quot(a.by_grp, min(q0 + i / 8, q1 - 1))][i % 8];
         __syncthreads();
     }
 
     // scores are taken as |scale| (+-q) . k, so that the largest product is the largest score
-    int vis[QT];                                            // keys [0, vis) are seen
+    int vis[2];                                             // keys [0, vis) are seen
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
+    for (int t = 0; t < 2; ++t) {
         const int64_t p = s.qs + node[t];
-        const bool live = q0 + rw * 32 + t * 16 + ql < q1 && p >= 0 && p < s.end;
+        const bool live = q0 + t * 16 + ql < q1 && p >= 0 && p < s.end;
         vis[t] = !live ? 0 : a.parent ? s.lc : p >= s.lc ? s.end : static_cast<int>(p) + 1;
         if (!live) node[t] = -1;
 #pragma unroll
@@ -163,21 +218,9 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_attention(PagedArgs a) {
     }
     const float sc = fmaxf(fabsf(a.scale) * kLog2eP, 1.17549435e-38f);
 
-    floatx16 o[RT][DT];
-    float m[QT], l[QT];                                     // l: of this lane's keys alone
-    auto begin = [&] {
+    float m[2];
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[t][dt][i] = 0.f;
-#pragma unroll
-        for (int t = 0; t < QT; ++t) l[t] = 0.f;
-    };
-    begin();
-#pragma unroll
-    for (int t = 0; t < QT; ++t) m[t] = -INFINITY;
+    for (int t = 0; t < 2; ++t) m[t] = -INFINITY;
     if (tid == 0) s_new = s_far = 0;
 
     // where this lane reads: keys' pieces, rotated keys' pieces, latents' components, weights
@@ -187,283 +230,687 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_attention(PagedArgs a) {
     uint32_t v_at;
     {
         const int j = lane & 15, cg = lane >> 4 & 1, row = 8 * gh + (F8 ? j >> 1 : j >> 2);
-        const int piece = wave * (PPR / 4) + (F8 ? cg : 2 * cg + (j >> 1 & 1));
+        const int piece = wave * (PPR / NW) + (F8 ? cg : 2 * cg + (j >> 1 & 1));
         v_at = row * RB + (piece >> 3) * 128 + ((piece ^ turned<F8>(row)) & 7) * 16 + (j & 1) * 8;
     }
     const char *const w_at = s_weight + l32 * kWeightRow + gh * 16;
 
     const int segment = kSegment << a.c.log_page;
-    // finding: only the rows' maxima, into m
-    auto pass = [&](bool finding) {
+    // Once, unless a score lies far above its row's m: then once more for the maxima alone, and again for the sums.
+    bool finding = false, again = false;
+    for (;;) {
+        floatx16 o[DT];
+        float l[2];                                        // of this lane's keys alone
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) l[t] = 0.f;
         for (int seg = kbeg; seg < kend; seg += segment) {
             const int seg_end = min(seg + segment, kend);
-            if (seg > kbeg || a.splits > 1) id = table_entry(a, b, seg >> a.c.log_page);
+            if (seg > kbeg || a.splits > 1 || again) id = table_entry(a, b, seg >> a.c.log_page);
             if (seg > kbeg) __syncthreads();                // the pages of the segment before are used up
             look_up(seg, seg_end, id);
             load(seg, ring);
-            for (int k0 = seg, buf = 0; k0 < seg_end; k0 += kKeys, buf ^= 1) {
-                wait_vm<0>();                               // this wave's part of the turn
+            if (NB > 2 && seg + kKeys < seg_end) load(seg + kKeys, ring + kStage);
+            int buf = 0;
+            for (int k0 = seg; k0 < seg_end; k0 += kKeys, buf = buf + 1 == NB ? 0 : buf + 1) {
+                // this wave's part of the turn
+                if (NB > 2 && k0 + kKeys < seg_end) wait_vm<LPT>();
+                else wait_vm<0>();
                 lds_barrier();                              // ... and the others'; the turn before is used up
-                if (k0 + kKeys < seg_end) load(k0 + kKeys, ring + (buf ^ 1) * kStage);
                 char *const stage = s_ring + buf * kStage;
                 const bool masked = k0 + kKeys > all_see || any_none;   // the same in the whole workgroup
                 if (masked) {
-                    // Places that hold no key of the sequence may hold anything, and a weight of zero does not make
-                    // a NaN harmless: they become zeros, as do latents that are not finite, whose keys are marked.
                     if (tid < 2) s_bad[tid] = 0;
                     lds_barrier();
-                    const int key = tid >> 2, part = tid & 3;
-                    const bool real = k0 + key < kend && page_of(k0 + key) < kNone;
-                    float *const scale = reinterpret_cast<float *>(stage + kScaleAt) + key;
-                    uint32_t top = 0;
-#pragma unroll 2
-                    for (int i = 0; i < PPR / 4; ++i) {
-                        u32x4 *at = reinterpret_cast<u32x4 *>(stage + key * RB + (part + 4 * i) * 16);
-                        u32x4 x = *at;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t t = not_finite<F8>(x[e], 0x01010101u);
-                            top |= t;
-                            x[e] = real ? x[e] & ~(t | (t - (t >> (F8 ? 7 : 15)))) : 0u;
-                        }
-                        *at = x;
-                    }
-                    bool bad = top != 0;
-                    if constexpr (F8) {
-                        const float sv = *scale;
-                        const bool wild = !(fabsf(sv) < INFINITY);
-                        bad |= wild;
-                        wait_lds();
-                        if (part == 0 && (wild || !real)) *scale = 0.f;   // (the four of a key are of one wave)
-                    }
-                    if (real && bad) atomicOr(&s_bad[key >> 5], 1u << (key & 31));
+                    const int key = k0 + tid / (T / kKeys);
+                    clean_turn<RB, kKeys, T, F8>(stage, reinterpret_cast<float *>(stage + kScaleAt), s_bad, tid,
+                                                 key < kend && page_of(key) < kNone);
                     lds_barrier();
                 }
-                // S^T
-                typedef std::conditional_t<RT == 2, floatx16, floatx4> Tile;
-                Tile st[QT];
+                // S^T.  Operands are read from LDS a group ahead of the products that take them.
+                constexpr int LOADS = CS / (F8 ? 2 : 1), G = F8 ? 4 : 8, NG = LOADS / G;
+                floatx4 st[2];
 #pragma unroll
-                for (int t = 0; t < QT; ++t)
+                for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int i = 0; i < NS; ++i) st[t][i] = 0.f;
-                auto multiply = [&](u32x4 k, int c) {
+                    for (int i = 0; i < 4; ++i) st[t][i] = 0.f;
+                u32x4 kf[2][G], rf[RS];
+                auto read_keys = [&](int g) __attribute__((always_inline)) {
 #pragma unroll
-                    for (int t = 0; t < QT; ++t) {
-                        if constexpr (RT == 2) st[t] = mfma32(k, qf[t][c], st[t]);
-                        else st[t] = mfma(k, qf[t][c], st[t]);
+                    for (int i = 0; i < G; ++i) {
+                        const int c = g * G + i;
+                        kf[g & 1][i] = *reinterpret_cast<const u32x4 *>(stage + (k_at ^ (c % 2 * 64)) + c / 2 * 128);
                     }
                 };
-                // sixteen-byte pieces of a key that a load's lanes take side by side
-                constexpr int LP = RT == 2 ? 2 : 4, PER = 8 / LP;
-                constexpr int LOADS = CS / (F8 ? 2 : 1);
+                auto read_rotated = [&]() __attribute__((always_inline)) {
 #pragma unroll
-                for (int c = 0; c < LOADS; ++c) {
-                    const u32x4 raw = *reinterpret_cast<const u32x4 *>(stage + (k_at ^ (c % PER * LP * 16)) + c / PER * 128);
-                    if constexpr (F8) {
-                        multiply(widen(raw[0], raw[1], 1.f), 2 * c);
-                        multiply(widen(raw[2], raw[3], 1.f), 2 * c + 1);
-                    } else {
-                        multiply(raw, c);
-                    }
-                }
-                float sv[F8 ? NS : 1];                      // scales of this lane's keys
-                if constexpr (F8) {
-#pragma unroll
-                    for (int e = 0; e < NS / 4; ++e) {
-                        const floatx4 x = *reinterpret_cast<const floatx4 *>(stage + kScaleAt + (kp * TK + 8 * e + 4 * kg) * 4);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) sv[4 * e + i] = x[i];
-                    }
-#pragma unroll
-                    for (int t = 0; t < QT; ++t)
-#pragma unroll
-                        for (int i = 0; i < NS; ++i) st[t][i] *= sv[i];
-                }
-#pragma unroll
-                for (int c = 0; c < RS; ++c)
-                    multiply(*reinterpret_cast<const u32x4 *>(stage + (r_at ^ (c * LP * 16))), CS + c);
-                if (masked) {
-                    const int kb = k0 + kp * TK;
-                    uint32_t real = low_bits(kend - kb);
-                    if (page_of(kb) >= kNone) real &= 0xffff0000u;
-                    if (TK == 32 && page_of(kb + 16) >= kNone) real &= 0x0000ffffu;
-                    const uint32_t bad = s_bad[kp * TK / 32] >> (kp * TK % 32 + 4 * kg);
-#pragma unroll
-                    for (int t = 0; t < QT; ++t) {
-                        uint32_t see = low_bits(vis[t] - kb);
-                        if (a.parent && node[t] >= 0) see |= window32(s_seen[rw * 32 + t * 16 + ql], kb - s.lc);
-                        see = (see & real) >> (4 * kg);
-#pragma unroll
-                        for (int i = 0; i < NS; ++i) {
-                            const int bit = 8 * (i / 4) + i % 4;
-                            if (!(see >> bit & 1)) st[t][i] = -INFINITY;
-                            else if (bad >> bit & 1) st[t][i] = NAN;
-                        }
-                    }
-                }
-                float bm[QT];
-                bool fresh = false;                         // a row's first keys, or a score far above m
-#pragma unroll
-                for (int t = 0; t < QT; ++t) {
-                    bm[t] = -INFINITY;
-#pragma unroll
-                    for (int i = 0; i < NS; ++i) bm[t] = fmaxf(bm[t], st[t][i]);
-                    if constexpr (RT == 2) {
-                        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(bm[t]), __float_as_uint(bm[t]), false, false);
-                        bm[t] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
-                    } else {
-                        bm[t] = max_rows(bm[t]);
-                    }
-                    bm[t] *= sc;
-                    fresh |= bm[t] > m[t] + kFar;           // always when m is still -inf
-                }
-                if (finding) {
-#pragma unroll
-                    for (int t = 0; t < QT; ++t) m[t] = fmaxf(m[t], bm[t]);
-                    continue;
-                }
-                float sum[QT];
-                auto weigh = [&] {
-#pragma unroll
-                    for (int t = 0; t < QT; ++t) {
-                        // a query that has seen nothing yet keeps m = -inf and adds nothing
-                        const float mm = m[t] == -INFINITY ? INFINITY : m[t];
-                        sum[t] = 0.f;
-                        char *to = s_weight + (rw * 32 + t * 16 + ql) * kWeightRow + (kp * TK + 4 * kg) * 2;
-#pragma unroll
-                        for (int e = 0; e < NS / 4; ++e) {
-                            float p[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                p[i] = __builtin_amdgcn_exp2f(fmaf(st[t][4 * e + i], sc, -mm));
-                                sum[t] += p[i];
-                                if constexpr (F8) p[i] *= sv[4 * e + i];
-                            }
-                            *reinterpret_cast<u32x2 *>(to + e * 16) = u32x2{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3])};
-                        }
-                    }
+                    for (int c = 0; c < RS; ++c) rf[c] = *reinterpret_cast<const u32x4 *>(stage + (r_at ^ (c * 64)));
                 };
-                weigh();
-                if (__ballot(fresh) != 0 && lane == 0) s_new = 1;
-                lds_barrier();                              // the weights are there
-                if (__builtin_expect(uniform(s_new), 0)) {
-                    // the same maximum in all waves, then the weights again
-                    if (kg == 0) {
+                auto multiply = [&](u32x4 k, int c) __attribute__((always_inline)) {
 #pragma unroll
-                        for (int t = 0; t < QT; ++t) s_max[kp][rw * 32 + t * 16 + ql] = bm[t];
-                    }
-                    lds_barrier();
-                    if (tid == 0) s_new = 0;
-                    bool far = false;
-#pragma unroll
-                    for (int t = 0; t < QT; ++t) {
-                        float top = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < KP; ++i) top = fmaxf(top, s_max[i][rw * 32 + t * 16 + ql]);
-                        if (m[t] == -INFINITY) m[t] = top;
-                        else far |= top > m[t] + kFar;
-                    }
-                    if (__ballot(far) != 0 && lane == 0) s_far = 1;
-                    weigh();
-                    lds_barrier();
-                    if (uniform(s_far)) return;
+                    for (int t = 0; t < 2; ++t) st[t] = mfma(k, qf[t][c], st[t]);
+                };
+                read_keys(0);
+                if constexpr (NG > 1) read_keys(1);
+                else read_rotated();
+                __builtin_amdgcn_sched_barrier(0);
+                {
+                    const int ahead = k0 + (NB - 1) * kKeys;
+                    const int to = NB > 2 ? (buf == 0 ? NB - 1 : buf - 1) : buf ^ 1;
+                    if (ahead < seg_end) load(ahead, ring + to * kStage);
                 }
+                floatx4 sv;                                 // scales of this lane's keys
+                if constexpr (F8) sv = *reinterpret_cast<const floatx4 *>(stage + kScaleAt + (kp * TK + 4 * kg) * 4);
 #pragma unroll
-                for (int t = 0; t < QT; ++t) l[t] += sum[t];
-                // O^T += C^T P^T
+                for (int g = 0; g < NG; ++g) {
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int v = 0; v < kKeys / 16; ++v) {
-                    u32x4 pb[RT];
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) pb[t] = *reinterpret_cast<const u32x4 *>(w_at + t * (32 * kWeightRow) + v * 32);
+                    for (int i = 0; i < G; ++i) {
+                        const u32x4 raw = kf[g & 1][i];
+                        const int c = g * G + i;
+                        if constexpr (F8) {
+                            multiply(widen(raw[0], raw[1], 1.f), 2 * c);
+                            multiply(widen(raw[2], raw[3], 1.f), 2 * c + 1);
+                        } else {
+                            multiply(raw, c);
+                        }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (g + 2 < NG) read_keys(g + 2);
+                    else if (g + 2 == NG) read_rotated();
+                }
+                // the second product's operands, sixteen keys at a time; the first ones now
+                constexpr int NV = kKeys / 16;
+                u32x4 pb[2], vf[2][DT];                     // (e4m3: two words of each)
+                auto read_values = [&](int v) __attribute__((always_inline)) {
+                    const char *const at = stage + v * 16 * RB;
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) {
-                        u32x4 vf;
-                        const char *at = stage + v * 16 * RB;
                         if constexpr (F8) {
                             const i32x2 raw = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(at + (v_at ^ (dt % 4 * 32))));
-                            vf = widen(raw[0], raw[1], 1.f);
+                            vf[v & 1][dt][0] = raw[0];
+                            vf[v & 1][dt][1] = raw[1];
                         } else {
                             const uint32_t here = (v_at ^ (dt % 2 * 64)) + dt / 2 * 128;
                             const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + here)));
                             const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 4 * RB + (here ^ 16))));
-                            vf = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                            vf[v & 1][dt] = u32x4{lo[0], lo[1], hi[0], hi[1]};
                         }
-#pragma unroll
-                        for (int t = 0; t < RT; ++t) o[t][dt] = mfma32(vf, pb[t], o[t][dt]);
                     }
+                };
+                auto read_weights = [&](int v) __attribute__((always_inline)) {
+                    pb[v & 1] = *reinterpret_cast<const u32x4 *>(w_at + v * 32);
+                };
+                read_values(0);
+                if constexpr (F8) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) st[t][i] *= sv[i];
+                }
+#pragma unroll
+                for (int c = 0; c < RS; ++c) multiply(rf[c], CS + c);
+                if (masked) {
+                    const int kb = k0 + kp * TK;
+                    uint32_t real = low_bits(kend - kb);
+                    if (page_of(kb) >= kNone) real = 0;
+                    const uint32_t bad = s_bad[kp * TK / 32] >> (kp * TK % 32 + 4 * kg);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        uint32_t see = low_bits(vis[t] - kb);
+                        if (a.parent && node[t] >= 0) see |= window32(s_seen[t * 16 + ql], kb - s.lc);
+                        see = (see & real) >> (4 * kg);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = (bad >> i & 1) != 0 ? NAN : st[t][i];
+                            st[t][i] = (see >> i & 1) != 0 ? x : -INFINITY;
+                        }
+                    }
+                }
+                float bm[2];
+                bool fresh = false;                         // a row's first keys, or a score far above m
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    bm[t] = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) bm[t] = fmaxf(bm[t], st[t][i]);
+                    bm[t] = max_rows(bm[t]) * sc;
+                    fresh |= bm[t] > m[t] + kFar;           // always when m is still -inf
+                }
+                float sum[2];
+                auto weigh = [&]() __attribute__((always_inline)) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        // a query that has seen nothing yet keeps m = -inf and adds nothing
+                        const float mm = m[t] == -INFINITY || finding ? INFINITY : m[t];
+                        sum[t] = 0.f;
+                        char *to = s_weight + (t * 16 + ql) * kWeightRow + (kp * TK + 4 * kg) * 2;
+                        float p[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            p[i] = __builtin_amdgcn_exp2f(fmaf(st[t][i], sc, -mm));
+                            sum[t] += p[i];
+                            if constexpr (F8) p[i] *= sv[i];
+                        }
+                        *reinterpret_cast<u32x2 *>(to) = u32x2{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3])};
+                    }
+                };
+                weigh();
+                if (finding) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) m[t] = fmaxf(m[t], bm[t]);
+                } else if (__ballot(fresh) != 0 && lane == 0) {
+                    s_new = 1;
+                }
+                lds_barrier();                              // the weights are there
+                read_weights(0);
+                if (__builtin_expect(uniform(s_new), 0)) {
+                    // the same maximum in all waves, then the weights again
+                    if (kg == 0) {
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) s_max[kp][t * 16 + ql] = bm[t];
+                    }
+                    lds_barrier();
+                    if (tid == 0) s_new = 0;
+                    bool above = false;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        float top = -INFINITY;
+#pragma unroll
+                        for (int i = 0; i < KP; ++i) top = fmaxf(top, s_max[i][t * 16 + ql]);
+                        if (m[t] == -INFINITY) m[t] = top;
+                        else above |= top > m[t] + kFar;
+                    }
+                    if (__ballot(above) != 0 && lane == 0) s_far = 1;
+                    weigh();
+                    lds_barrier();
+                    read_weights(0);
+                }
+#pragma unroll
+                for (int t = 0; t < 2; ++t) l[t] += sum[t];
+                // O^T += C^T P^T
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    if (v + 1 < NV) {
+                        read_values(v + 1);
+                        read_weights(v + 1);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        const u32x4 raw = vf[v & 1][dt], c = F8 ? widen(raw[0], raw[1], 1.f) : raw;
+                        o[dt] = mfma32(c, pb[v & 1], o[dt]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
-    };
-    // every row's maximum and sum, joined over the parts of the keys
-    auto join_max = [&] {
+        wait_vm<0>();
         __syncthreads();
-        if (kg == 0) {
+        if (!finding && uniform(s_far) == 0) {
 #pragma unroll
-            for (int t = 0; t < QT; ++t) s_max[kp][rw * 32 + t * 16 + ql] = m[t];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-#pragma unroll
-            for (int i = 0; i < KP; ++i) m[t] = fmaxf(m[t], s_max[i][rw * 32 + t * 16 + ql]);
-        }
-    };
-    pass(false);
-    __syncthreads();
-    if (__builtin_expect(uniform(s_far), 0)) {
-        wait_vm<0>();                                       // (a turn may still be on its way)
-        __syncthreads();
-        if (tid == 0) s_new = s_far = 0;
-        pass(true);
-        join_max();
-        begin();
-        pass(false);
-        __syncthreads();
-    }
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-        if constexpr (RT == 1) l[t] += __shfl_xor(l[t], 16);
-        l[t] += __shfl_xor(l[t], 32);
-        if (kg == 0) {
-            s_sum[kp][rw * 32 + t * 16 + ql] = node[t] >= 0 ? l[t] : 0.f;   // (unmasked turns give padding rows some weights)
-            s_max[kp][rw * 32 + t * 16 + ql] = node[t] >= 0 ? m[t] : -INFINITY;
-        }
-    }
-    __syncthreads();
-    // O^T tile dt, elements 4e .. 4e + 3: components 32 dt + 8 e + 4 gh + 0..3 of the wave's quarter, of row l32
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const int row = t * 32 + l32, qi = q0 + row;
-        if (qi >= q1) continue;
-        float L = 0.f;
-#pragma unroll
-        for (int i = 0; i < KP; ++i) L += s_sum[i][row];
-        if (cut.pieces == 1) {
-            const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;   // NaN stays
-            char *dst = static_cast<char *>(a.out) + ((R0 + qi) * DC + wave * (DC / 4) + 4 * gh) * 2;
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    floatx4 x;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = L == 0.f ? 0.f : o[t][dt][4 * e + i] * inv;
-                    *reinterpret_cast<u32x2 *>(dst + (32 * dt + 8 * e) * 2) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+            for (int t = 0; t < 2; ++t) {
+                l[t] += __shfl_xor(l[t], 16);
+                l[t] += __shfl_xor(l[t], 32);
+                if (kg == 0) {
+                    s_sum[kp][t * 16 + ql] = node[t] >= 0 ? l[t] : 0.f;   // (unmasked turns give padding rows some weights)
+                    s_max[kp][t * 16 + ql] = node[t] >= 0 ? m[t] : -INFINITY;
                 }
+            }
+            __syncthreads();
+            // O^T tile dt, elements 4e .. 4e + 3: components 32 dt + 8 e + 4 gh + 0..3 of the wave's part, of row l32
+            const int qi = q0 + l32;
+            if (qi >= q1) return;
+            float L = 0.f;
+#pragma unroll
+            for (int i = 0; i < KP; ++i) L += s_sum[i][l32];
+            store_sums<DC, DT>(a, o, R0 + qi, wave * (DC / NW) + 4 * gh, cut.pieces, w_.piece, s_max[0][l32], L, wave == 0 && gh == 0);
+            return;
+        }
+        if (finding) {                                      // every row's maximum, joined over the parts of the keys
+            if (kg == 0) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) s_max[kp][t * 16 + ql] = m[t];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < KP; ++i) m[t] = fmaxf(m[t], s_max[i][t * 16 + ql]);
+            finding = false;
         } else {
-            const int64_t at = w_.piece * (static_cast<int64_t>(a.B) * rows) + R0 + qi;
-            float *po = a.part_o + at * DC + wave * (DC / 4) + 4 * gh;
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    *reinterpret_cast<floatx4 *>(po + 32 * dt + 8 * e) =
-                        floatx4{o[t][dt][4 * e], o[t][dt][4 * e + 1], o[t][dt][4 * e + 2], o[t][dt][4 * e + 3]};
-            if (wave == 0 && gh == 0) a.part_ml[at] = make_float2(s_max[0][row], L);
+            __syncthreads();                                // every wave knows of it
+            if (tid == 0) s_far = 0;
+            finding = again = true;
         }
     }
+}
+
+// More rows: 64 of them a workgroup, with four waves for the scores and four for the sums, one of each on a SIMD.
+// While the latter add up one turn, the former work on the next, so that the matrix cores are fed by one wave while the
+// other is at its exponentials, conversions or waits.  (One wave for both leaves them idle then: a lone wave
+// issues a vector instruction every 7.5 cycles.  Two for both would need 144 registers of queries and 64 of sums
+// each, and room to work.)
+//
+// Scores: 32 rows and half of a turn's keys a wave, with products of 32 x 32 (turns of 64 keys) or 16 x 16 (32
+// keys, where 64 would not fit three times into LDS).  Sums: all rows and a quarter of the components a wave.
+//
+// After barrier i turn i is staged and turn i - 1 weighed: the scores' waves take turn i, the sums' waves turn
+// i - 1, and load ahead.  Rows' maxima as in k_latent_few.
+template <int DC, bool F8>
+__global__ __launch_bounds__(512, 1) void k_latent_many(PagedArgs a) {
+    constexpr int EB = F8 ? 1 : 2, RB = DC * EB;            // bytes of a latent
+    constexpr int KS = RB > 512 ? 32 : 64;                  // keys of a turn
+    constexpr bool WIDE = KS == 64;
+    constexpr int QT = WIDE ? 1 : 2, QW = WIDE ? 32 : 16;   // query tiles of a scores' wave, and their width
+    constexpr int SK = WIDE ? 16 : 32;                      // components of a k-step of its products
+    constexpr int CS = DC / SK, RS = kRotated / SK;         // its k-steps, of latents and of rotated keys
+    constexpr int NS = WIDE ? 16 : 4;                       // scores of a lane and query tile
+    constexpr int TK = KS / 2;                              // keys of a wave's scores
+    constexpr int DT = DC / 4 / 32;                         // component tiles of a sums' wave
+    constexpr int kRotAt = KS * RB, kScaleAt = kRotAt + KS * kRotBytes, kStage = kScaleAt + (F8 ? KS * 4 : 0);
+    constexpr int NB = RB > 512 ? 4 : 3, AHEAD = NB - 2;    // turns in LDS, and on their way
+    constexpr int RPI = 1024 / RB, PPR = RB / 16;           // rows of a load, pieces of a row
+    constexpr int SR = KS / 4;                              // keys that a sums' wave loads
+    constexpr int LPT = SR / RPI + SR / 8 + (F8 ? 1 : 0);   // its loads of a turn
+    constexpr int kWeightRow = KS * 2 + 16;                 // bytes
+    constexpr int ROWS = kManyRows;
+    __shared__ __attribute__((aligned(128))) char s_ring[NB * kStage];
+    __shared__ __attribute__((aligned(16))) char s_weight[2][ROWS * kWeightRow];
+    __shared__ uint32_t s_page[kThreads];
+    __shared__ uint32_t s_seen[ROWS][8];                    // ancestors of the rows' nodes
+    __shared__ float s_max[2][ROWS];
+    __shared__ float s_sum[2][ROWS];
+    __shared__ uint32_t s_bad[2];                           // of a turn's keys: latent or scale not finite
+    __shared__ int s_new, s_far, s_none;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int gh = lane >> 5, l32 = lane & 31;
+    const int rows = a.n_q * a.Hq;
+    const Place w_ = place_of(a);
+    const int b = w_.b;
+    if (b >= a.B) return;
+    const int q0 = w_.block * ROWS, q1 = min(q0 + ROWS, rows);
+    const int64_t R0 = static_cast<int64_t>(b) * rows;
+    const Seq s = sequence_of(a, b);
+    const Cut cut = cut_of(a, s, q0, q1);
+    if (w_.piece >= cut.pieces) return;
+    const int kbeg = w_.piece * cut.chunk, kend = min(kbeg + cut.chunk, cut.kend);
+    const int all_see = seen_by_all(a, s, q0, kend);        // keys below are seen by every row that sees any
+    if (a.parent) {
+        uint32_t(*const anc)[8] = reinterpret_cast<uint32_t(*)[8]>(s_ring);
+        find_ancestors(a, b, anc, reinterpret_cast<int *>(s_ring + kMaxSeqRows * 32));
+        s_seen[tid / 8][tid % 8] = anc[quot(a.by_grp, min(q0 + tid / 8, q1 - 1))][tid % 8];
+        __syncthreads();
+    }
+    if (tid == 0) s_new = s_far = 0;
+
+    const int P1 = (1 << a.c.log_page) - 1;
+    const int segment = kSegment << a.c.log_page;
+    const uint32_t ring = uniform(lds_address(s_ring));
+    const float sc = fmaxf(fabsf(a.scale) * kLog2eP, 1.17549435e-38f);
+
+    // All of it, as one kind of wave does it: both meet the same barriers.
+    auto work = [&](auto kind) __attribute__((always_inline)) {
+        constexpr bool SCORES = decltype(kind)::value;
+        // scores: queries, in the order in which the keys' pieces come (of e4m3 a lane's sixteen bytes are two k-steps)
+        const int ql = WIDE ? l32 : lane & 15, kg = WIDE ? gh : lane >> 4;   // query, k-piece
+        const int rw = wave & 1, kp = wave >> 1 & 1;
+        [[maybe_unused]] u32x4 qf[QT][CS + RS];
+        [[maybe_unused]] int node[QT], vis[QT];             // keys [0, vis) are seen
+        [[maybe_unused]] float m[QT];
+        [[maybe_unused]] const uint32_t k_at = (kp * TK + ql) * RB + ((kg ^ turned<F8>(ql)) & 7) * 16;
+        [[maybe_unused]] const uint32_t r_at = kRotAt + (kp * TK + ql) * kRotBytes + ((kg ^ ql) & 7) * 16;
+        if constexpr (SCORES) {
+            const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;   // scores as |scale| (+-q) . k: the largest product is the largest
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                const int row = q0 + rw * 32 + t * 16 + ql, qi = min(row, q1 - 1);
+                node[t] = quot(a.by_grp, qi);
+                const char *qrow = static_cast<const char *>(a.q) + (R0 + qi) * ((DC + kRotated) * 2);
+                const int64_t p = s.qs + node[t];
+                const bool live = row < q1 && p >= 0 && p < s.end;
+                vis[t] = !live ? 0 : a.parent ? s.lc : p >= s.lc ? s.end : static_cast<int>(p) + 1;
+                if (!live) node[t] = -1;
+                m[t] = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < CS + RS; ++c) {
+                    const int d = c >= CS ? DC + (c - CS) * SK + kg * 8 : F8 ? c / 2 * (2 * SK) + kg * 16 + c % 2 * 8 : c * SK + kg * 8;
+                    qf[t][c] = *reinterpret_cast<const u32x4 *>(qrow + d * 2);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) qf[t][c][x] = live ? qf[t][c][x] ^ flip : 0u;
+                }
+            }
+        }
+        // sums
+        const int pw = wave & 3;
+        [[maybe_unused]] uint32_t v_at = 0;
+        if constexpr (!SCORES) {
+            const int j = lane & 15, cg = lane >> 4 & 1, row = 8 * gh + (F8 ? j >> 1 : j >> 2);
+            const int piece = pw * (PPR / 4) + (F8 ? cg : 2 * cg + (j >> 1 & 1));
+            v_at = row * RB + (piece >> 3) * 128 + ((piece ^ turned<F8>(row)) & 7) * 16 + (j & 1) * 8;
+        }
+        int first_page = 0, last_page = 0;                  // of those in LDS
+        bool any_none = false;
+        auto page_of = [&](int key) { return s_page[min(key >> a.c.log_page, last_page) - first_page]; };
+        // this wave's keys of a turn (all of one page), into LDS
+        [[maybe_unused]] auto load = [&](int k0, int buf) {
+            const uint32_t stage = ring + buf * kStage;
+            const int key = k0 + pw * SR;
+            const int64_t page = uniform(page_of(key) & ~kNone);
+            const int64_t place = (page << a.c.log_page) + (key & P1);
+            const char *c = a.c.k + place * RB, *rot = a.c.v + place * kRotBytes;
+#pragma unroll
+            for (int i = 0; i < SR / RPI; ++i) {
+                const int row = i * RPI + lane / PPR;       // (a wave's first key is a multiple of eight)
+                load_lds16<false>(c + row * RB + ((lane % PPR) ^ turned<F8>(row)) * 16, stage + pw * (SR * RB) + i * 1024);
+            }
+#pragma unroll
+            for (int i = 0; i < SR / 8; ++i) {
+                const int row = i * 8 + lane / 8;
+                load_lds16<false>(rot + row * kRotBytes + ((lane % 8) ^ (row & 7)) * 16, stage + kRotAt + pw * (SR * kRotBytes) + i * 1024);
+            }
+            if (F8 && lane < SR) load_lds4(reinterpret_cast<const char *>(a.c.k_scale + place + lane), stage + kScaleAt + pw * (SR * 4));
+        };
+
+        // Once, unless a score lies far above its row's m: then once more for the maxima alone, and again for the sums.
+        bool finding = false;
+        for (;;) {
+            [[maybe_unused]] floatx16 o[2][DT];
+            [[maybe_unused]] float l[QT];                   // of this lane's keys alone
+            if constexpr (SCORES) {
+#pragma unroll
+                for (int t = 0; t < QT; ++t) l[t] = 0.f;
+            } else {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[t][dt][i] = 0.f;
+            }
+            for (int seg = kbeg; seg < kend; seg += segment) {
+                const int seg_end = min(seg + segment, kend), turns = (seg_end - seg + KS - 1) / KS;
+                first_page = seg >> a.c.log_page;
+                last_page = (seg_end - 1) >> a.c.log_page;
+                const uint32_t entry = table_entry(a, b, first_page);
+                __syncthreads();                            // the pages of the segment before are used up
+                if (tid == 0) s_none = 0;
+                __syncthreads();
+                if (tid <= last_page - first_page) {        // a page that is none is read as page 0, and not used
+                    const bool none = entry >= static_cast<uint32_t>(a.c.n_pages);
+                    s_page[tid] = none ? kNone : entry;
+                    if (none) s_none = 1;
+                }
+                __syncthreads();
+                any_none = uniform(s_none) != 0;
+                if constexpr (!SCORES) {
+#pragma unroll
+                    for (int i = 0; i < AHEAD; ++i)
+                        if (i < turns) load(seg + i * KS, i);
+                }
+                [[maybe_unused]] typename std::conditional<WIDE, floatx16, floatx4>::type st[QT];
+                [[maybe_unused]] float sv[F8 ? NS : 1];     // scales of this lane's keys
+                [[maybe_unused]] float bm[QT], sum[QT];
+                int buf = 0;                                // of turn i
+                for (int i = 0; i <= turns; ++i, buf = buf + 1 == NB ? 0 : buf + 1) {
+                    const int k0 = seg + i * KS;
+                    if constexpr (!SCORES) {                // turn i has come
+                        if (AHEAD > 1 && i + 1 < turns) wait_vm<LPT>();
+                        else wait_vm<0>();
+                    }
+                    lds_barrier();
+                    [[maybe_unused]] auto weigh = [&](int turn) __attribute__((always_inline)) {
+#pragma unroll
+                        for (int t = 0; t < QT; ++t) {
+                            // a query that has seen nothing yet keeps m = -inf and adds nothing
+                            const float mm = m[t] == -INFINITY || finding ? INFINITY : m[t];
+                            sum[t] = 0.f;
+                            char *to = s_weight[turn & 1] + (rw * 32 + t * QW + ql) * kWeightRow + (kp * TK + 4 * kg) * 2;
+#pragma unroll
+                            for (int e = 0; e < NS / 4; ++e) {
+                                float p[4];
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) {
+                                    p[x] = __builtin_amdgcn_exp2f(fmaf(st[t][4 * e + x], sc, -mm));
+                                    sum[t] += p[x];
+                                    if constexpr (F8) p[x] *= sv[4 * e + x];
+                                }
+                                *reinterpret_cast<u32x2 *>(to + e * 16) = u32x2{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3])};
+                            }
+                        }
+                    };
+                    if (__builtin_expect(uniform(s_new), 0)) {
+                        // the same maximum in all waves, then the weights of turn i - 1 again
+                        if constexpr (SCORES) {
+                            if (kg == 0) {
+#pragma unroll
+                                for (int t = 0; t < QT; ++t) s_max[kp][rw * 32 + t * QW + ql] = bm[t];
+                            }
+                        }
+                        lds_barrier();
+                        if constexpr (SCORES) {
+                            if (tid == 0) s_new = 0;
+                            bool above = false;
+#pragma unroll
+                            for (int t = 0; t < QT; ++t) {
+                                const int row = rw * 32 + t * QW + ql;
+                                const float top = fmaxf(s_max[0][row], s_max[1][row]);
+                                if (m[t] == -INFINITY) m[t] = top;
+                                else above |= top > m[t] + kFar;
+                            }
+                            if (__ballot(above) != 0 && lane == 0) s_far = 1;
+                            weigh(i - 1);
+                        }
+                        lds_barrier();
+                    }
+                    const bool masked = i < turns && (k0 + KS > all_see || any_none);   // the same in the whole workgroup
+                    char *const stage = s_ring + buf * kStage;
+                    if (masked) {
+                        if (tid < 2) s_bad[tid] = 0;
+                        lds_barrier();
+                        const int key = k0 + tid / (512 / KS);
+                        clean_turn<RB, KS, 512, F8>(stage, reinterpret_cast<float *>(stage + kScaleAt), s_bad, tid,
+                                                    key < kend && page_of(key) < kNone);
+                        lds_barrier();
+                    }
+                    if constexpr (SCORES) {
+                        if (i > 0) {
+#pragma unroll
+                            for (int t = 0; t < QT; ++t) l[t] += sum[t];
+                        }
+                        if (i == turns) break;
+                        // S^T.  Operands are read from LDS a group ahead of the products that take them.
+                        constexpr int LP = WIDE ? 2 : 4, PER = 8 / LP;   // pieces of a key that a load's lanes take side by side
+                        constexpr int LOADS = CS / (F8 ? 2 : 1), G = F8 ? 2 : 4, NG = LOADS / G;
+#pragma unroll
+                        for (int t = 0; t < QT; ++t)
+#pragma unroll
+                            for (int x = 0; x < NS; ++x) st[t][x] = 0.f;
+                        u32x4 kf[2][G], rf[RS];
+                        auto read_keys = [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+                            for (int x = 0; x < G; ++x) {
+                                const int c = g * G + x;
+                                kf[g & 1][x] = *reinterpret_cast<const u32x4 *>(stage + (k_at ^ (c % PER * LP * 16)) + c / PER * 128);
+                            }
+                        };
+                        auto multiply = [&](u32x4 k, int c) __attribute__((always_inline)) {
+#pragma unroll
+                            for (int t = 0; t < QT; ++t) {
+                                if constexpr (WIDE) st[t] = mfma32(k, qf[t][c], st[t]);
+                                else st[t] = mfma(k, qf[t][c], st[t]);
+                            }
+                        };
+                        read_keys(0);
+                        read_keys(1);
+                        if constexpr (F8) {
+#pragma unroll
+                            for (int e = 0; e < NS / 4; ++e) {
+                                const floatx4 x = *reinterpret_cast<const floatx4 *>(stage + kScaleAt + (kp * TK + 8 * e + 4 * kg) * 4);
+#pragma unroll
+                                for (int y = 0; y < 4; ++y) sv[4 * e + y] = x[y];
+                            }
+                        }
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) {
+                            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                            for (int x = 0; x < G; ++x) {
+                                const u32x4 raw = kf[g & 1][x];
+                                const int c = g * G + x;
+                                if constexpr (F8) {
+                                    multiply(widen(raw[0], raw[1], 1.f), 2 * c);
+                                    multiply(widen(raw[2], raw[3], 1.f), 2 * c + 1);
+                                } else {
+                                    multiply(raw, c);
+                                }
+                            }
+                            __builtin_amdgcn_sched_barrier(0);
+                            if (g + 2 < NG) {
+                                read_keys(g + 2);
+                            } else if (g + 2 == NG) {
+#pragma unroll
+                                for (int c = 0; c < RS; ++c) rf[c] = *reinterpret_cast<const u32x4 *>(stage + (r_at ^ (c * LP * 16)));
+                            }
+                        }
+                        if constexpr (F8) {
+#pragma unroll
+                            for (int t = 0; t < QT; ++t)
+#pragma unroll
+                                for (int x = 0; x < NS; ++x) st[t][x] *= sv[x];
+                        }
+#pragma unroll
+                        for (int c = 0; c < RS; ++c) multiply(rf[c], CS + c);
+                        if (masked) {
+                            const int kb = k0 + kp * TK;
+                            uint32_t real = low_bits(kend - kb);
+                            if (page_of(kb) >= kNone) real &= 0xffff0000u;
+                            if (TK == 32 && page_of(kb + 16) >= kNone) real &= 0x0000ffffu;
+                            const uint32_t bad = s_bad[kp * TK / 32] >> (kp * TK % 32 + 4 * kg);
+#pragma unroll
+                            for (int t = 0; t < QT; ++t) {
+                                uint32_t see = low_bits(vis[t] - kb);
+                                if (a.parent && node[t] >= 0) see |= window32(s_seen[rw * 32 + t * QW + ql], kb - s.lc);
+                                see = (see & real) >> (4 * kg);
+#pragma unroll
+                                for (int x = 0; x < NS; ++x) {
+                                    const int bit = 8 * (x / 4) + x % 4;
+                                    const float y = (bad >> bit & 1) != 0 ? NAN : st[t][x];
+                                    st[t][x] = (see >> bit & 1) != 0 ? y : -INFINITY;
+                                }
+                            }
+                        }
+                        bool fresh = false;                 // a row's first keys, or a score far above m
+#pragma unroll
+                        for (int t = 0; t < QT; ++t) {
+                            bm[t] = -INFINITY;
+#pragma unroll
+                            for (int x = 0; x < NS; ++x) bm[t] = fmaxf(bm[t], st[t][x]);
+                            if constexpr (WIDE) {
+                                const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(bm[t]), __float_as_uint(bm[t]), false, false);
+                                bm[t] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * sc;
+                            } else {
+                                bm[t] = max_rows(bm[t]) * sc;
+                            }
+                            fresh |= bm[t] > m[t] + kFar;   // always when m is still -inf
+                        }
+                        weigh(i);
+                        if (finding) {
+#pragma unroll
+                            for (int t = 0; t < QT; ++t) m[t] = fmaxf(m[t], bm[t]);
+                        } else if (__ballot(fresh) != 0 && lane == 0) {
+                            s_new = 1;
+                        }
+                    } else {
+                        const int to = buf + AHEAD >= NB ? buf + AHEAD - NB : buf + AHEAD;
+                        if (i + AHEAD < turns) load(k0 + AHEAD * KS, to);
+                        if (i == 0) continue;
+                        // O^T += C^T P^T of turn i - 1, sixteen keys at a time
+                        const char *const held = s_ring + (buf == 0 ? NB - 1 : buf - 1) * kStage;
+                        const char *const w_at = s_weight[(i - 1) & 1] + l32 * kWeightRow + gh * 16;
+                        constexpr int NV = KS / 16;
+                        u32x4 pb[2][2], vf[2][DT];          // (e4m3: two words of each)
+                        auto read = [&](int v) __attribute__((always_inline)) {
+                            const char *const at = held + v * 16 * RB;
+#pragma unroll
+                            for (int t = 0; t < 2; ++t) pb[v & 1][t] = *reinterpret_cast<const u32x4 *>(w_at + t * (32 * kWeightRow) + v * 32);
+#pragma unroll
+                            for (int dt = 0; dt < DT; ++dt) {
+                                if constexpr (F8) {
+                                    const i32x2 raw = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(at + (v_at ^ (dt % 4 * 32))));
+                                    vf[v & 1][dt][0] = raw[0];
+                                    vf[v & 1][dt][1] = raw[1];
+                                } else {
+                                    const uint32_t here = (v_at ^ (dt % 2 * 64)) + dt / 2 * 128;
+                                    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + here)));
+                                    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 4 * RB + (here ^ 16))));
+                                    vf[v & 1][dt] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                                }
+                            }
+                        };
+                        read(0);
+#pragma unroll
+                        for (int v = 0; v < NV; ++v) {
+                            if (v + 1 < NV) read(v + 1);
+                            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                            for (int dt = 0; dt < DT; ++dt) {
+                                const u32x4 raw = vf[v & 1][dt], c = F8 ? widen(raw[0], raw[1], 1.f) : raw;
+#pragma unroll
+                                for (int t = 0; t < 2; ++t) o[t][dt] = mfma32(c, pb[v & 1][t], o[t][dt]);
+                            }
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+            const bool far = uniform(s_far) != 0;
+            if constexpr (SCORES) {
+#pragma unroll
+                for (int t = 0; t < QT; ++t) {
+                    if constexpr (!WIDE) l[t] += __shfl_xor(l[t], 16);
+                    l[t] += __shfl_xor(l[t], 32);
+                    const int row = rw * 32 + t * QW + ql;
+                    if (kg == 0) {
+                        // (unmasked turns give padding rows some weights)
+                        s_sum[kp][row] = node[t] >= 0 ? l[t] : 0.f;
+                        s_max[kp][row] = node[t] >= 0 || finding ? m[t] : -INFINITY;
+                    }
+                }
+            }
+            __syncthreads();
+            if (!finding && !far) {
+                if constexpr (!SCORES) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const int row = t * 32 + l32, qi = q0 + row;
+                        if (qi < q1)
+                            store_sums<DC, DT>(a, o[t], R0 + qi, pw * (DC / 4) + 4 * gh, cut.pieces, w_.piece, s_max[0][row],
+                                               s_sum[0][row] + s_sum[1][row], pw == 0 && gh == 0);
+                    }
+                }
+                return;
+            }
+            if constexpr (SCORES) {
+                if (finding) {                              // every row's maximum, joined over the parts of the keys
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) {
+                        const int row = rw * 32 + t * QW + ql;
+                        m[t] = fmaxf(s_max[0][row], s_max[1][row]);
+                    }
+                }
+            }
+            if (tid == 0) s_far = 0;                        // (read by all before the barrier above)
+            finding = !finding;
+        }
+    };
+    if (wave < 4) work(std::true_type{});
+    else work(std::false_type{});
 }
 
 // Joins the pieces of the rows that were cut: one wave per row, lane s weighs piece s, then each lane
@@ -478,7 +925,7 @@ __global__ __launch_bounds__(256) void k_latent_join(PagedArgs a) {
     const int rows = a.n_q * a.Hq;
     const int b = quot(a.by_seq_rows, static_cast<uint32_t>(R));
     const int qi = static_cast<int>(R - static_cast<int64_t>(b) * rows);
-    const int tile = 32 * a.row_waves, q0 = qi / tile * tile;
+    const int tile = kFewRows * a.row_waves, q0 = qi / tile * tile;
     float2 ml = a.part_ml[min(lane, a.splits - 1) * rows_all + R];
     const Cut cut = cut_of(a, sequence_of(a, b), q0, min(q0 + tile, rows));
     if (cut.pieces == 1) return;                            // written whole
@@ -512,8 +959,8 @@ __global__ __launch_bounds__(256) void k_latent_join(PagedArgs a) {
 }
 
 template <int DC, bool F8> void run_attention(const PagedArgs &a, unsigned grid, hipStream_t s) {
-    if (a.row_waves == 2) hipLaunchKernelGGL((k_latent_attention<DC, F8, 2>), dim3(grid), dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((k_latent_attention<DC, F8, 1>), dim3(grid), dim3(kThreads), 0, s, a);
+    if (a.row_waves == 2) hipLaunchKernelGGL((k_latent_many<DC, F8>), dim3(grid), dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((k_latent_few<DC, F8>), dim3(grid), dim3(kThreads), 0, s, a);
 }
 
 }  // namespace
@@ -522,8 +969,8 @@ PagedPlan latent_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq) {
     PagedPlan p{1, 1, 0, 1, kMinPieceLatent, static_cast<int64_t>(B) * n_q * Hq, 0};
     const int64_t rows = static_cast<int64_t>(n_q) * Hq;
     if (B <= 0 || rows == 0) return p;
-    p.row_waves = rows <= 32 ? 1 : 2;
-    p.blocks = static_cast<int32_t>((rows + 32 * p.row_waves - 1) / (32 * p.row_waves));
+    p.row_waves = rows <= kFewRows ? 1 : kManyRows / kFewRows;
+    p.blocks = static_cast<int32_t>((rows + kFewRows * p.row_waves - 1) / (kFewRows * p.row_waves));
     const int64_t units = static_cast<int64_t>(B) * p.blocks, room = static_cast<int64_t>(c.max_pages) << c.log_page;
     // a workgroup fills a CU: as many pieces as give each one
     if (units <= kCus / 2)
