@@ -24,6 +24,21 @@ struct LatentAppendArgs {
     FastDiv by_n;              // set by the launch
 };
 
+// An attention call.  A unit is a block of a sequence's rows; units are numbered by sequence.
+struct LatentArgs : PagedArgs {
+    int32_t units, whole;      // units in all, and the first ones, that are not cut
+};
+
+// How a call's units are dealt: rounds of one for every CU, and the rest cut into pieces that fill a last round.
+struct LatentPlan {
+    int32_t rows;              // of a unit, at most
+    int32_t blocks;            // units of a sequence
+    int64_t units, whole;
+    int32_t splits;            // pieces of the units that are cut
+    int64_t grid;              // workgroups
+    int64_t parts;             // rows of pieces: workspace for {max, sum} and sums each
+};
+
 // Query rows of the expanded form, whose keys and values are not paged.
 struct ExpandedArgs {
     const char *q, *k, *v, *k_r;        // bf16
@@ -37,8 +52,8 @@ struct ExpandedArgs {
 
 hipError_t launch_latent_append(LatentAppendArgs a, hipStream_t s);
 hipError_t launch_latent_keep(const KeepArgs &a, hipStream_t s);
-PagedPlan latent_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq);
-hipError_t launch_latent_attention(PagedArgs a, const PagedPlan &p, hipStream_t s);
+LatentPlan latent_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq);
+hipError_t launch_latent_attention(LatentArgs a, const LatentPlan &p, hipStream_t s);
 int64_t expanded_workgroups(int32_t B, int32_t n_q, int32_t H);
 hipError_t launch_expanded_attention(ExpandedArgs a, hipStream_t s);
 

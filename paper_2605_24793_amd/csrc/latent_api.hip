@@ -66,24 +66,21 @@ cospec_status check_attention_sizes(const cospec_latent_cache *c, int32_t B, int
 }
 
 // The pieces' sums, then their {max, weight sum} pairs.
-size_t sums_bytes(const PagedPlan &p, int32_t D) {
-    return round_up(static_cast<size_t>(p.splits) * static_cast<size_t>(p.rows) * static_cast<size_t>(D) * 4);
+size_t sums_bytes(const LatentPlan &p, int32_t D) { return round_up(static_cast<size_t>(p.parts) * static_cast<size_t>(D) * 4); }
+
+size_t plan_bytes(const LatentPlan &p, int32_t D) {
+    return p.parts == 0 ? 0 : sums_bytes(p, D) + round_up(static_cast<size_t>(p.parts) * 8);
 }
 
-size_t plan_bytes(const PagedPlan &p, int32_t D) {
-    if (p.splits < 2) return 0;
-    return sums_bytes(p, D) + round_up(static_cast<size_t>(p.splits) * static_cast<size_t>(p.rows) * 8);
-}
-
-cospec_status attend(PagedArgs &a, const cospec_latent_cache *cache, void *workspace, size_t workspace_bytes,
+cospec_status attend(LatentArgs &a, const cospec_latent_cache *cache, void *workspace, size_t workspace_bytes,
                      hipStream_t stream) {
     const cospec_status st = check_latent(cache);
     if (st != COSPEC_OK) return st;
     if (!given(a.q, 16) || !given(a.out, 16) || !given(a.ctx_len, 4)) return COSPEC_ERR_INVALID_ARG;
     a.c = latent_args(cache);
-    const PagedPlan p = latent_plan(a.c, a.B, a.n_q, a.Hq);
-    if (p.grid > kMaxWorkgroups || (p.rows + 3) / 4 > kMaxWorkgroups) return COSPEC_ERR_UNSUPPORTED;
-    if (p.splits > 1) {
+    const LatentPlan p = latent_plan(a.c, a.B, a.n_q, a.Hq);
+    if (p.grid > kMaxWorkgroups / 2) return COSPEC_ERR_UNSUPPORTED;
+    if (p.parts > 0) {
         if (!given(workspace, kAlign) || workspace_bytes < plan_bytes(p, a.c.D)) return COSPEC_ERR_WORKSPACE;
         a.part_o = static_cast<float *>(workspace);
         a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + sums_bytes(p, a.c.D));
@@ -177,7 +174,7 @@ cospec_status cospec_latent_attention(const void *q, const cospec_latent_cache *
     if (st != COSPEC_OK) return st;
     if (static_cast<int64_t>(B) * n_q == 0) return COSPEC_OK;
     if (!given(q_start, 4)) return COSPEC_ERR_INVALID_ARG;
-    PagedArgs a{};
+    LatentArgs a{};
     a.q = q; a.ctx_len = ctx_len; a.q_start = q_start; a.B = B; a.n_q = n_q; a.Hq = Hq; a.K = K;
     a.scale = scale; a.out = out;
     return attend(a, cache, workspace, workspace_bytes, stream);
@@ -192,7 +189,7 @@ cospec_status cospec_latent_tree_attention(const void *q, const cospec_latent_ca
     if (N > COSPEC_MAX_N) return COSPEC_ERR_UNSUPPORTED;
     if (B == 0) return COSPEC_OK;
     if (!given(parent, 4)) return COSPEC_ERR_INVALID_ARG;
-    PagedArgs a{};
+    LatentArgs a{};
     a.q = q; a.ctx_len = ctx_len; a.parent = parent; a.B = B; a.n_q = N; a.Hq = Hq;
     a.scale = scale; a.out = out;
     return attend(a, cache, workspace, workspace_bytes, stream);

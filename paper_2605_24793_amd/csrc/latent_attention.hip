@@ -21,23 +21,111 @@ constexpr int kRotBytes = kRotated * 2;
 constexpr int kMinPieceLatent = 256;  // keys of a piece, at least
 constexpr float kFar = 60.f;          // log2 units a score may exceed a row's m by (weights and sums are floats)
 
-// 4 bytes per lane into LDS at byte lds + 4 * lane (see load_lds16).
+// 16 (or 4) bytes per lane from base + off[i] + 1024 i, off an offset of the lane's own, into LDS at byte lds + 1024 i +
+// 16 * lane (4 * lane).  A wave that loads while another one multiplies gets its vector instructions into the few
+// cycles between products: so the lanes' offsets are made once, and a turn's addresses are scalar.  (See load_lds16.)
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-__device__ inline void load_lds4(const char *src, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds), "v"(src) : "memory", "m0");
+template <int N> __device__ inline void load_lds_rows(const char *base, const uint32_t *off, uint32_t lds) {
+    if constexpr (N == 1)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1"
+                     : : "s"(lds), "s"(base), "v"(off[0]) : "memory", "m0");
+    else if constexpr (N == 2)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024"
+                     : : "s"(lds), "s"(base), "v"(off[0]), "v"(off[1]) : "memory", "m0");
+    else {
+        static_assert(N % 4 == 0);
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\t"
+                     "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:3072"
+                     : : "s"(lds), "s"(base), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]) : "memory", "m0");
+        if constexpr (N > 4) load_lds_rows<N - 4>(base + 4096, off + 4, lds + 4096);
+    }
+}
+
+__device__ inline void load_lds4(const char *base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %2, %1" : : "s"(lds), "s"(base), "v"(off) : "memory", "m0");
 }
 #pragma clang diagnostic pop
 
-// A latent row of the turn holds its sixteen-byte pieces in another order: piece i at place i ^ turned(key), so that
-// neither product's reads meet in LDS banks: the first one's, eight rows' same piece, and the second one's,
-// which read four rows (bf16) or eight (e4m3) of sixteen components.
-template <bool F8> __device__ inline int turned(int key) { return F8 ? key & 7 : (key & 3) << 1 | (key >> 2 & 1); }
+// A latent's sixteen-byte pieces lie in LDS in another order: piece i at place i ^ turned(key), sixteen at a time, so that
+// neither product's reads meet in the 64 banks: the first one's, sixteen rows' same piece, and the second one's, two
+// pieces of eight rows (e4m3) or four of four (bf16).  Rotated keys, eight pieces each, likewise.
+template <bool F8> __device__ inline int turned(int key) {
+    return F8 ? (key & 7) << 1 | (key >> 3 & 1) : (key & 3) << 2 | (key >> 2 & 3);
+}
+
+__device__ inline int turned_rotated(int key) { return key >> 1 & 7; }
+
+// A wave's part of a turn, SR keys from `first` on (all of one page), on its way into LDS.
+template <int DC, bool F8, int SR> struct TurnLoads {
+    static constexpr int RB = DC * (F8 ? 1 : 2), RPI = 1024 / RB, PPR = RB / 16;   // rows of a load, pieces of a row
+    static constexpr int NC = SR / RPI, NR = SR / 8;        // loads of latents, of rotated keys
+    static constexpr int COUNT = NC + NR + (F8 ? 1 : 0);
+    uint32_t c_off[NC], r_off[NR];
+    int first;
+
+    __device__ inline void begin(int lane, int first_key) {
+        first = first_key;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int row = lane / PPR;
+            c_off[i] = row * RB + ((lane % PPR) ^ turned<F8>(first + i * RPI + row)) * 16;
+        }
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int row = lane / 8;
+            r_off[i] = row * kRotBytes + ((lane % 8) ^ turned_rotated(first + i * 8 + row)) * 16;
+        }
+    }
+    // The page of a turn's keys, or page 0 (what is no key of the sequence is not used).
+    __device__ inline uint32_t page(const PageArgs &c, const int32_t *row, int k0, int kend) const {
+        const uint32_t id = scalar_load(row + (min(k0 + first, kend - 1) >> c.log_page));
+        return id < static_cast<uint32_t>(c.n_pages) ? id : 0u;
+    }
+    __device__ inline void load(const PageArgs &c, uint32_t page, int k0, uint32_t stage, int rot_at, int scale_at, int lane) const {
+        const int64_t place = (static_cast<int64_t>(page) << c.log_page) + ((k0 + first) & ((1 << c.log_page) - 1));
+        load_lds_rows<NC>(c.k + place * RB, c_off, stage + first * RB);
+        load_lds_rows<NR>(c.v + place * kRotBytes, r_off, stage + rot_at + first * kRotBytes);
+        if (F8 && lane < SR) load_lds4(reinterpret_cast<const char *>(c.k_scale + place), lane * 4, stage + scale_at + first * 4);
+    }
+};
+
+// Which unit a workgroup takes, and which piece of its keys.  Whole units come first.  Workgroups are dealt to the
+// XCDs round-robin: each XCD takes consecutive units, which are blocks of the same sequences and read the
+// same keys from its L2; a sequence's last rows, which see the most keys, come first.
+struct Unit {
+    int b, block, piece;
+    int cut;                   // among the units that are cut, or -1: whole
+};
+
+__device__ inline Unit unit_at(const LatentArgs &a, int u, int piece, int cut) {
+    const int b = quot(a.by_blocks, u);
+    return Unit{b, static_cast<int>(a.by_blocks.d) - 1 - (u - b * static_cast<int>(a.by_blocks.d)), piece, cut};
+}
+
+__device__ inline Unit unit_of_workgroup(const LatentArgs &a) {
+    const int w = blockIdx.x;
+    if (w < a.whole) return unit_at(a, w % kXcds * (a.whole / kXcds) + w / kXcds, 0, -1);
+    const int cut = quot(a.by_splits, w - a.whole), piece = w - a.whole - cut * a.splits;
+    return unit_at(a, a.whole + cut, piece, a.splits > 1 ? cut : -1);
+}
+
+__device__ inline Cut cut_of_unit(const LatentArgs &a, const Unit &u, const Seq &s, int q0, int q1) {
+    Cut c = cut_of(a, s, q0, q1);
+    if (u.cut < 0) c.chunk = c.kend, c.pieces = 1;
+    return c;
+}
+
+// The workspace's row of a unit's row, in its piece.
+__device__ inline int64_t part_row(const LatentArgs &a, const Unit &u, int row, int rows) {
+    return (static_cast<int64_t>(u.cut) * a.splits + u.piece) * rows + row;
+}
 
 // A lane's part of row R's sums: tile dt, elements 4e .. 4e + 3 are the components d0 + 32 dt + 8 e + 0..3.  Whole
-// rows are divided by the weights' sum L, pieces stored as they are, with {m, L} by one lane (`first`).
+// rows are divided by the weights' sum L; pieces are stored as they are at row `at` of the workspace, with {m, L} by one
+// lane (`first`).
 template <int DC, int DT>
-__device__ inline void store_sums(const PagedArgs &a, const floatx16 (&o)[DT], int64_t R, int d0, int pieces, int piece,
+__device__ inline void store_sums(const LatentArgs &a, const floatx16 (&o)[DT], int64_t R, int d0, int pieces, int64_t at,
                                   float m, float L, bool first) {
     if (pieces == 1) {
         const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;   // NaN stays
@@ -52,7 +140,6 @@ __device__ inline void store_sums(const PagedArgs &a, const floatx16 (&o)[DT], i
                 *reinterpret_cast<u32x2 *>(dst + (32 * dt + 8 * e) * 2) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
             }
     } else {
-        const int64_t at = piece * (static_cast<int64_t>(a.B) * a.n_q * a.Hq) + R;
         float *po = a.part_o + at * DC + d0;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
@@ -110,19 +197,19 @@ __device__ inline void clean_turn(char *stage, float *scales, uint32_t *bad, int
 // sums (the rest of the pass that finds it is for nothing: nothing else may leave the loop, or the compiler
 // keeps the sums twice).
 template <int DC, bool F8>
-__global__ __launch_bounds__(kThreads, 1) void k_latent_few(PagedArgs a) {
+__global__ __launch_bounds__(kThreads, 1) void k_latent_few(LatentArgs a) {
     constexpr int EB = F8 ? 1 : 2, RB = DC * EB;            // bytes of a latent
     constexpr int ROWS = kFewRows, NW = kWaves, T = kThreads;
     constexpr int KP = 4, TK = kKeys / KP;                  // parts of a turn's keys among the waves' scores, and their keys
     constexpr int CS = DC / 32, RS = kRotated / 32;         // k-steps of the first product, of latents and of rotated keys
     constexpr int DT = DC / NW / 32;                        // component tiles of a wave
     constexpr int kRotAt = kKeys * RB, kScaleAt = kRotAt + kKeys * kRotBytes, kStage = kScaleAt + (F8 ? kKeys * 4 : 0);
-    constexpr int RPI = 1024 / RB, PPR = RB / 16;           // rows of a load, pieces of a row
+    constexpr int PPR = RB / 16;                            // pieces of a row
     constexpr int kWeightRow = kKeys * 2 + 16;              // bytes
     constexpr int NB = kStage > 48 * 1024 ? 2 : 3;          // turns in LDS: the one worked on, and those on their way
     constexpr int SR = kKeys / NW;                          // keys that a wave loads
-    constexpr int LPT = SR / RPI + SR / 8 + (F8 ? 1 : 0);   // loads of a wave's part of a turn
-    __shared__ __attribute__((aligned(128))) char s_ring[NB * kStage];
+    constexpr int LPT = TurnLoads<DC, F8, SR>::COUNT;       // loads of a wave's part of a turn
+    __shared__ __attribute__((aligned(256))) char s_ring[NB * kStage];
     __shared__ __attribute__((aligned(16))) char s_weight[ROWS * kWeightRow];
     __shared__ uint32_t s_page[kThreads];
     __shared__ uint32_t s_seen[ROWS][8];                    // ancestors of the rows' nodes
@@ -136,11 +223,10 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(PagedArgs a) {
     const int ql = lane & 15, kg = lane >> 4;               // of the first product: query, k-piece
     const int kp = wave;
     const int rows = a.n_q * a.Hq;
-    const Place w_ = place_of(a);
+    const Unit w_ = unit_of_workgroup(a);
     const int b = w_.b;
-    if (b >= a.B) return;
     const int q0 = w_.block * ROWS, q1 = min(q0 + ROWS, rows);
-    uint32_t id = a.splits == 1 ? table_entry(a, b, 0) : 0u;
+    uint32_t id = w_.cut < 0 ? table_entry(a, b, 0) : 0u;
     const int64_t R0 = static_cast<int64_t>(b) * rows;
     u32x4 qf[2][CS + RS];                                   // of the wave's two query tiles
     int node[2];
@@ -159,35 +245,19 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(PagedArgs a) {
         for (int c = 0; c < RS; ++c) qf[t][CS + c] = *reinterpret_cast<const u32x4 *>(qrow + (DC + c * 32 + kg * 8) * 2);
     }
     const Seq s = sequence_of(a, b);
-    const Cut cut = cut_of(a, s, q0, q1);
+    const Cut cut = cut_of_unit(a, w_, s, q0, q1);
     if (w_.piece >= cut.pieces) return;
     const int kbeg = w_.piece * cut.chunk, kend = min(kbeg + cut.chunk, cut.kend);
     const int all_see = seen_by_all(a, s, q0, kend);        // keys below are seen by every row that sees any
 
-    const int P1 = (1 << a.c.log_page) - 1;
     int first_page = 0, last_page = 0;                      // of those in LDS
     bool any_none = false;
     const uint32_t ring = uniform(lds_address(s_ring));
     auto page_of = [&](int key) { return s_page[min(key >> a.c.log_page, last_page) - first_page]; };
-    // this wave's keys of a turn (all of one page), into LDS
-    auto load = [&](int k0, uint32_t stage) {
-        const int key = k0 + wave * SR;
-        const int64_t page = uniform(page_of(key) & ~kNone);
-        const int64_t place = (page << a.c.log_page) + (key & P1);
-        const char *c = a.c.k + place * RB, *rot = a.c.v + place * kRotBytes;
-        const uint32_t at = stage + wave * (SR * RB);
-#pragma unroll
-        for (int i = 0; i < SR / RPI; ++i) {
-            const int row = i * RPI + lane / PPR;           // (a wave's first key is a multiple of eight)
-            load_lds16<false>(c + row * RB + ((lane % PPR) ^ turned<F8>(row)) * 16, at + i * 1024);
-        }
-#pragma unroll
-        for (int i = 0; i < SR / 8; ++i) {
-            const int row = i * 8 + lane / 8;
-            load_lds16<false>(rot + row * kRotBytes + ((lane % 8) ^ (row & 7)) * 16, stage + kRotAt + wave * (SR * kRotBytes) + i * 1024);
-        }
-        if (F8 && lane < SR) load_lds4(reinterpret_cast<const char *>(a.c.k_scale + place + lane), stage + kScaleAt + wave * (SR * 4));
-    };
+    const int32_t *const pages = a.c.table + static_cast<int64_t>(b) * a.c.max_pages;
+    TurnLoads<DC, F8, SR> loads;
+    loads.begin(lane, wave * SR);
+    auto load = [&](int k0, uint32_t stage) { loads.load(a.c, loads.page(a.c, pages, k0, kend), k0, stage, kRotAt, kScaleAt, lane); };
     auto look_up = [&](int from, int to, uint32_t entry) {  // of keys [from, to), this thread's table entry given
         first_page = from >> a.c.log_page;
         last_page = (to - 1) >> a.c.log_page;
@@ -225,13 +295,13 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(PagedArgs a) {
 
     // where this lane reads: keys' pieces, rotated keys' pieces, latents' components, weights
     const int krow = kp * TK + ql;
-    const uint32_t k_at = krow * RB + ((kg ^ turned<F8>(ql)) & 7) * 16;
-    const uint32_t r_at = kRotAt + krow * kRotBytes + ((kg ^ ql) & 7) * 16;
+    const uint32_t k_at = krow * RB + (kg ^ turned<F8>(krow)) * 16;
+    const uint32_t r_at = kRotAt + krow * kRotBytes + (kg ^ turned_rotated(krow)) * 16;
     uint32_t v_at;
     {
         const int j = lane & 15, cg = lane >> 4 & 1, row = 8 * gh + (F8 ? j >> 1 : j >> 2);
         const int piece = wave * (PPR / NW) + (F8 ? cg : 2 * cg + (j >> 1 & 1));
-        v_at = row * RB + (piece >> 3) * 128 + ((piece ^ turned<F8>(row)) & 7) * 16 + (j & 1) * 8;
+        v_at = row * RB + (piece >> 4) * 256 + ((piece ^ turned<F8>(row)) & 15) * 16 + (j & 1) * 8;
     }
     const char *const w_at = s_weight + l32 * kWeightRow + gh * 16;
 
@@ -249,7 +319,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(PagedArgs a) {
         for (int t = 0; t < 2; ++t) l[t] = 0.f;
         for (int seg = kbeg; seg < kend; seg += segment) {
             const int seg_end = min(seg + segment, kend);
-            if (seg > kbeg || a.splits > 1 || again) id = table_entry(a, b, seg >> a.c.log_page);
+            if (seg > kbeg || w_.cut >= 0 || again) id = table_entry(a, b, seg >> a.c.log_page);
             if (seg > kbeg) __syncthreads();                // the pages of the segment before are used up
             look_up(seg, seg_end, id);
             load(seg, ring);
@@ -282,7 +352,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(PagedArgs a) {
 #pragma unroll
                     for (int i = 0; i < G; ++i) {
                         const int c = g * G + i;
-                        kf[g & 1][i] = *reinterpret_cast<const u32x4 *>(stage + (k_at ^ (c % 2 * 64)) + c / 2 * 128);
+                        kf[g & 1][i] = *reinterpret_cast<const u32x4 *>(stage + (k_at ^ (c % 4 * 64)) + c / 4 * 256);
                     }
                 };
                 auto read_rotated = [&]() __attribute__((always_inline)) {
@@ -330,11 +400,11 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(PagedArgs a) {
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) {
                         if constexpr (F8) {
-                            const i32x2 raw = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(at + (v_at ^ (dt % 4 * 32))));
+                            const i32x2 raw = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(at + (v_at ^ (dt * 32))));
                             vf[v & 1][dt][0] = raw[0];
                             vf[v & 1][dt][1] = raw[1];
                         } else {
-                            const uint32_t here = (v_at ^ (dt % 2 * 64)) + dt / 2 * 128;
+                            const uint32_t here = v_at ^ (dt * 64);
                             const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + here)));
                             const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 4 * RB + (here ^ 16))));
                             vf[v & 1][dt] = u32x4{lo[0], lo[1], hi[0], hi[1]};
@@ -467,7 +537,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(PagedArgs a) {
             float L = 0.f;
 #pragma unroll
             for (int i = 0; i < KP; ++i) L += s_sum[i][l32];
-            store_sums<DC, DT>(a, o, R0 + qi, wave * (DC / NW) + 4 * gh, cut.pieces, w_.piece, s_max[0][l32], L, wave == 0 && gh == 0);
+            store_sums<DC, DT>(a, o, R0 + qi, wave * (DC / NW) + 4 * gh, cut.pieces, part_row(a, w_, l32, ROWS), s_max[0][l32], L, wave == 0 && gh == 0);
             return;
         }
         if (finding) {                                      // every row's maximum, joined over the parts of the keys
@@ -501,7 +571,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(PagedArgs a) {
 // After barrier i turn i is staged and turn i - 1 weighed: the scores' waves take turn i, the sums' waves turn
 // i - 1, and load ahead.  Rows' maxima as in k_latent_few.
 template <int DC, bool F8>
-__global__ __launch_bounds__(512, 1) void k_latent_many(PagedArgs a) {
+__global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
     constexpr int EB = F8 ? 1 : 2, RB = DC * EB;            // bytes of a latent
     constexpr int KS = RB > 512 ? 32 : 64;                  // keys of a turn
     constexpr bool WIDE = KS == 64;
@@ -513,12 +583,12 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(PagedArgs a) {
     constexpr int DT = DC / 4 / 32;                         // component tiles of a sums' wave
     constexpr int kRotAt = KS * RB, kScaleAt = kRotAt + KS * kRotBytes, kStage = kScaleAt + (F8 ? KS * 4 : 0);
     constexpr int NB = RB > 512 ? 4 : 3, AHEAD = NB - 2;    // turns in LDS, and on their way
-    constexpr int RPI = 1024 / RB, PPR = RB / 16;           // rows of a load, pieces of a row
+    constexpr int PPR = RB / 16;                            // pieces of a row
     constexpr int SR = KS / 4;                              // keys that a sums' wave loads
-    constexpr int LPT = SR / RPI + SR / 8 + (F8 ? 1 : 0);   // its loads of a turn
+    constexpr int LPT = TurnLoads<DC, F8, SR>::COUNT;       // its loads of a turn
     constexpr int kWeightRow = KS * 2 + 16;                 // bytes
     constexpr int ROWS = kManyRows;
-    __shared__ __attribute__((aligned(128))) char s_ring[NB * kStage];
+    __shared__ __attribute__((aligned(256))) char s_ring[NB * kStage];
     __shared__ __attribute__((aligned(16))) char s_weight[2][ROWS * kWeightRow];
     __shared__ uint32_t s_page[kThreads];
     __shared__ uint32_t s_seen[ROWS][8];                    // ancestors of the rows' nodes
@@ -530,13 +600,12 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(PagedArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int gh = lane >> 5, l32 = lane & 31;
     const int rows = a.n_q * a.Hq;
-    const Place w_ = place_of(a);
+    const Unit w_ = unit_of_workgroup(a);
     const int b = w_.b;
-    if (b >= a.B) return;
     const int q0 = w_.block * ROWS, q1 = min(q0 + ROWS, rows);
     const int64_t R0 = static_cast<int64_t>(b) * rows;
     const Seq s = sequence_of(a, b);
-    const Cut cut = cut_of(a, s, q0, q1);
+    const Cut cut = cut_of_unit(a, w_, s, q0, q1);
     if (w_.piece >= cut.pieces) return;
     const int kbeg = w_.piece * cut.chunk, kend = min(kbeg + cut.chunk, cut.kend);
     const int all_see = seen_by_all(a, s, q0, kend);        // keys below are seen by every row that sees any
@@ -548,7 +617,6 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(PagedArgs a) {
     }
     if (tid == 0) s_new = s_far = 0;
 
-    const int P1 = (1 << a.c.log_page) - 1;
     const int segment = kSegment << a.c.log_page;
     const uint32_t ring = uniform(lds_address(s_ring));
     const float sc = fmaxf(fabsf(a.scale) * kLog2eP, 1.17549435e-38f);
@@ -562,8 +630,9 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(PagedArgs a) {
         [[maybe_unused]] u32x4 qf[QT][CS + RS];
         [[maybe_unused]] int node[QT], vis[QT];             // keys [0, vis) are seen
         [[maybe_unused]] float m[QT];
-        [[maybe_unused]] const uint32_t k_at = (kp * TK + ql) * RB + ((kg ^ turned<F8>(ql)) & 7) * 16;
-        [[maybe_unused]] const uint32_t r_at = kRotAt + (kp * TK + ql) * kRotBytes + ((kg ^ ql) & 7) * 16;
+        const int krow = kp * TK + ql;
+        [[maybe_unused]] const uint32_t k_at = krow * RB + (kg ^ turned<F8>(krow)) * 16;
+        [[maybe_unused]] const uint32_t r_at = kRotAt + krow * kRotBytes + (kg ^ turned_rotated(krow)) * 16;
         if constexpr (SCORES) {
             const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;   // scores as |scale| (+-q) . k: the largest product is the largest
 #pragma unroll
@@ -591,29 +660,16 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(PagedArgs a) {
         if constexpr (!SCORES) {
             const int j = lane & 15, cg = lane >> 4 & 1, row = 8 * gh + (F8 ? j >> 1 : j >> 2);
             const int piece = pw * (PPR / 4) + (F8 ? cg : 2 * cg + (j >> 1 & 1));
-            v_at = row * RB + (piece >> 3) * 128 + ((piece ^ turned<F8>(row)) & 7) * 16 + (j & 1) * 8;
+            v_at = row * RB + (piece >> 4) * 256 + ((piece ^ turned<F8>(row)) & 15) * 16 + (j & 1) * 8;
         }
         int first_page = 0, last_page = 0;                  // of those in LDS
         bool any_none = false;
         auto page_of = [&](int key) { return s_page[min(key >> a.c.log_page, last_page) - first_page]; };
-        // this wave's keys of a turn (all of one page), into LDS
-        [[maybe_unused]] auto load = [&](int k0, int buf) {
-            const uint32_t stage = ring + buf * kStage;
-            const int key = k0 + pw * SR;
-            const int64_t page = uniform(page_of(key) & ~kNone);
-            const int64_t place = (page << a.c.log_page) + (key & P1);
-            const char *c = a.c.k + place * RB, *rot = a.c.v + place * kRotBytes;
-#pragma unroll
-            for (int i = 0; i < SR / RPI; ++i) {
-                const int row = i * RPI + lane / PPR;       // (a wave's first key is a multiple of eight)
-                load_lds16<false>(c + row * RB + ((lane % PPR) ^ turned<F8>(row)) * 16, stage + pw * (SR * RB) + i * 1024);
-            }
-#pragma unroll
-            for (int i = 0; i < SR / 8; ++i) {
-                const int row = i * 8 + lane / 8;
-                load_lds16<false>(rot + row * kRotBytes + ((lane % 8) ^ (row & 7)) * 16, stage + kRotAt + pw * (SR * kRotBytes) + i * 1024);
-            }
-            if (F8 && lane < SR) load_lds4(reinterpret_cast<const char *>(a.c.k_scale + place + lane), stage + kScaleAt + pw * (SR * 4));
+        const int32_t *const pages = a.c.table + static_cast<int64_t>(b) * a.c.max_pages;
+        [[maybe_unused]] TurnLoads<DC, F8, SR> loads;
+        if constexpr (!SCORES) loads.begin(lane, pw * SR);
+        [[maybe_unused]] auto load = [&](uint32_t page, int k0, int buf) {
+            loads.load(a.c, page, k0, ring + buf * kStage, kRotAt, kScaleAt, lane);
         };
 
         // Once, unless a score lies far above its row's m: then once more for the maxima alone, and again for the sums.
@@ -647,10 +703,12 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(PagedArgs a) {
                 }
                 __syncthreads();
                 any_none = uniform(s_none) != 0;
+                [[maybe_unused]] uint32_t next = 0;         // the page that is loaded from next
                 if constexpr (!SCORES) {
 #pragma unroll
                     for (int i = 0; i < AHEAD; ++i)
-                        if (i < turns) load(seg + i * KS, i);
+                        if (i < turns) load(loads.page(a.c, pages, seg + i * KS, kend), seg + i * KS, i);
+                    next = loads.page(a.c, pages, seg + AHEAD * KS, kend);
                 }
                 [[maybe_unused]] typename std::conditional<WIDE, floatx16, floatx4>::type st[QT];
                 [[maybe_unused]] float sv[F8 ? NS : 1];     // scales of this lane's keys
@@ -724,7 +782,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(PagedArgs a) {
                         }
                         if (i == turns) break;
                         // S^T.  Operands are read from LDS a group ahead of the products that take them.
-                        constexpr int LP = WIDE ? 2 : 4, PER = 8 / LP;   // pieces of a key that a load's lanes take side by side
+                        constexpr int LP = WIDE ? 2 : 4, PER = 16 / LP;  // pieces of a key that a load's lanes take side by side
                         constexpr int LOADS = CS / (F8 ? 2 : 1), G = F8 ? 2 : 4, NG = LOADS / G;
 #pragma unroll
                         for (int t = 0; t < QT; ++t)
@@ -735,7 +793,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(PagedArgs a) {
 #pragma unroll
                             for (int x = 0; x < G; ++x) {
                                 const int c = g * G + x;
-                                kf[g & 1][x] = *reinterpret_cast<const u32x4 *>(stage + (k_at ^ (c % PER * LP * 16)) + c / PER * 128);
+                                kf[g & 1][x] = *reinterpret_cast<const u32x4 *>(stage + (k_at ^ (c % PER * LP * 16)) + c / PER * 256);
                             }
                         };
                         auto multiply = [&](u32x4 k, int c) __attribute__((always_inline)) {
@@ -827,7 +885,8 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(PagedArgs a) {
                         }
                     } else {
                         const int to = buf + AHEAD >= NB ? buf + AHEAD - NB : buf + AHEAD;
-                        if (i + AHEAD < turns) load(k0 + AHEAD * KS, to);
+                        if (i + AHEAD < turns) load(next, k0 + AHEAD * KS, to);
+                        next = loads.page(a.c, pages, k0 + (AHEAD + 1) * KS, kend);
                         if (i == 0) continue;
                         // O^T += C^T P^T of turn i - 1, sixteen keys at a time
                         const char *const held = s_ring + (buf == 0 ? NB - 1 : buf - 1) * kStage;
@@ -841,11 +900,11 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(PagedArgs a) {
 #pragma unroll
                             for (int dt = 0; dt < DT; ++dt) {
                                 if constexpr (F8) {
-                                    const i32x2 raw = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(at + (v_at ^ (dt % 4 * 32))));
+                                    const i32x2 raw = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(at + (v_at ^ (dt * 32))));
                                     vf[v & 1][dt][0] = raw[0];
                                     vf[v & 1][dt][1] = raw[1];
                                 } else {
-                                    const uint32_t here = (v_at ^ (dt % 2 * 64)) + dt / 2 * 128;
+                                    const uint32_t here = v_at ^ (dt * 64);
                                     const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + here)));
                                     const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 4 * RB + (here ^ 16))));
                                     vf[v & 1][dt] = u32x4{lo[0], lo[1], hi[0], hi[1]};
@@ -890,7 +949,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(PagedArgs a) {
                     for (int t = 0; t < 2; ++t) {
                         const int row = t * 32 + l32, qi = q0 + row;
                         if (qi < q1)
-                            store_sums<DC, DT>(a, o[t], R0 + qi, pw * (DC / 4) + 4 * gh, cut.pieces, w_.piece, s_max[0][row],
+                            store_sums<DC, DT>(a, o[t], R0 + qi, pw * (DC / 4) + 4 * gh, cut.pieces, part_row(a, w_, row, ROWS), s_max[0][row],
                                                s_sum[0][row] + s_sum[1][row], pw == 0 && gh == 0);
                     }
                 }
@@ -913,23 +972,23 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(PagedArgs a) {
     else work(std::false_type{});
 }
 
-// Joins the pieces of the rows that were cut: one wave per row, lane s weighs piece s, then each lane
+// Joins the pieces of the units that were cut: one wave per row, lane s weighs piece s, then each lane
 // takes DC / 64 components of every piece.
 template <int DC>
-__global__ __launch_bounds__(256) void k_latent_join(PagedArgs a) {
+__global__ __launch_bounds__(256) void k_latent_join(LatentArgs a) {
     constexpr int EACH = DC / 256;                          // four components at a time
     const int lane = threadIdx.x & 63;
-    const int64_t rows_all = static_cast<int64_t>(a.B) * a.n_q * a.Hq;
-    const int64_t R = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (R >= rows_all) return;
-    const int rows = a.n_q * a.Hq;
-    const int b = quot(a.by_seq_rows, static_cast<uint32_t>(R));
-    const int qi = static_cast<int>(R - static_cast<int64_t>(b) * rows);
-    const int tile = kFewRows * a.row_waves, q0 = qi / tile * tile;
-    float2 ml = a.part_ml[min(lane, a.splits - 1) * rows_all + R];
-    const Cut cut = cut_of(a, sequence_of(a, b), q0, min(q0 + tile, rows));
-    if (cut.pieces == 1) return;                            // written whole
-    const int n = cut.pieces;
+    const int rows = a.n_q * a.Hq, unit_rows = a.row_tiles;
+    const int x = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int cut = x / unit_rows, row = x - cut * unit_rows;   // (a power of two)
+    const Unit u = unit_at(a, a.whole + cut, 0, cut);
+    const int q0 = u.block * unit_rows, q1 = min(q0 + unit_rows, rows);
+    if (q0 + row >= q1) return;
+    const int64_t R = static_cast<int64_t>(u.b) * rows + q0 + row, at = part_row(a, u, row, unit_rows);
+    float2 ml = a.part_ml[at + static_cast<int64_t>(min(lane, a.splits - 1)) * unit_rows];
+    const Cut c = cut_of(a, sequence_of(a, u.b), q0, q1);
+    if (c.pieces == 1) return;                              // written whole
+    const int n = c.pieces;
     if (lane >= n) ml = make_float2(-INFINITY, 0.f);
     float M = ml.x;
 #pragma unroll
@@ -946,7 +1005,7 @@ __global__ __launch_bounds__(256) void k_latent_join(PagedArgs a) {
         const bool none = __shfl(ml.x, p) == -INFINITY;     // (its sums may be anything)
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
-            const floatx4 v = *(reinterpret_cast<const floatx4 *>(a.part_o + (p * rows_all + R) * DC) + e * 64 + lane);
+            const floatx4 v = *(reinterpret_cast<const floatx4 *>(a.part_o + (at + static_cast<int64_t>(p) * unit_rows) * DC) + e * 64 + lane);
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[e][i] = none ? acc[e][i] : fmaf(wp, v[i], acc[e][i]);
         }
@@ -958,44 +1017,45 @@ __global__ __launch_bounds__(256) void k_latent_join(PagedArgs a) {
             u32x2{bf16_pair(acc[e][0] * inv, acc[e][1] * inv), bf16_pair(acc[e][2] * inv, acc[e][3] * inv)};
 }
 
-template <int DC, bool F8> void run_attention(const PagedArgs &a, unsigned grid, hipStream_t s) {
-    if (a.row_waves == 2) hipLaunchKernelGGL((k_latent_many<DC, F8>), dim3(grid), dim3(512), 0, s, a);
+template <int DC, bool F8> void run_attention(const LatentArgs &a, unsigned grid, hipStream_t s) {
+    if (a.row_tiles == kManyRows) hipLaunchKernelGGL((k_latent_many<DC, F8>), dim3(grid), dim3(512), 0, s, a);
     else hipLaunchKernelGGL((k_latent_few<DC, F8>), dim3(grid), dim3(kThreads), 0, s, a);
 }
 
 }  // namespace
 
-PagedPlan latent_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq) {
-    PagedPlan p{1, 1, 0, 1, kMinPieceLatent, static_cast<int64_t>(B) * n_q * Hq, 0};
+LatentPlan latent_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq) {
+    LatentPlan p{};
+    p.splits = 1;
     const int64_t rows = static_cast<int64_t>(n_q) * Hq;
     if (B <= 0 || rows == 0) return p;
-    p.row_waves = rows <= kFewRows ? 1 : kManyRows / kFewRows;
-    p.blocks = static_cast<int32_t>((rows + kFewRows * p.row_waves - 1) / (kFewRows * p.row_waves));
-    const int64_t units = static_cast<int64_t>(B) * p.blocks, room = static_cast<int64_t>(c.max_pages) << c.log_page;
-    // a workgroup fills a CU: as many pieces as give each one
-    if (units <= kCus / 2)
-        p.splits = static_cast<int32_t>(std::max<int64_t>(
-            std::min({kCus / units, (room + p.min_piece - 1) / p.min_piece, kMaxPieces}), 1));
-    p.grid = (static_cast<int64_t>(B) * p.splits + kXcds - 1) / kXcds * kXcds * p.blocks;     // each XCD takes as many
+    p.rows = rows <= kFewRows ? kFewRows : kManyRows;
+    p.blocks = static_cast<int32_t>((rows + p.rows - 1) / p.rows);
+    p.units = static_cast<int64_t>(B) * p.blocks;
+    // A workgroup fills a CU, so units come in rounds of one for each; what is left over is cut into pieces that fill
+    // the CUs once.
+    p.whole = p.units / kCus * kCus;
+    const int64_t left = p.units - p.whole, room = static_cast<int64_t>(c.max_pages) << c.log_page;
+    if (left > 0) p.splits = static_cast<int32_t>(std::max<int64_t>(std::min({kCus / left, (room + kMinPieceLatent - 1) / kMinPieceLatent, kMaxPieces}), 1));
+    p.grid = p.whole + left * p.splits;
+    p.parts = p.splits > 1 ? left * p.splits * p.rows : 0;
     return p;
 }
 
-hipError_t launch_latent_attention(PagedArgs a, const PagedPlan &p, hipStream_t s) {
-    a.row_tiles = p.row_tiles;
-    a.row_waves = p.row_waves;
+hipError_t launch_latent_attention(LatentArgs a, const LatentPlan &p, hipStream_t s) {
+    a.row_tiles = p.rows;
     a.splits = p.splits;
-    a.min_piece = p.min_piece;
+    a.min_piece = kMinPieceLatent;
+    a.units = static_cast<int32_t>(p.units);
+    a.whole = static_cast<int32_t>(p.whole);
     a.by_grp = fast_div(a.Hq);
     a.by_blocks = fast_div(p.blocks);
-    a.by_heads = fast_div(1);
     a.by_splits = fast_div(p.splits);
-    a.by_seq_rows = fast_div(static_cast<uint32_t>(a.n_q) * static_cast<uint32_t>(a.Hq));
-    a.by_hq = fast_div(a.Hq);
     const unsigned grid = static_cast<unsigned>(p.grid);
     if (a.c.D == 512) a.c.f8 ? run_attention<512, true>(a, grid, s) : run_attention<512, false>(a, grid, s);
     else a.c.f8 ? run_attention<256, true>(a, grid, s) : run_attention<256, false>(a, grid, s);
     if (p.splits > 1) {
-        const dim3 jgrid(static_cast<unsigned>((p.rows + 3) / 4));
+        const dim3 jgrid(static_cast<unsigned>((p.units - p.whole) * p.rows / 4));
         if (a.c.D == 512) hipLaunchKernelGGL(k_latent_join<512>, jgrid, dim3(256), 0, s, a);
         else hipLaunchKernelGGL(k_latent_join<256>, jgrid, dim3(256), 0, s, a);
     }
