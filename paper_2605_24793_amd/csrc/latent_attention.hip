@@ -559,6 +559,34 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(LatentArgs a) {
     }
 }
 
+// A workgroup's queries (64 rows that lie one after the other in memory) on their way into LDS, by T threads: a lane of a
+// product reads a row's pieces, which from memory would take a line for each.  Piece p of row r lies at place
+// p ^ turned_rotated(r) of its eight.
+template <int DC, int T> __device__ inline void load_queries(const char *rows_at, int rows, uint32_t to, int wave, int lane) {
+    constexpr int QB = (DC + kRotated) * 2, PQ = QB / 16, N = kManyRows * QB / 1024 / (T / 64);
+    static_assert(kManyRows * QB % (1024 * (T / 64)) == 0 && PQ % 8 == 0 && QB % 256 == 128);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int at = (wave * N + i) * 64 + lane, r = at / PQ, p = (at - r * PQ) ^ turned_rotated(r);
+        load_lds16<false>(rows_at + static_cast<int64_t>(min(r, rows - 1)) * QB + p * 16, to + (wave * N + i) * 1024);
+    }
+}
+
+template <int DC> __device__ inline u32x4 query_piece(const char *queries, int row, int piece) {
+    constexpr int QB = (DC + kRotated) * 2;
+    return *reinterpret_cast<const u32x4 *>(queries + row * QB + (piece ^ turned_rotated(row)) * 16);
+}
+
+// Rows in LDS, `stride` bytes apart, to memory at `to`, where they lie one after the other.
+template <int ROW_BYTES, int T> __device__ inline void store_rows(const char *from, int stride, int rows, char *to, int tid) {
+    constexpr int PR = ROW_BYTES / 16;
+    asm volatile("" : "+v"(tid));                           // (addresses are found here, and not kept through the loop before)
+    for (int i = tid; i < rows * PR; i += T) {
+        const int r = i / PR, p = i % PR;
+        *reinterpret_cast<u32x4 *>(to + static_cast<int64_t>(i) * 16) = *reinterpret_cast<const u32x4 *>(from + r * stride + p * 16);
+    }
+}
+
 // More rows: 64 of them a workgroup, with four waves for the scores and four for the sums, one of each on a SIMD.
 // While the latter add up one turn, the former work on the next, so that the matrix cores are fed by one wave while the
 // other is at its exponentials, conversions or waits.  (One wave for both leaves them idle then: a lone wave
@@ -604,9 +632,16 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
     const int b = w_.b;
     const int q0 = w_.block * ROWS, q1 = min(q0 + ROWS, rows);
     const int64_t R0 = static_cast<int64_t>(b) * rows;
+    // the queries go behind the turns that are loaded before they are read
+    char *const s_q = s_ring + AHEAD * kStage;
+    static_assert(AHEAD * kStage + ROWS * (DC + kRotated) * 2 <= NB * kStage);
+    load_queries<DC, 512>(static_cast<const char *>(a.q) + (R0 + q0) * ((DC + kRotated) * 2), q1 - q0, uniform(lds_address(s_q)), wave, lane);
     const Seq s = sequence_of(a, b);
     const Cut cut = cut_of_unit(a, w_, s, q0, q1);
-    if (w_.piece >= cut.pieces) return;
+    if (w_.piece >= cut.pieces) {
+        wait_vm<0>();                                       // (nothing may come into LDS that is another's then)
+        return;
+    }
     const int kbeg = w_.piece * cut.chunk, kend = min(kbeg + cut.chunk, cut.kend);
     const int all_see = seen_by_all(a, s, q0, kend);        // keys below are seen by every row that sees any
     if (a.parent) {
@@ -616,6 +651,8 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
         __syncthreads();
     }
     if (tid == 0) s_new = s_far = 0;
+    wait_vm<0>();
+    __syncthreads();                                        // the queries are there
 
     const int segment = kSegment << a.c.log_page;
     const uint32_t ring = uniform(lds_address(s_ring));
@@ -639,7 +676,6 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
             for (int t = 0; t < QT; ++t) {
                 const int row = q0 + rw * 32 + t * 16 + ql, qi = min(row, q1 - 1);
                 node[t] = quot(a.by_grp, qi);
-                const char *qrow = static_cast<const char *>(a.q) + (R0 + qi) * ((DC + kRotated) * 2);
                 const int64_t p = s.qs + node[t];
                 const bool live = row < q1 && p >= 0 && p < s.end;
                 vis[t] = !live ? 0 : a.parent ? s.lc : p >= s.lc ? s.end : static_cast<int>(p) + 1;
@@ -648,7 +684,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
 #pragma unroll
                 for (int c = 0; c < CS + RS; ++c) {
                     const int d = c >= CS ? DC + (c - CS) * SK + kg * 8 : F8 ? c / 2 * (2 * SK) + kg * 16 + c % 2 * 8 : c * SK + kg * 8;
-                    qf[t][c] = *reinterpret_cast<const u32x4 *>(qrow + d * 2);
+                    qf[t][c] = query_piece<DC>(s_q, row - q0, d / 8);
 #pragma unroll
                     for (int x = 0; x < 4; ++x) qf[t][c][x] = live ? qf[t][c][x] ^ flip : 0u;
                 }
@@ -944,14 +980,52 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
             }
             __syncthreads();
             if (!finding && !far) {
-                if constexpr (!SCORES) {
+                // O^T tile dt, elements 4e .. 4e + 3: components 32 dt + 8 e + 4 gh + 0..3 of the wave's quarter, of row l32
+                // of tile t: through LDS, so that whole rows are stored
+                if (cut.pieces == 1) {
+                    constexpr int STRIDE = DC * 2 + 16;
+                    static_assert(ROWS * STRIDE <= NB * kStage);
+                    if constexpr (!SCORES) {
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            const int row = t * 32 + l32;
+                            const float L = s_sum[0][row] + s_sum[1][row];
+                            const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;   // NaN stays
+                            char *dst = s_ring + row * STRIDE + (pw * (DC / 4) + 4 * gh) * 2;
+#pragma unroll
+                            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    floatx4 x;
+#pragma unroll
+                                    for (int y = 0; y < 4; ++y) x[y] = L == 0.f ? 0.f : o[t][dt][4 * e + y] * inv;
+                                    *reinterpret_cast<u32x2 *>(dst + (32 * dt + 8 * e) * 2) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+                                }
+                        }
+                    }
+                    __syncthreads();
+                    store_rows<DC * 2, 512>(s_ring, STRIDE, q1 - q0, static_cast<char *>(a.out) + (R0 + q0) * (DC * 2), tid);
+                } else {
+                    constexpr int STRIDE = DC * 4 + 16;
+                    static_assert(32 * STRIDE <= NB * kStage);
+                    const int64_t at = part_row(a, w_, 0, ROWS);
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
-                        const int row = t * 32 + l32, qi = q0 + row;
-                        if (qi < q1)
-                            store_sums<DC, DT>(a, o[t], R0 + qi, pw * (DC / 4) + 4 * gh, cut.pieces, part_row(a, w_, row, ROWS), s_max[0][row],
-                                               s_sum[0][row] + s_sum[1][row], pw == 0 && gh == 0);
+                        if (t) __syncthreads();
+                        if constexpr (!SCORES) {
+                            char *dst = s_ring + l32 * STRIDE + (pw * (DC / 4) + 4 * gh) * 4;
+#pragma unroll
+                            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    *reinterpret_cast<floatx4 *>(dst + (32 * dt + 8 * e) * 4) =
+                                        floatx4{o[t][dt][4 * e], o[t][dt][4 * e + 1], o[t][dt][4 * e + 2], o[t][dt][4 * e + 3]};
+                        }
+                        __syncthreads();
+                        const int here = min(q1 - q0 - t * 32, 32);
+                        if (here > 0) store_rows<DC * 4, 512>(s_ring, STRIDE, here, reinterpret_cast<char *>(a.part_o + (at + t * 32) * DC), tid);
                     }
+                    if (tid < q1 - q0) a.part_ml[at + tid] = make_float2(s_max[0][tid], s_sum[0][tid] + s_sum[1][tid]);
                 }
                 return;
             }
