@@ -121,33 +121,37 @@ __device__ inline int64_t part_row(const LatentArgs &a, const Unit &u, int row, 
     return (static_cast<int64_t>(u.cut) * a.splits + u.piece) * rows + row;
 }
 
-// A lane's part of row R's sums: tile dt, elements 4e .. 4e + 3 are the components d0 + 32 dt + 8 e + 0..3.  Whole
-// rows are divided by the weights' sum L; pieces are stored as they are at row `at` of the workspace, with {m, L} by one
-// lane (`first`).
-template <int DC, int DT>
-__device__ inline void store_sums(const LatentArgs &a, const floatx16 (&o)[DT], int64_t R, int d0, int pieces, int64_t at,
-                                  float m, float L, bool first) {
-    if (pieces == 1) {
-        const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;   // NaN stays
-        char *dst = static_cast<char *>(a.out) + (R * DC + d0) * 2;
+// A lane's part of a row's sums into LDS: tile dt, elements 4e .. 4e + 3 are the components 32 dt + 8 e + 0..3 from `dst`
+// on.  Whole rows are divided by the weights' sum L; pieces are kept as they are.
+template <int DT> __device__ inline void put_rows(const floatx16 (&o)[DT], float L, char *dst) {
+    const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;   // NaN stays
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                floatx4 x;
+        for (int e = 0; e < 4; ++e) {
+            floatx4 x;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = L == 0.f ? 0.f : o[dt][4 * e + i] * inv;
-                *reinterpret_cast<u32x2 *>(dst + (32 * dt + 8 * e) * 2) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
-            }
-    } else {
-        float *po = a.part_o + at * DC + d0;
+            for (int y = 0; y < 4; ++y) x[y] = L == 0.f ? 0.f : o[dt][4 * e + y] * inv;
+            *reinterpret_cast<u32x2 *>(dst + (32 * dt + 8 * e) * 2) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+        }
+}
+
+template <int DT> __device__ inline void put_sums(const floatx16 (&o)[DT], char *dst) {
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                *reinterpret_cast<floatx4 *>(po + 32 * dt + 8 * e) =
-                    floatx4{o[dt][4 * e], o[dt][4 * e + 1], o[dt][4 * e + 2], o[dt][4 * e + 3]};
-        if (first) a.part_ml[at] = make_float2(m, L);
+        for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<floatx4 *>(dst + (32 * dt + 8 * e) * 4) =
+                floatx4{o[dt][4 * e], o[dt][4 * e + 1], o[dt][4 * e + 2], o[dt][4 * e + 3]};
+}
+
+// Rows in LDS, `stride` bytes apart, to memory at `to`, where they lie one after the other.
+template <int ROW_BYTES, int T> __device__ inline void store_rows(const char *from, int stride, int rows, char *to, int tid) {
+    constexpr int PR = ROW_BYTES / 16;
+    asm volatile("" : "+v"(tid));                           // (addresses are found here, and not kept through the loop before)
+    for (int i = tid; i < rows * PR; i += T) {
+        const int r = i / PR, p = i % PR;
+        *reinterpret_cast<u32x4 *>(to + static_cast<int64_t>(i) * 16) = *reinterpret_cast<const u32x4 *>(from + r * stride + p * 16);
     }
 }
 
@@ -226,7 +230,6 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(LatentArgs a) {
     const Unit w_ = unit_of_workgroup(a);
     const int b = w_.b;
     const int q0 = w_.block * ROWS, q1 = min(q0 + ROWS, rows);
-    uint32_t id = w_.cut < 0 ? table_entry(a, b, 0) : 0u;
     const int64_t R0 = static_cast<int64_t>(b) * rows;
     u32x4 qf[2][CS + RS];                                   // of the wave's two query tiles
     int node[2];
@@ -255,6 +258,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(LatentArgs a) {
     const uint32_t ring = uniform(lds_address(s_ring));
     auto page_of = [&](int key) { return s_page[min(key >> a.c.log_page, last_page) - first_page]; };
     const int32_t *const pages = a.c.table + static_cast<int64_t>(b) * a.c.max_pages;
+    uint32_t id = table_entry(a, b, kbeg >> a.c.log_page);
     TurnLoads<DC, F8, SR> loads;
     loads.begin(lane, wave * SR);
     auto load = [&](int k0, uint32_t stage) { loads.load(a.c, loads.page(a.c, pages, k0, kend), k0, stage, kRotAt, kScaleAt, lane); };
@@ -265,26 +269,45 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(LatentArgs a) {
         if (in) s_page[tid] = none ? kNone : entry;         // a page that is none is read as page 0, and not used
         any_none = __syncthreads_or(in && none);
     };
+    const int segment = kSegment << a.c.log_page;
+    // the first turns are on their way while the rest is made ready, in the last one's place
+    if (kbeg < kend) load(kbeg, ring);
+    if (NB > 2 && kbeg + kKeys < min(kbeg + segment, kend)) load(kbeg + kKeys, ring + kStage);
     if (a.parent) {
-        uint32_t(*const anc)[8] = reinterpret_cast<uint32_t(*)[8]>(s_ring);
-        find_ancestors(a, b, anc, reinterpret_cast<int *>(s_ring + kMaxSeqRows * 32));
+        char *const room = s_ring + (NB - 1) * kStage;
+        uint32_t(*const anc)[8] = reinterpret_cast<uint32_t(*)[8]>(room);
+        find_ancestors(a, b, anc, reinterpret_cast<int *>(room + kMaxSeqRows * 32));
         for (int i = tid; i < ROWS * 8; i += T) s_seen[i / 8][i % 8] = anc[quot(a.by_grp, min(q0 + i / 8, q1 - 1))][i % 8];
         __syncthreads();
     }
 
-    // scores are taken as |scale| (+-q) . k, so that the largest product is the largest score
     int vis[2];                                             // keys [0, vis) are seen
-    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+    auto live = [&](int row) { const int64_t p = s.qs + quot(a.by_grp, row); return row < q1 && p >= 0 && p < s.end; };
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         const int64_t p = s.qs + node[t];
-        const bool live = q0 + t * 16 + ql < q1 && p >= 0 && p < s.end;
-        vis[t] = !live ? 0 : a.parent ? s.lc : p >= s.lc ? s.end : static_cast<int>(p) + 1;
-        if (!live) node[t] = -1;
+        const bool sees = live(q0 + t * 16 + ql);
+        vis[t] = !sees ? 0 : a.parent ? s.lc : p >= s.lc ? s.end : static_cast<int>(p) + 1;
+        if (!sees) node[t] = -1;
+    }
+    // (the queries have come: else the loop would wait for them, and for every load, in each turn)
 #pragma unroll
-        for (int c = 0; c < CS + RS; ++c)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) qf[t][c][x] = live ? qf[t][c][x] ^ flip : 0u;
+        for (int c = 0; c < CS + RS; ++c) asm volatile("" : "+v"(qf[t][c]));
+    // scores are taken as |scale| (+-q) . k, so that the largest product is the largest score; rows that see nothing are
+    // zeros (behind the last row it is there once more)
+    if (a.scale < 0.f || !live(q0) || !live(q1 - 1)) {
+        const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int64_t p = s.qs + quot(a.by_grp, min(q0 + t * 16 + ql, q1 - 1));
+            const bool use = p >= 0 && p < s.end;
+#pragma unroll
+            for (int c = 0; c < CS + RS; ++c)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) qf[t][c][x] = use ? qf[t][c][x] ^ flip : 0u;
+        }
     }
     const float sc = fmaxf(fabsf(a.scale) * kLog2eP, 1.17549435e-38f);
 
@@ -305,7 +328,6 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(LatentArgs a) {
     }
     const char *const w_at = s_weight + l32 * kWeightRow + gh * 16;
 
-    const int segment = kSegment << a.c.log_page;
     // Once, unless a score lies far above its row's m: then once more for the maxima alone, and again for the sums.
     bool finding = false, again = false;
     for (;;) {
@@ -319,11 +341,13 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(LatentArgs a) {
         for (int t = 0; t < 2; ++t) l[t] = 0.f;
         for (int seg = kbeg; seg < kend; seg += segment) {
             const int seg_end = min(seg + segment, kend);
-            if (seg > kbeg || w_.cut >= 0 || again) id = table_entry(a, b, seg >> a.c.log_page);
-            if (seg > kbeg) __syncthreads();                // the pages of the segment before are used up
+            if (seg > kbeg || again) {
+                id = table_entry(a, b, seg >> a.c.log_page);
+                __syncthreads();                            // the turns and pages of the segment before are used up
+                load(seg, ring);
+                if (NB > 2 && seg + kKeys < seg_end) load(seg + kKeys, ring + kStage);
+            }
             look_up(seg, seg_end, id);
-            load(seg, ring);
-            if (NB > 2 && seg + kKeys < seg_end) load(seg + kKeys, ring + kStage);
             int buf = 0;
             for (int k0 = seg; k0 < seg_end; k0 += kKeys, buf = buf + 1 == NB ? 0 : buf + 1) {
                 // this wave's part of the turn
@@ -531,13 +555,25 @@ __global__ __launch_bounds__(kThreads, 1) void k_latent_few(LatentArgs a) {
                 }
             }
             __syncthreads();
-            // O^T tile dt, elements 4e .. 4e + 3: components 32 dt + 8 e + 4 gh + 0..3 of the wave's part, of row l32
-            const int qi = q0 + l32;
-            if (qi >= q1) return;
+            // O^T tile dt, elements 4e .. 4e + 3: components 32 dt + 8 e + 4 gh + 0..3 of the wave's part, of row l32;
+            // through LDS, so that whole rows are stored
             float L = 0.f;
 #pragma unroll
             for (int i = 0; i < KP; ++i) L += s_sum[i][l32];
-            store_sums<DC, DT>(a, o, R0 + qi, wave * (DC / NW) + 4 * gh, cut.pieces, part_row(a, w_, l32, ROWS), s_max[0][l32], L, wave == 0 && gh == 0);
+            if (cut.pieces == 1) {
+                constexpr int STRIDE = DC * 2 + 16;
+                put_rows<DT>(o, L, s_ring + l32 * STRIDE + (wave * (DC / NW) + 4 * gh) * 2);
+                __syncthreads();
+                store_rows<DC * 2, T>(s_ring, STRIDE, q1 - q0, static_cast<char *>(a.out) + (R0 + q0) * (DC * 2), tid);
+            } else {
+                constexpr int STRIDE = DC * 4 + 16;
+                static_assert(ROWS * STRIDE <= NB * kStage);
+                const int64_t at = part_row(a, w_, 0, ROWS);
+                put_sums<DT>(o, s_ring + l32 * STRIDE + (wave * (DC / NW) + 4 * gh) * 4);
+                __syncthreads();
+                store_rows<DC * 4, T>(s_ring, STRIDE, q1 - q0, reinterpret_cast<char *>(a.part_o + at * DC), tid);
+                if (wave == 0 && gh == 0 && l32 < q1 - q0) a.part_ml[at + l32] = make_float2(s_max[0][l32], L);
+            }
             return;
         }
         if (finding) {                                      // every row's maximum, joined over the parts of the keys
@@ -575,16 +611,6 @@ template <int DC, int T> __device__ inline void load_queries(const char *rows_at
 template <int DC> __device__ inline u32x4 query_piece(const char *queries, int row, int piece) {
     constexpr int QB = (DC + kRotated) * 2;
     return *reinterpret_cast<const u32x4 *>(queries + row * QB + (piece ^ turned_rotated(row)) * 16);
-}
-
-// Rows in LDS, `stride` bytes apart, to memory at `to`, where they lie one after the other.
-template <int ROW_BYTES, int T> __device__ inline void store_rows(const char *from, int stride, int rows, char *to, int tid) {
-    constexpr int PR = ROW_BYTES / 16;
-    asm volatile("" : "+v"(tid));                           // (addresses are found here, and not kept through the loop before)
-    for (int i = tid; i < rows * PR; i += T) {
-        const int r = i / PR, p = i % PR;
-        *reinterpret_cast<u32x4 *>(to + static_cast<int64_t>(i) * 16) = *reinterpret_cast<const u32x4 *>(from + r * stride + p * 16);
-    }
 }
 
 // More rows: 64 of them a workgroup, with four waves for the scores and four for the sums, one of each on a SIMD.
@@ -989,18 +1015,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
 #pragma unroll
                         for (int t = 0; t < 2; ++t) {
                             const int row = t * 32 + l32;
-                            const float L = s_sum[0][row] + s_sum[1][row];
-                            const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;   // NaN stays
-                            char *dst = s_ring + row * STRIDE + (pw * (DC / 4) + 4 * gh) * 2;
-#pragma unroll
-                            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    floatx4 x;
-#pragma unroll
-                                    for (int y = 0; y < 4; ++y) x[y] = L == 0.f ? 0.f : o[t][dt][4 * e + y] * inv;
-                                    *reinterpret_cast<u32x2 *>(dst + (32 * dt + 8 * e) * 2) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
-                                }
+                            put_rows<DT>(o[t], s_sum[0][row] + s_sum[1][row], s_ring + row * STRIDE + (pw * (DC / 4) + 4 * gh) * 2);
                         }
                     }
                     __syncthreads();
@@ -1012,15 +1027,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         if (t) __syncthreads();
-                        if constexpr (!SCORES) {
-                            char *dst = s_ring + l32 * STRIDE + (pw * (DC / 4) + 4 * gh) * 4;
-#pragma unroll
-                            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    *reinterpret_cast<floatx4 *>(dst + (32 * dt + 8 * e) * 4) =
-                                        floatx4{o[t][dt][4 * e], o[t][dt][4 * e + 1], o[t][dt][4 * e + 2], o[t][dt][4 * e + 3]};
-                        }
+                        if constexpr (!SCORES) put_sums<DT>(o[t], s_ring + l32 * STRIDE + (pw * (DC / 4) + 4 * gh) * 4);
                         __syncthreads();
                         const int here = min(q1 - q0 - t * 32, 32);
                         if (here > 0) store_rows<DC * 4, 512>(s_ring, STRIDE, here, reinterpret_cast<char *>(a.part_o + (at + t * 32) * DC), tid);
