@@ -1081,14 +1081,22 @@ __global__ __launch_bounds__(256) void k_latent_join(LatentArgs a) {
     floatx4 acc[EACH];
 #pragma unroll
     for (int e = 0; e < EACH; ++e) acc[e] = floatx4{0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < n; ++p) {
-        const float wp = __shfl(w, p);
-        const bool none = __shfl(ml.x, p) == -INFINITY;     // (its sums may be anything)
+    constexpr int AT_ONCE = 4;                              // pieces whose loads are out together
+    for (int p0 = 0; p0 < n; p0 += AT_ONCE) {
+        floatx4 v[AT_ONCE][EACH];
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            const floatx4 v = *(reinterpret_cast<const floatx4 *>(a.part_o + (at + static_cast<int64_t>(p) * unit_rows) * DC) + e * 64 + lane);
+        for (int p = 0; p < AT_ONCE; ++p)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[e][i] = none ? acc[e][i] : fmaf(wp, v[i], acc[e][i]);
+            for (int e = 0; e < EACH; ++e)
+                v[p][e] = *(reinterpret_cast<const floatx4 *>(a.part_o + (at + static_cast<int64_t>(min(p0 + p, n - 1)) * unit_rows) * DC) + e * 64 + lane);
+#pragma unroll
+        for (int p = 0; p < AT_ONCE; ++p) {
+            const float wp = __shfl(w, p0 + p);
+            const bool none = p0 + p >= n || __shfl(ml.x, p0 + p) == -INFINITY;   // (its sums may be anything)
+#pragma unroll
+            for (int e = 0; e < EACH; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[e][i] = none ? acc[e][i] : fmaf(wp, v[p][e][i], acc[e][i]);
         }
     }
     const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
