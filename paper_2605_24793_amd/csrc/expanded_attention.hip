@@ -23,14 +23,13 @@ constexpr int kKeys = 64;             // of a turn
 __device__ inline int turned(int key) { return (key & 3) << 1 | (key >> 2 & 1); }
 
 template <int D, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void k_expanded_attention(ExpandedArgs a) {
+__global__ __launch_bounds__(64 * NW, 2) void k_expanded_attention(ExpandedArgs a) {
     constexpr int RB = D * 2, DR = kRotated;
     constexpr int CS = D / 16, RS = DR / 16, DT = D / 32, KT = kKeys / 32;
     constexpr int kRotAt = kKeys * RB, kValuesAt = kRotAt + kKeys * DR * 2, kStage = kValuesAt + kKeys * RB;
     constexpr int PPR = RB / 16;                            // pieces of a row
     constexpr int ROWS = 32 * NW;
     __shared__ __attribute__((aligned(128))) char s_ring[2 * kStage];
-    __shared__ uint32_t s_bad[2];                           // keys whose values are not finite
 
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int gh = lane >> 5, l32 = lane & 31;
@@ -118,9 +117,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_expanded_attention(ExpandedArgs 
         const bool masked = k0 + kKeys > all_see;           // the same in the whole workgroup
         if (masked) {
             // values that are not finite become zeros (a weight of zero would not keep them from the rows that
-            // do not see them), and their keys are marked
-            if (tid < 2) s_bad[tid] = 0;
-            lds_barrier();
+            // do not see them), and their rotated keys NaN: so are the scores then of the rows that do
             constexpr int PT = NW;                          // threads of a key
             const int key = tid / PT;
             uint32_t top = 0;
@@ -139,7 +136,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_expanded_attention(ExpandedArgs 
                 if (any) *at = x;
                 top |= any;
             }
-            if (top) atomicOr(&s_bad[key >> 5], 1u << (key & 31));
+            if (top) *reinterpret_cast<uint32_t *>(stage + kRotAt + key * (DR * 2)) = 0x7fff7fffu;
             lds_barrier();
         }
         if (k0 < most) {
@@ -161,12 +158,11 @@ __global__ __launch_bounds__(64 * NW, 1) void k_expanded_attention(ExpandedArgs 
             if (masked) {
 #pragma unroll
                 for (int t = 0; t < KT; ++t) {
-                    const uint32_t see = low_bits(vis - (k0 + 32 * t)) >> (4 * gh), bad = s_bad[t] >> (4 * gh);
+                    const uint32_t see = low_bits(vis - (k0 + 32 * t)) >> (4 * gh);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int bit = 8 * (i / 4) + i % 4;
                         if (!(see >> bit & 1)) st[t][i] = -INFINITY;
-                        else if (bad >> bit & 1) st[t][i] = NAN;
                     }
                 }
             }
@@ -234,7 +230,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_expanded_attention(ExpandedArgs 
 }
 
 // Waves of a workgroup: rows beyond 128 fill eight.
-int waves_of(int32_t n_q) { return n_q > 128 ? 8 : 4; }
+int waves_of(int32_t n_q) { return 4; }
 
 template <int D> void run_expanded(const ExpandedArgs &a, unsigned grid, hipStream_t s) {
     if (waves_of(a.n_q) == 8) hipLaunchKernelGGL((k_expanded_attention<D, 8>), dim3(grid), dim3(512), 0, s, a);
