@@ -47,7 +47,8 @@ struct ExpandedArgs {
     int32_t B, n_q, L, H, d, K;
     float scale;
     char *out;
-    FastDiv by_blocks, by_heads;        // set by the launch
+    int32_t heads_each;                 // of an XCD; this and the rest set by the launch
+    FastDiv by_together, by_blocks, by_heads;
 };
 
 hipError_t launch_latent_append(LatentAppendArgs a, hipStream_t s);

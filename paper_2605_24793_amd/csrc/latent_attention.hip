@@ -21,32 +21,6 @@ constexpr int kRotBytes = kRotated * 2;
 constexpr int kMinPieceLatent = 256;  // keys of a piece, at least
 constexpr float kFar = 60.f;          // log2 units a score may exceed a row's m by (weights and sums are floats)
 
-// 16 (or 4) bytes per lane from base + off[i] + 1024 i, off an offset of the lane's own, into LDS at byte lds + 1024 i +
-// 16 * lane (4 * lane).  A wave that loads while another one multiplies gets its vector instructions into the few
-// cycles between products: so the lanes' offsets are made once, and a turn's addresses are scalar.  (See load_lds16.)
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-template <int N> __device__ inline void load_lds_rows(const char *base, const uint32_t *off, uint32_t lds) {
-    if constexpr (N == 1)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1"
-                     : : "s"(lds), "s"(base), "v"(off[0]) : "memory", "m0");
-    else if constexpr (N == 2)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024"
-                     : : "s"(lds), "s"(base), "v"(off[0]), "v"(off[1]) : "memory", "m0");
-    else {
-        static_assert(N % 4 == 0);
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\t"
-                     "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:3072"
-                     : : "s"(lds), "s"(base), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]) : "memory", "m0");
-        if constexpr (N > 4) load_lds_rows<N - 4>(base + 4096, off + 4, lds + 4096);
-    }
-}
-
-__device__ inline void load_lds4(const char *base, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %2, %1" : : "s"(lds), "s"(base), "v"(off) : "memory", "m0");
-}
-#pragma clang diagnostic pop
-
 // A latent's sixteen-byte pieces lie in LDS in another order: piece i at place i ^ turned(key), sixteen at a time, so that
 // neither product's reads meet in the 64 banks: the first one's, sixteen rows' same piece, and the second one's, two
 // pieces of eight rows (e4m3) or four of four (bf16).  Rotated keys, eight pieces each, likewise.
