@@ -163,6 +163,13 @@ def test_scales_of_scores(scale):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F8])
+@pytest.mark.parametrize("Hq,n,q_start", [(5, 9, -4), (3, 70, 50), (7, 10, 58), (4, 5, -2), (5, 4, 61)])
+def test_negative_scales_and_rows_that_see_nothing(dtype, Hq, n, q_start):
+    """Queries before the first position and behind the last one, in blocks that are not full, of few rows and of many."""
+    _run_hybrid(dtype, 512, 32, Hq, [60, 61], [q_start, q_start], 1, n, seed=n, scale=-0.07)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F8])
 @pytest.mark.parametrize("Hq,n", [(8, 1), (40, 2)])
 def test_scores_that_rise_far(dtype, Hq, n):
     # later keys' scores lie far above the first turn's, for some rows: its sums would overflow
@@ -495,6 +502,32 @@ def test_expanded_values_that_are_not_finite(n):
         assert torch.equal(out[0, :bad], good[0, :bad])
         assert torch.equal(out[0, :, 0], good[0, :, 0])
         assert bool((~torch.isfinite(out[0, bad:, 1])).any(-1).all())
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("layout", ["heads first", "one key for all", "wide"])
+def test_expanded_strides(d, layout):
+    """Heads before positions, one position's key and value for every position, and rows of 2^24 bytes and more."""
+    L, H, ctx, K, n = 150, 2, 140, 2, 150
+    g = _gen(8)
+    q = torch.randn(1, n, H, d + 64, generator=g).to(BF16)
+    k, v = (torch.randn(1, L, H, d, generator=g).to(BF16) for _ in range(2))
+    k_r = torch.randn(1, L, 64, generator=g).to(BF16)
+    if layout == "heads first":
+        dk, dv = (x.to(DEV).transpose(1, 2).contiguous().transpose(1, 2) for x in (k, v))
+    elif layout == "one key for all":
+        k, v = (x[:, :1].expand(1, L, H, d) for x in (k, v))
+        dk, dv = (x[:, :1].contiguous().to(DEV).expand(1, L, H, d) for x in (k, v))
+    else:
+        room = torch.empty(1, L, 2 ** 23 + 1024, dtype=BF16, device=DEV)
+        wide = room[..., :2 * H * d].view(1, L, 2 * H, d)
+        wide.copy_(torch.cat((k, v), 2).to(DEV))
+        dk, dv = wide[:, :, :H], wide[:, :, H:]
+    got = cs.expanded_attention(q.to(DEV), dk, dv, k_r.to(DEV), _int([ctx]), _int([0]), K, 0.08).double().cpu()
+    sees = ref.hybrid_sees(ctx, 0, K, n, L)
+    for h in range(H):
+        want, off = _attend_kv(q[0, :, h], k[0, :, h], k_r[0], v[0, :, h], sees, 0.08)
+        assert bool(((got[0, :, h] - want).abs() <= off).all()), h
 
 
 def test_expanded_scores_that_rise():
