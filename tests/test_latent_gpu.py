@@ -537,6 +537,35 @@ def test_expanded_scores_that_rise():
     _run_expanded(128, 2, [180], [0], 1, 185, seed=6, special=special)
 
 
+# --------------------------------------------------------------------------- a large cache
+
+@pytest.mark.parametrize("dtype", [BF16, F8])
+def test_places_past_32_bits(dtype):
+    """The last pages of a cache whose latents, and then some, lie past 2^32 bytes, against the same in a small cache."""
+    P, dc, T, n = 64, 512, 8, 250
+    n_pages = 2 ** 32 // (P * dc * (2 if dtype == BF16 else 1)) + 40
+    near, g = torch.tensor([[3, 1, 2, 0]]), _gen(31)
+    tables = [near.int().to(DEV), (n_pages - T + near).int().to(DEV)]
+    caches = [cs.LatentCache.empty(T, dc, P, dtype), cs.LatentCache.empty(n_pages, dc, P, dtype)]
+    down = torch.randn(1, n, dc + 64, generator=g).to(BF16).to(DEV)
+    queries = [(torch.randn(1, m, Hq, dc + 64, generator=g) * 0.6).to(BF16).to(DEV) for m, Hq in ((1, 16), (5, 32))]
+    path = _int([[0, 2, 4] + [-1] * 5])
+    outs = []
+    for cache, table in zip(caches, tables):
+        cs.latent_append(cache, table, _int([0]), down[..., :dc], down[..., dc:])
+        outs.append([cs.latent_attention(q, cache, table, _int([n - 7]), _int([n - 9]), 2, 0.07) for q in queries])
+        outs[-1].append(cs.latent_tree_attention(queries[1], cache, table, _int([n - 5]), _int([[-1, 0, 0, 1, 2]]), 0.07))
+        cs.latent_keep(cache, table, _int([n - 8]), path)
+        cs.pages_copy(cs.PagePool.empty(cache.n_pages, P), [cache], table.view(2, 2) + _int([0, 4]))
+    for a, b in zip(*outs):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+    for small, large in zip(caches[0]._planes(), caches[1]._planes()):
+        small, large = (x.view(torch.uint8) for x in (small, large[-T:]))
+        # pages 3 and 2 went to places 1 + 4 and 0 + 4; page 0 has places that nothing was written to
+        assert torch.equal(small[[1, 2, 3, 4, 5]], large[[1, 2, 3, 4, 5]]) and torch.equal(small[0, :n % P], large[0, :n % P])
+        assert torch.equal(large[5], large[3]) and torch.equal(large[4], large[2])
+
+
 # ----------------------------------------------------------------- as a serving loop uses them
 
 def test_a_round_of_a_latent_layer():
