@@ -15,7 +15,6 @@
 namespace cospec {
 namespace {
 
-constexpr int kKeys = 64;             // of a turn
 constexpr int kFewRows = 32, kManyRows = 64;   // of a workgroup
 constexpr int kRotBytes = kRotated * 2;
 constexpr int kMinPieceLatent = 256;  // keys of a piece, at least
@@ -160,425 +159,17 @@ __device__ inline void clean_turn(char *stage, float *scales, uint32_t *bad, int
     if (real && marked) atomicOr(&bad[key >> 5], 1u << (key & 31));
 }
 
-// Up to 32 rows.  A workgroup takes a sequence, or a piece of its keys, in turns of 64 keys; the next turns' latents
-// are on their way into LDS while one is worked on.  Its four waves share both products out differently.  Scores:
-// sixteen of the turn's keys each.  Sums: a quarter of the components each.  So a latent is read from LDS
-// once for either, and a wave holds the queries and a quarter of the sums.  The rounded weights go
-// from one to the other through LDS.
-//
-// S^T = K Q^T and O^T = C^T P^T: the second product's operand C^T has positions where the rows lie; LDS turns
-// them while they are read (ds_read_b64_tr).
-//
-// A row's weights are 2^(s - m) with m the maximum of the first turn in which it sees a key: that is as exact as with
-// the running one, as long as no later score is kFar above it.  Then the sums need not be scaled
-// down on the way, and all waves know m.  Where a score is, the piece is taken again: its maxima first, then the
-// sums (the rest of the pass that finds it is for nothing: nothing else may leave the loop, or the compiler
-// keeps the sums twice).
-template <int DC, bool F8>
-__global__ __launch_bounds__(kThreads, 1) void k_latent_few(LatentArgs a) {
-    constexpr int EB = F8 ? 1 : 2, RB = DC * EB;            // bytes of a latent
-    constexpr int ROWS = kFewRows, NW = kWaves, T = kThreads;
-    constexpr int KP = 4, TK = kKeys / KP;                  // parts of a turn's keys among the waves' scores, and their keys
-    constexpr int CS = DC / 32, RS = kRotated / 32;         // k-steps of the first product, of latents and of rotated keys
-    constexpr int DT = DC / NW / 32;                        // component tiles of a wave
-    constexpr int kRotAt = kKeys * RB, kScaleAt = kRotAt + kKeys * kRotBytes, kStage = kScaleAt + (F8 ? kKeys * 4 : 0);
-    constexpr int PPR = RB / 16;                            // pieces of a row
-    constexpr int kWeightRow = kKeys * 2 + 16;              // bytes
-    constexpr int NB = kStage > 48 * 1024 ? 2 : 3;          // turns in LDS: the one worked on, and those on their way
-    constexpr int SR = kKeys / NW;                          // keys that a wave loads
-    constexpr int LPT = TurnLoads<DC, F8, SR>::COUNT;       // loads of a wave's part of a turn
-    __shared__ __attribute__((aligned(256))) char s_ring[NB * kStage];
-    __shared__ __attribute__((aligned(16))) char s_weight[ROWS * kWeightRow];
-    __shared__ uint32_t s_page[kThreads];
-    __shared__ uint32_t s_seen[ROWS][8];                    // ancestors of the rows' nodes
-    __shared__ float s_max[KP][ROWS];
-    __shared__ float s_sum[KP][ROWS];
-    __shared__ uint32_t s_bad[2];                           // of a turn's keys: latent or scale not finite
-    __shared__ int s_new, s_far;
-
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-    const int gh = lane >> 5, l32 = lane & 31;
-    const int ql = lane & 15, kg = lane >> 4;               // of the first product: query, k-piece
-    const int kp = wave;
-    const int rows = a.n_q * a.Hq;
-    const Unit w_ = unit_of_workgroup(a);
-    const int b = w_.b;
-    const int q0 = w_.block * ROWS, q1 = min(q0 + ROWS, rows);
-    const int64_t R0 = static_cast<int64_t>(b) * rows;
-    u32x4 qf[2][CS + RS];                                   // of the wave's two query tiles
-    int node[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const int qi = min(q0 + t * 16 + ql, q1 - 1);
-        node[t] = quot(a.by_grp, qi);
-        const char *qrow = static_cast<const char *>(a.q) + (R0 + qi) * ((DC + kRotated) * 2);
-#pragma unroll
-        for (int c = 0; c < CS; ++c) {
-            // in the order in which the keys' pieces come: of e4m3 a lane's sixteen bytes are two k-steps
-            const int d = F8 ? c / 2 * 64 + kg * 16 + c % 2 * 8 : c * 32 + kg * 8;
-            qf[t][c] = *reinterpret_cast<const u32x4 *>(qrow + d * 2);
-        }
-#pragma unroll
-        for (int c = 0; c < RS; ++c) qf[t][CS + c] = *reinterpret_cast<const u32x4 *>(qrow + (DC + c * 32 + kg * 8) * 2);
-    }
-    const Seq s = sequence_of(a, b);
-    const Cut cut = cut_of_unit(a, w_, s, q0, q1);
-    if (w_.piece >= cut.pieces) return;
-    const int kbeg = w_.piece * cut.chunk, kend = min(kbeg + cut.chunk, cut.kend);
-    const int all_see = seen_by_all(a, s, q0, kend);        // keys below are seen by every row that sees any
-
-    int first_page = 0, last_page = 0;                      // of those in LDS
-    bool any_none = false;
-    const uint32_t ring = uniform(lds_address(s_ring));
-    auto page_of = [&](int key) { return s_page[min(key >> a.c.log_page, last_page) - first_page]; };
-    const int32_t *const pages = a.c.table + static_cast<int64_t>(b) * a.c.max_pages;
-    uint32_t id = table_entry(a, b, kbeg >> a.c.log_page);
-    TurnLoads<DC, F8, SR> loads;
-    loads.begin(lane, wave * SR);
-    auto load = [&](int k0, uint32_t stage) { loads.load(a.c, loads.page(a.c, pages, k0, kend), k0, stage, kRotAt, kScaleAt, lane); };
-    auto look_up = [&](int from, int to, uint32_t entry) {  // of keys [from, to), this thread's table entry given
-        first_page = from >> a.c.log_page;
-        last_page = (to - 1) >> a.c.log_page;
-        const bool in = tid <= last_page - first_page, none = entry >= static_cast<uint32_t>(a.c.n_pages);
-        if (in) s_page[tid] = none ? kNone : entry;         // a page that is none is read as page 0, and not used
-        any_none = __syncthreads_or(in && none);
-    };
-    const int segment = kSegment << a.c.log_page;
-    // the first turns are on their way while the rest is made ready, in the last one's place
-    if (kbeg < kend) load(kbeg, ring);
-    if (NB > 2 && kbeg + kKeys < min(kbeg + segment, kend)) load(kbeg + kKeys, ring + kStage);
-    if (a.parent) {
-        char *const room = s_ring + (NB - 1) * kStage;
-        uint32_t(*const anc)[8] = reinterpret_cast<uint32_t(*)[8]>(room);
-        find_ancestors(a, b, anc, reinterpret_cast<int *>(room + kMaxSeqRows * 32));
-        for (int i = tid; i < ROWS * 8; i += T) s_seen[i / 8][i % 8] = anc[quot(a.by_grp, min(q0 + i / 8, q1 - 1))][i % 8];
-        __syncthreads();
-    }
-
-    int vis[2];                                             // keys [0, vis) are seen
-    auto live = [&](int row) { const int64_t p = s.qs + quot(a.by_grp, row); return row < q1 && p >= 0 && p < s.end; };
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const int64_t p = s.qs + node[t];
-        const bool sees = live(q0 + t * 16 + ql);
-        vis[t] = !sees ? 0 : a.parent ? s.lc : p >= s.lc ? s.end : static_cast<int>(p) + 1;
-        if (!sees) node[t] = -1;
-    }
-    // (the queries have come: else the loop would wait for them, and for every load, in each turn)
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int c = 0; c < CS + RS; ++c) asm volatile("" : "+v"(qf[t][c]));
-    // scores are taken as |scale| (+-q) . k, so that the largest product is the largest score; rows that see nothing are
-    // zeros (behind the last row it is there once more)
-    if (a.scale < 0.f || !live(q0) || !live(q1 - 1)) {
-        const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int64_t p = s.qs + quot(a.by_grp, min(q0 + t * 16 + ql, q1 - 1));
-            const bool use = p >= 0 && p < s.end;
-#pragma unroll
-            for (int c = 0; c < CS + RS; ++c)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) qf[t][c][x] = use ? qf[t][c][x] ^ flip : 0u;
-        }
-    }
-    const float sc = fmaxf(fabsf(a.scale) * kLog2eP, 1.17549435e-38f);
-
-    float m[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) m[t] = -INFINITY;
-    if (tid == 0) s_new = s_far = 0;
-
-    // where this lane reads: keys' pieces, rotated keys' pieces, latents' components, weights
-    const int krow = kp * TK + ql;
-    const uint32_t k_at = krow * RB + (kg ^ turned<F8>(krow)) * 16;
-    const uint32_t r_at = kRotAt + krow * kRotBytes + (kg ^ turned_rotated(krow)) * 16;
-    uint32_t v_at;
-    {
-        const int j = lane & 15, cg = lane >> 4 & 1, row = 8 * gh + (F8 ? j >> 1 : j >> 2);
-        const int piece = wave * (PPR / NW) + (F8 ? cg : 2 * cg + (j >> 1 & 1));
-        v_at = row * RB + (piece >> 4) * 256 + ((piece ^ turned<F8>(row)) & 15) * 16 + (j & 1) * 8;
-    }
-    const char *const w_at = s_weight + l32 * kWeightRow + gh * 16;
-
-    // Once, unless a score lies far above its row's m: then once more for the maxima alone, and again for the sums.
-    bool finding = false, again = false;
-    for (;;) {
-        floatx16 o[DT];
-        float l[2];                                        // of this lane's keys alone
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) l[t] = 0.f;
-        for (int seg = kbeg; seg < kend; seg += segment) {
-            const int seg_end = min(seg + segment, kend);
-            if (seg > kbeg || again) {
-                id = table_entry(a, b, seg >> a.c.log_page);
-                __syncthreads();                            // the turns and pages of the segment before are used up
-                load(seg, ring);
-                if (NB > 2 && seg + kKeys < seg_end) load(seg + kKeys, ring + kStage);
-            }
-            look_up(seg, seg_end, id);
-            int buf = 0;
-            for (int k0 = seg; k0 < seg_end; k0 += kKeys, buf = buf + 1 == NB ? 0 : buf + 1) {
-                // this wave's part of the turn
-                if (NB > 2 && k0 + kKeys < seg_end) wait_vm<LPT>();
-                else wait_vm<0>();
-                lds_barrier();                              // ... and the others'; the turn before is used up
-                char *const stage = s_ring + buf * kStage;
-                const bool masked = k0 + kKeys > all_see || any_none;   // the same in the whole workgroup
-                if (masked) {
-                    if (tid < 2) s_bad[tid] = 0;
-                    lds_barrier();
-                    const int key = k0 + tid / (T / kKeys);
-                    clean_turn<RB, kKeys, T, F8>(stage, reinterpret_cast<float *>(stage + kScaleAt), s_bad, tid,
-                                                 key < kend && page_of(key) < kNone);
-                    lds_barrier();
-                }
-                // S^T.  Operands are read from LDS a group ahead of the products that take them.
-                constexpr int LOADS = CS / (F8 ? 2 : 1), G = F8 ? 4 : 8, NG = LOADS / G;
-                floatx4 st[2];
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) st[t][i] = 0.f;
-                u32x4 kf[2][G], rf[RS];
-                auto read_keys = [&](int g) __attribute__((always_inline)) {
-#pragma unroll
-                    for (int i = 0; i < G; ++i) {
-                        const int c = g * G + i;
-                        kf[g & 1][i] = *reinterpret_cast<const u32x4 *>(stage + (k_at ^ (c % 4 * 64)) + c / 4 * 256);
-                    }
-                };
-                auto read_rotated = [&]() __attribute__((always_inline)) {
-#pragma unroll
-                    for (int c = 0; c < RS; ++c) rf[c] = *reinterpret_cast<const u32x4 *>(stage + (r_at ^ (c * 64)));
-                };
-                auto multiply = [&](u32x4 k, int c) __attribute__((always_inline)) {
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) st[t] = mfma(k, qf[t][c], st[t]);
-                };
-                read_keys(0);
-                if constexpr (NG > 1) read_keys(1);
-                else read_rotated();
-                __builtin_amdgcn_sched_barrier(0);
-                {
-                    const int ahead = k0 + (NB - 1) * kKeys;
-                    const int to = NB > 2 ? (buf == 0 ? NB - 1 : buf - 1) : buf ^ 1;
-                    if (ahead < seg_end) load(ahead, ring + to * kStage);
-                }
-                floatx4 sv;                                 // scales of this lane's keys
-                if constexpr (F8) sv = *reinterpret_cast<const floatx4 *>(stage + kScaleAt + (kp * TK + 4 * kg) * 4);
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int i = 0; i < G; ++i) {
-                        const u32x4 raw = kf[g & 1][i];
-                        const int c = g * G + i;
-                        if constexpr (F8) {
-                            multiply(widen(raw[0], raw[1], 1.f), 2 * c);
-                            multiply(widen(raw[2], raw[3], 1.f), 2 * c + 1);
-                        } else {
-                            multiply(raw, c);
-                        }
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (g + 2 < NG) read_keys(g + 2);
-                    else if (g + 2 == NG) read_rotated();
-                }
-                // the second product's operands, sixteen keys at a time; the first ones now
-                constexpr int NV = kKeys / 16;
-                u32x4 pb[2], vf[2][DT];                     // (e4m3: two words of each)
-                auto read_values = [&](int v) __attribute__((always_inline)) {
-                    const char *const at = stage + v * 16 * RB;
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) {
-                        if constexpr (F8) {
-                            const i32x2 raw = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(at + (v_at ^ (dt * 32))));
-                            vf[v & 1][dt][0] = raw[0];
-                            vf[v & 1][dt][1] = raw[1];
-                        } else {
-                            const uint32_t here = v_at ^ (dt * 64);
-                            const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + here)));
-                            const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 4 * RB + (here ^ 16))));
-                            vf[v & 1][dt] = u32x4{lo[0], lo[1], hi[0], hi[1]};
-                        }
-                    }
-                };
-                auto read_weights = [&](int v) __attribute__((always_inline)) {
-                    pb[v & 1] = *reinterpret_cast<const u32x4 *>(w_at + v * 32);
-                };
-                read_values(0);
-                if constexpr (F8) {
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) st[t][i] *= sv[i];
-                }
-#pragma unroll
-                for (int c = 0; c < RS; ++c) multiply(rf[c], CS + c);
-                if (masked) {
-                    const int kb = k0 + kp * TK;
-                    uint32_t real = low_bits(kend - kb);
-                    if (page_of(kb) >= kNone) real = 0;
-                    const uint32_t bad = s_bad[kp * TK / 32] >> (kp * TK % 32 + 4 * kg);
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        uint32_t see = low_bits(vis[t] - kb);
-                        if (a.parent && node[t] >= 0) see |= window32(s_seen[t * 16 + ql], kb - s.lc);
-                        see = (see & real) >> (4 * kg);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float x = (bad >> i & 1) != 0 ? NAN : st[t][i];
-                            st[t][i] = (see >> i & 1) != 0 ? x : -INFINITY;
-                        }
-                    }
-                }
-                float bm[2];
-                bool fresh = false;                         // a row's first keys, or a score far above m
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    bm[t] = -INFINITY;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) bm[t] = fmaxf(bm[t], st[t][i]);
-                    bm[t] = max_rows(bm[t]) * sc;
-                    fresh |= bm[t] > m[t] + kFar;           // always when m is still -inf
-                }
-                float sum[2];
-                auto weigh = [&]() __attribute__((always_inline)) {
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        // a query that has seen nothing yet keeps m = -inf and adds nothing
-                        const float mm = m[t] == -INFINITY || finding ? INFINITY : m[t];
-                        sum[t] = 0.f;
-                        char *to = s_weight + (t * 16 + ql) * kWeightRow + (kp * TK + 4 * kg) * 2;
-                        float p[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            p[i] = __builtin_amdgcn_exp2f(fmaf(st[t][i], sc, -mm));
-                            sum[t] += p[i];
-                            if constexpr (F8) p[i] *= sv[i];
-                        }
-                        *reinterpret_cast<u32x2 *>(to) = u32x2{bf16_pair(p[0], p[1]), bf16_pair(p[2], p[3])};
-                    }
-                };
-                weigh();
-                if (finding) {
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) m[t] = fmaxf(m[t], bm[t]);
-                } else if (__ballot(fresh) != 0 && lane == 0) {
-                    s_new = 1;
-                }
-                lds_barrier();                              // the weights are there
-                read_weights(0);
-                if (__builtin_expect(uniform(s_new), 0)) {
-                    // the same maximum in all waves, then the weights again
-                    if (kg == 0) {
-#pragma unroll
-                        for (int t = 0; t < 2; ++t) s_max[kp][t * 16 + ql] = bm[t];
-                    }
-                    lds_barrier();
-                    if (tid == 0) s_new = 0;
-                    bool above = false;
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        float top = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < KP; ++i) top = fmaxf(top, s_max[i][t * 16 + ql]);
-                        if (m[t] == -INFINITY) m[t] = top;
-                        else above |= top > m[t] + kFar;
-                    }
-                    if (__ballot(above) != 0 && lane == 0) s_far = 1;
-                    weigh();
-                    lds_barrier();
-                    read_weights(0);
-                }
-#pragma unroll
-                for (int t = 0; t < 2; ++t) l[t] += sum[t];
-                // O^T += C^T P^T
-#pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    if (v + 1 < NV) {
-                        read_values(v + 1);
-                        read_weights(v + 1);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) {
-                        const u32x4 raw = vf[v & 1][dt], c = F8 ? widen(raw[0], raw[1], 1.f) : raw;
-                        o[dt] = mfma32(c, pb[v & 1], o[dt]);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-        }
-        wait_vm<0>();
-        __syncthreads();
-        if (!finding && uniform(s_far) == 0) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                l[t] += __shfl_xor(l[t], 16);
-                l[t] += __shfl_xor(l[t], 32);
-                if (kg == 0) {
-                    s_sum[kp][t * 16 + ql] = node[t] >= 0 ? l[t] : 0.f;   // (unmasked turns give padding rows some weights)
-                    s_max[kp][t * 16 + ql] = node[t] >= 0 ? m[t] : -INFINITY;
-                }
-            }
-            __syncthreads();
-            // O^T tile dt, elements 4e .. 4e + 3: components 32 dt + 8 e + 4 gh + 0..3 of the wave's part, of row l32;
-            // through LDS, so that whole rows are stored
-            float L = 0.f;
-#pragma unroll
-            for (int i = 0; i < KP; ++i) L += s_sum[i][l32];
-            if (cut.pieces == 1) {
-                constexpr int STRIDE = DC * 2 + 16;
-                put_rows<DT>(o, L, s_ring + l32 * STRIDE + (wave * (DC / NW) + 4 * gh) * 2);
-                __syncthreads();
-                store_rows<DC * 2, T>(s_ring, STRIDE, q1 - q0, static_cast<char *>(a.out) + (R0 + q0) * (DC * 2), tid);
-            } else {
-                constexpr int STRIDE = DC * 4 + 16;
-                static_assert(ROWS * STRIDE <= NB * kStage);
-                const int64_t at = part_row(a, w_, 0, ROWS);
-                put_sums<DT>(o, s_ring + l32 * STRIDE + (wave * (DC / NW) + 4 * gh) * 4);
-                __syncthreads();
-                store_rows<DC * 4, T>(s_ring, STRIDE, q1 - q0, reinterpret_cast<char *>(a.part_o + at * DC), tid);
-                if (wave == 0 && gh == 0 && l32 < q1 - q0) a.part_ml[at + l32] = make_float2(s_max[0][l32], L);
-            }
-            return;
-        }
-        if (finding) {                                      // every row's maximum, joined over the parts of the keys
-            if (kg == 0) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t) s_max[kp][t * 16 + ql] = m[t];
-            }
-            __syncthreads();
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < KP; ++i) m[t] = fmaxf(m[t], s_max[i][t * 16 + ql]);
-            finding = false;
-        } else {
-            __syncthreads();                                // every wave knows of it
-            if (tid == 0) s_far = 0;
-            finding = again = true;
-        }
-    }
-}
-
-// A workgroup's queries (64 rows that lie one after the other in memory) on their way into LDS, by T threads: a lane of a
+// A workgroup's queries (ROWS rows that lie one after the other in memory) on their way into LDS, by T threads: a lane of a
 // product reads a row's pieces, which from memory would take a line for each.  Piece p of row r lies at place
 // p ^ turned_rotated(r) of its eight.
-template <int DC, int T> __device__ inline void load_queries(const char *rows_at, int rows, uint32_t to, int wave, int lane) {
-    constexpr int QB = (DC + kRotated) * 2, PQ = QB / 16, N = kManyRows * QB / 1024 / (T / 64);
-    static_assert(kManyRows * QB % (1024 * (T / 64)) == 0 && PQ % 8 == 0 && QB % 256 == 128);
+template <int DC, int ROWS, int T> __device__ inline void load_queries(const char *rows_at, int rows, uint32_t to, int wave, int lane) {
+    constexpr int QB = (DC + kRotated) * 2, PQ = QB / 16, LOADS = ROWS * QB / 1024, N = (LOADS + T / 64 - 1) / (T / 64);
+    static_assert(ROWS * QB % 1024 == 0 && PQ % 8 == 0 && QB % 256 == 128);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int at = (wave * N + i) * 64 + lane, r = at / PQ, p = (at - r * PQ) ^ turned_rotated(r);
-        load_lds16<false>(rows_at + static_cast<int64_t>(min(r, rows - 1)) * QB + p * 16, to + (wave * N + i) * 1024);
+        if (LOADS % (T / 64) == 0 || wave * N + i < LOADS)
+            load_lds16<false>(rows_at + static_cast<int64_t>(min(r, rows - 1)) * QB + p * 16, to + (wave * N + i) * 1024);
     }
 }
 
@@ -598,30 +189,30 @@ template <int DC> __device__ inline u32x4 query_piece(const char *queries, int r
 //
 // After barrier i turn i is staged and turn i - 1 weighed: the scores' waves take turn i, the sums' waves turn
 // i - 1, and load ahead.  Rows' maxima as in k_latent_few.
-template <int DC, bool F8>
-__global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
+template <int DC, bool F8, int ROWS>
+__global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
     constexpr int EB = F8 ? 1 : 2, RB = DC * EB;            // bytes of a latent
     constexpr int KS = RB > 512 ? 32 : 64;                  // keys of a turn
-    constexpr bool WIDE = KS == 64;
-    constexpr int QT = WIDE ? 1 : 2, QW = WIDE ? 32 : 16;   // query tiles of a scores' wave, and their width
+    constexpr bool WIDE = KS == 64 && ROWS == 64;           // scores by 32 x 32 products, or by 16 x 16
+    constexpr int QW = WIDE ? 32 : 16, TK = QW;             // rows and keys of a tile of scores
+    constexpr int KP = KS / TK, RP = 4 / KP;                // parts of the keys, and of the rows, among the scores' waves
+    constexpr int QT = ROWS / RP / QW;                      // tiles of a wave
     constexpr int SK = WIDE ? 16 : 32;                      // components of a k-step of its products
     constexpr int CS = DC / SK, RS = kRotated / SK;         // its k-steps, of latents and of rotated keys
     constexpr int NS = WIDE ? 16 : 4;                       // scores of a lane and query tile
-    constexpr int TK = KS / 2;                              // keys of a wave's scores
-    constexpr int DT = DC / 4 / 32;                         // component tiles of a sums' wave
+    constexpr int DT = DC / 4 / 32, RT = ROWS / 32;         // component tiles, and tiles of rows, of a sums' wave
     constexpr int kRotAt = KS * RB, kScaleAt = kRotAt + KS * kRotBytes, kStage = kScaleAt + (F8 ? KS * 4 : 0);
     constexpr int NB = RB > 512 ? 4 : 3, AHEAD = NB - 2;    // turns in LDS, and on their way
     constexpr int PPR = RB / 16;                            // pieces of a row
     constexpr int SR = KS / 4;                              // keys that a sums' wave loads
     constexpr int LPT = TurnLoads<DC, F8, SR>::COUNT;       // its loads of a turn
     constexpr int kWeightRow = KS * 2 + 16;                 // bytes
-    constexpr int ROWS = kManyRows;
     __shared__ __attribute__((aligned(256))) char s_ring[NB * kStage];
     __shared__ __attribute__((aligned(16))) char s_weight[2][ROWS * kWeightRow];
     __shared__ uint32_t s_page[kThreads];
     __shared__ uint32_t s_seen[ROWS][8];                    // ancestors of the rows' nodes
-    __shared__ float s_max[2][ROWS];
-    __shared__ float s_sum[2][ROWS];
+    __shared__ float s_max[KP][ROWS];
+    __shared__ float s_sum[KP][ROWS];
     __shared__ uint32_t s_bad[2];                           // of a turn's keys: latent or scale not finite
     __shared__ int s_new, s_far, s_none;
 
@@ -635,7 +226,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
     // the queries go behind the turns that are loaded before they are read
     char *const s_q = s_ring + AHEAD * kStage;
     static_assert(AHEAD * kStage + ROWS * (DC + kRotated) * 2 <= NB * kStage);
-    load_queries<DC, 512>(static_cast<const char *>(a.q) + (R0 + q0) * ((DC + kRotated) * 2), q1 - q0, uniform(lds_address(s_q)), wave, lane);
+    load_queries<DC, ROWS, 512>(static_cast<const char *>(a.q) + (R0 + q0) * ((DC + kRotated) * 2), q1 - q0, uniform(lds_address(s_q)), wave, lane);
     const Seq s = sequence_of(a, b);
     const Cut cut = cut_of_unit(a, w_, s, q0, q1);
     if (w_.piece >= cut.pieces) {
@@ -647,7 +238,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
     if (a.parent) {
         uint32_t(*const anc)[8] = reinterpret_cast<uint32_t(*)[8]>(s_ring);
         find_ancestors(a, b, anc, reinterpret_cast<int *>(s_ring + kMaxSeqRows * 32));
-        s_seen[tid / 8][tid % 8] = anc[quot(a.by_grp, min(q0 + tid / 8, q1 - 1))][tid % 8];
+        if (tid < ROWS * 8) s_seen[tid / 8][tid % 8] = anc[quot(a.by_grp, min(q0 + tid / 8, q1 - 1))][tid % 8];
         __syncthreads();
     }
     if (tid == 0) s_new = s_far = 0;
@@ -658,12 +249,25 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
     const uint32_t ring = uniform(lds_address(s_ring));
     const float sc = fmaxf(fabsf(a.scale) * kLog2eP, 1.17549435e-38f);
 
+    auto joined_max = [&](int row) {
+        float x = s_max[0][row];
+#pragma unroll
+        for (int i = 1; i < KP; ++i) x = fmaxf(x, s_max[i][row]);
+        return x;
+    };
+    auto joined_sum = [&](int row) {
+        float x = s_sum[0][row];
+#pragma unroll
+        for (int i = 1; i < KP; ++i) x += s_sum[i][row];
+        return x;
+    };
+
     // All of it, as one kind of wave does it: both meet the same barriers.
     auto work = [&](auto kind) __attribute__((always_inline)) {
         constexpr bool SCORES = decltype(kind)::value;
         // scores: queries, in the order in which the keys' pieces come (of e4m3 a lane's sixteen bytes are two k-steps)
         const int ql = WIDE ? l32 : lane & 15, kg = WIDE ? gh : lane >> 4;   // query, k-piece
-        const int rw = wave & 1, kp = wave >> 1 & 1;
+        const int rw = (wave & 3) % RP, kp = (wave & 3) / RP;
         [[maybe_unused]] u32x4 qf[QT][CS + RS];
         [[maybe_unused]] int node[QT], vis[QT];             // keys [0, vis) are seen
         [[maybe_unused]] float m[QT];
@@ -674,7 +278,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
             const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;   // scores as |scale| (+-q) . k: the largest product is the largest
 #pragma unroll
             for (int t = 0; t < QT; ++t) {
-                const int row = q0 + rw * 32 + t * 16 + ql, qi = min(row, q1 - 1);
+                const int row = q0 + rw * (QT * QW) + t * QW + ql, qi = min(row, q1 - 1);
                 node[t] = quot(a.by_grp, qi);
                 const int64_t p = s.qs + node[t];
                 const bool live = row < q1 && p >= 0 && p < s.end;
@@ -711,14 +315,14 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
         // Once, unless a score lies far above its row's m: then once more for the maxima alone, and again for the sums.
         bool finding = false;
         for (;;) {
-            [[maybe_unused]] floatx16 o[2][DT];
+            [[maybe_unused]] floatx16 o[RT][DT];
             [[maybe_unused]] float l[QT];                   // of this lane's keys alone
             if constexpr (SCORES) {
 #pragma unroll
                 for (int t = 0; t < QT; ++t) l[t] = 0.f;
             } else {
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < RT; ++t)
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -763,7 +367,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
                             // a query that has seen nothing yet keeps m = -inf and adds nothing
                             const float mm = m[t] == -INFINITY || finding ? INFINITY : m[t];
                             sum[t] = 0.f;
-                            char *to = s_weight[turn & 1] + (rw * 32 + t * QW + ql) * kWeightRow + (kp * TK + 4 * kg) * 2;
+                            char *to = s_weight[turn & 1] + (rw * (QT * QW) + t * QW + ql) * kWeightRow + (kp * TK + 4 * kg) * 2;
 #pragma unroll
                             for (int e = 0; e < NS / 4; ++e) {
                                 float p[4];
@@ -782,7 +386,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
                         if constexpr (SCORES) {
                             if (kg == 0) {
 #pragma unroll
-                                for (int t = 0; t < QT; ++t) s_max[kp][rw * 32 + t * QW + ql] = bm[t];
+                                for (int t = 0; t < QT; ++t) s_max[kp][rw * (QT * QW) + t * QW + ql] = bm[t];
                             }
                         }
                         lds_barrier();
@@ -791,8 +395,8 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
                             bool above = false;
 #pragma unroll
                             for (int t = 0; t < QT; ++t) {
-                                const int row = rw * 32 + t * QW + ql;
-                                const float top = fmaxf(s_max[0][row], s_max[1][row]);
+                                const int row = rw * (QT * QW) + t * QW + ql;
+                                const float top = joined_max(row);
                                 if (m[t] == -INFINITY) m[t] = top;
                                 else above |= top > m[t] + kFar;
                             }
@@ -888,7 +492,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
 #pragma unroll
                             for (int t = 0; t < QT; ++t) {
                                 uint32_t see = low_bits(vis[t] - kb);
-                                if (a.parent && node[t] >= 0) see |= window32(s_seen[rw * 32 + t * QW + ql], kb - s.lc);
+                                if (a.parent && node[t] >= 0) see |= window32(s_seen[rw * (QT * QW) + t * QW + ql], kb - s.lc);
                                 see = (see & real) >> (4 * kg);
 #pragma unroll
                                 for (int x = 0; x < NS; ++x) {
@@ -928,11 +532,11 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
                         const char *const held = s_ring + (buf == 0 ? NB - 1 : buf - 1) * kStage;
                         const char *const w_at = s_weight[(i - 1) & 1] + l32 * kWeightRow + gh * 16;
                         constexpr int NV = KS / 16;
-                        u32x4 pb[2][2], vf[2][DT];          // (e4m3: two words of each)
+                        u32x4 pb[2][RT], vf[2][DT];          // (e4m3: two words of each)
                         auto read = [&](int v) __attribute__((always_inline)) {
                             const char *const at = held + v * 16 * RB;
 #pragma unroll
-                            for (int t = 0; t < 2; ++t) pb[v & 1][t] = *reinterpret_cast<const u32x4 *>(w_at + t * (32 * kWeightRow) + v * 32);
+                            for (int t = 0; t < RT; ++t) pb[v & 1][t] = *reinterpret_cast<const u32x4 *>(w_at + t * (32 * kWeightRow) + v * 32);
 #pragma unroll
                             for (int dt = 0; dt < DT; ++dt) {
                                 if constexpr (F8) {
@@ -956,7 +560,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
                             for (int dt = 0; dt < DT; ++dt) {
                                 const u32x4 raw = vf[v & 1][dt], c = F8 ? widen(raw[0], raw[1], 1.f) : raw;
 #pragma unroll
-                                for (int t = 0; t < 2; ++t) o[t][dt] = mfma32(c, pb[v & 1][t], o[t][dt]);
+                                for (int t = 0; t < RT; ++t) o[t][dt] = mfma32(c, pb[v & 1][t], o[t][dt]);
                             }
                             __builtin_amdgcn_sched_barrier(0);
                         }
@@ -970,7 +574,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
                 for (int t = 0; t < QT; ++t) {
                     if constexpr (!WIDE) l[t] += __shfl_xor(l[t], 16);
                     l[t] += __shfl_xor(l[t], 32);
-                    const int row = rw * 32 + t * QW + ql;
+                    const int row = rw * (QT * QW) + t * QW + ql;
                     if (kg == 0) {
                         // (unmasked turns give padding rows some weights)
                         s_sum[kp][row] = node[t] >= 0 ? l[t] : 0.f;
@@ -987,9 +591,9 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
                     static_assert(ROWS * STRIDE <= NB * kStage);
                     if constexpr (!SCORES) {
 #pragma unroll
-                        for (int t = 0; t < 2; ++t) {
+                        for (int t = 0; t < RT; ++t) {
                             const int row = t * 32 + l32;
-                            put_rows<DT>(o[t], s_sum[0][row] + s_sum[1][row], s_ring + row * STRIDE + (pw * (DC / 4) + 4 * gh) * 2);
+                            put_rows<DT>(o[t], joined_sum(row), s_ring + row * STRIDE + (pw * (DC / 4) + 4 * gh) * 2);
                         }
                     }
                     __syncthreads();
@@ -999,14 +603,14 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
                     static_assert(32 * STRIDE <= NB * kStage);
                     const int64_t at = part_row(a, w_, 0, ROWS);
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) {
+                    for (int t = 0; t < RT; ++t) {
                         if (t) __syncthreads();
                         if constexpr (!SCORES) put_sums<DT>(o[t], s_ring + l32 * STRIDE + (pw * (DC / 4) + 4 * gh) * 4);
                         __syncthreads();
                         const int here = min(q1 - q0 - t * 32, 32);
                         if (here > 0) store_rows<DC * 4, 512>(s_ring, STRIDE, here, reinterpret_cast<char *>(a.part_o + (at + t * 32) * DC), tid);
                     }
-                    if (tid < q1 - q0) a.part_ml[at + tid] = make_float2(s_max[0][tid], s_sum[0][tid] + s_sum[1][tid]);
+                    if (tid < q1 - q0) a.part_ml[at + tid] = make_float2(s_max[0][tid], joined_sum(tid));
                 }
                 return;
             }
@@ -1014,8 +618,8 @@ __global__ __launch_bounds__(512, 1) void k_latent_many(LatentArgs a) {
                 if (finding) {                              // every row's maximum, joined over the parts of the keys
 #pragma unroll
                     for (int t = 0; t < QT; ++t) {
-                        const int row = rw * 32 + t * QW + ql;
-                        m[t] = fmaxf(s_max[0][row], s_max[1][row]);
+                        const int row = rw * (QT * QW) + t * QW + ql;
+                        m[t] = joined_max(row);
                     }
                 }
             }
@@ -1081,8 +685,8 @@ __global__ __launch_bounds__(256) void k_latent_join(LatentArgs a) {
 }
 
 template <int DC, bool F8> void run_attention(const LatentArgs &a, unsigned grid, hipStream_t s) {
-    if (a.row_tiles == kManyRows) hipLaunchKernelGGL((k_latent_many<DC, F8>), dim3(grid), dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((k_latent_few<DC, F8>), dim3(grid), dim3(kThreads), 0, s, a);
+    if (a.row_tiles == kManyRows) hipLaunchKernelGGL((k_latent_attention<DC, F8, kManyRows>), dim3(grid), dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((k_latent_attention<DC, F8, kFewRows>), dim3(grid), dim3(512), 0, s, a);
 }
 
 }  // namespace
