@@ -17,7 +17,14 @@ namespace {
 
 constexpr int kFewRows = 32, kManyRows = 64;   // of a workgroup
 constexpr int kRotBytes = kRotated * 2;
-constexpr int kMinPieceLatent = 256;  // keys of a piece, at least
+
+// Keys of a piece, at least, where there are up to 16 pieces, and beyond.  Short pieces save turns, but the join reads every
+// one of them.  A query of 16 heads after 2000 positions (e4m3, d_c = 512): 16 pieces of 128 keys 13.2 us, 8 of 256 14.3, 4
+// of 512 18; after 8000 positions 63 of 128 17.0, 32 of 256 15.8; four queries of 32 heads after 4000 positions 32 of 128
+// 17.7, 16 of 256 16.3.
+constexpr int kMinPieceLatent = 128, kMinOfManyPieces = 256;
+constexpr int64_t kFewPieces = 16;
+
 constexpr float kFar = 60.f;          // log2 units a score may exceed a row's m by (weights and sums are floats)
 
 // A latent's sixteen-byte pieces lie in LDS in another order: piece i at place i ^ turned(key), sixteen at a time, so that
@@ -631,15 +638,16 @@ __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
     else work(std::false_type{});
 }
 
-// Joins the pieces of the units that were cut: one wave per row, lane s weighs piece s, then each lane
-// takes DC / 64 components of every piece.
+// Joins the pieces of the units that were cut.  It waits for memory, so a workgroup takes a row and has eight pieces' loads out
+// at a time (16 heads, 32 pieces: 17.9 us for both launches with a wave a row and four pieces, 15.8 so); lane s weighs piece s, then each thread takes
+// DC / 256 components of every piece.  A launch after the pieces' own: their order is the same every time.
 template <int DC>
 __global__ __launch_bounds__(256) void k_latent_join(LatentArgs a) {
-    constexpr int EACH = DC / 256;                          // four components at a time
+    constexpr int EACH = DC / 256, AT_ONCE = 8;             // components of a thread; pieces whose loads are out together
+    using part = typename std::conditional<EACH == 2, float2, float>::type;
     const int lane = threadIdx.x & 63;
     const int rows = a.n_q * a.Hq, unit_rows = a.row_tiles;
-    const int x = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int cut = x / unit_rows, row = x - cut * unit_rows;   // (a power of two)
+    const int cut = blockIdx.x / unit_rows, row = blockIdx.x - cut * unit_rows;   // (a power of two)
     const Unit u = unit_at(a, a.whole + cut, 0, cut);
     const int q0 = u.block * unit_rows, q1 = min(q0 + unit_rows, rows);
     if (q0 + row >= q1) return;
@@ -648,40 +656,41 @@ __global__ __launch_bounds__(256) void k_latent_join(LatentArgs a) {
     const Cut c = cut_of(a, sequence_of(a, u.b), q0, q1);
     if (c.pieces == 1) return;                              // written whole
     const int n = c.pieces;
-    if (lane >= n) ml = make_float2(-INFINITY, 0.f);
-    float M = ml.x;
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
-    const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
-    float l = ml.x == -INFINITY ? 0.f : w * ml.y;
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off);
-    floatx4 acc[EACH];
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) acc[e] = floatx4{0.f, 0.f, 0.f, 0.f};
-    constexpr int AT_ONCE = 4;                              // pieces whose loads are out together
+    const part *from = reinterpret_cast<const part *>(a.part_o + at * DC) + threadIdx.x;
+    const int64_t step = static_cast<int64_t>(unit_rows) * 256;
+    float acc[2] = {0.f, 0.f};
+    float w = 0.f, l = 0.f;
     for (int p0 = 0; p0 < n; p0 += AT_ONCE) {
-        floatx4 v[AT_ONCE][EACH];
+        part v[AT_ONCE];
 #pragma unroll
-        for (int p = 0; p < AT_ONCE; ++p)
+        for (int p = 0; p < AT_ONCE; ++p) v[p] = from[min(p0 + p, n - 1) * step];
+        if (p0 == 0) {                                      // while the first ones come
+            if (lane >= n) ml = make_float2(-INFINITY, 0.f);
+            float M = ml.x;
 #pragma unroll
-            for (int e = 0; e < EACH; ++e)
-                v[p][e] = *(reinterpret_cast<const floatx4 *>(a.part_o + (at + static_cast<int64_t>(min(p0 + p, n - 1)) * unit_rows) * DC) + e * 64 + lane);
+            for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
+            w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+            l = ml.x == -INFINITY ? 0.f : w * ml.y;
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off);
+        }
 #pragma unroll
         for (int p = 0; p < AT_ONCE; ++p) {
             const float wp = __shfl(w, p0 + p);
             const bool none = p0 + p >= n || __shfl(ml.x, p0 + p) == -INFINITY;   // (its sums may be anything)
-#pragma unroll
-            for (int e = 0; e < EACH; ++e)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[e][i] = none ? acc[e][i] : fmaf(wp, v[p][e][i], acc[e][i]);
+            if constexpr (EACH == 2) {
+                acc[0] = none ? acc[0] : fmaf(wp, v[p].x, acc[0]);
+                acc[1] = none ? acc[1] : fmaf(wp, v[p].y, acc[1]);
+            } else {
+                acc[0] = none ? acc[0] : fmaf(wp, v[p], acc[0]);
+            }
         }
     }
     const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-#pragma unroll
-    for (int e = 0; e < EACH; ++e)
-        *(reinterpret_cast<u32x2 *>(static_cast<char *>(a.out) + R * DC * 2) + e * 64 + lane) =
-            u32x2{bf16_pair(acc[e][0] * inv, acc[e][1] * inv), bf16_pair(acc[e][2] * inv, acc[e][3] * inv)};
+    const uint32_t out = bf16_pair(acc[0] * inv, acc[1] * inv);
+    char *const dst = static_cast<char *>(a.out) + R * DC * 2;
+    if constexpr (EACH == 2) reinterpret_cast<uint32_t *>(dst)[threadIdx.x] = out;
+    else reinterpret_cast<uint16_t *>(dst)[threadIdx.x] = static_cast<uint16_t>(out);
 }
 
 template <int DC, bool F8> void run_attention(const LatentArgs &a, unsigned grid, hipStream_t s) {
@@ -703,7 +712,8 @@ LatentPlan latent_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq) {
     // the CUs once.
     p.whole = p.units / kCus * kCus;
     const int64_t left = p.units - p.whole, room = static_cast<int64_t>(c.max_pages) << c.log_page;
-    if (left > 0) p.splits = static_cast<int32_t>(std::max<int64_t>(std::min({kCus / left, (room + kMinPieceLatent - 1) / kMinPieceLatent, kMaxPieces}), 1));
+    const int64_t most = std::max(std::min((room + kMinPieceLatent - 1) / kMinPieceLatent, kFewPieces), (room + kMinOfManyPieces - 1) / kMinOfManyPieces);
+    if (left > 0) p.splits = static_cast<int32_t>(std::max<int64_t>(std::min({kCus / left, most, kMaxPieces}), 1));
     p.grid = p.whole + left * p.splits;
     p.parts = p.splits > 1 ? left * p.splits * p.rows : 0;
     return p;
@@ -722,7 +732,7 @@ hipError_t launch_latent_attention(LatentArgs a, const LatentPlan &p, hipStream_
     if (a.c.D == 512) a.c.f8 ? run_attention<512, true>(a, grid, s) : run_attention<512, false>(a, grid, s);
     else a.c.f8 ? run_attention<256, true>(a, grid, s) : run_attention<256, false>(a, grid, s);
     if (p.splits > 1) {
-        const dim3 jgrid(static_cast<unsigned>((p.units - p.whole) * p.rows / 4));
+        const dim3 jgrid(static_cast<unsigned>((p.units - p.whole) * p.rows));
         if (a.c.D == 512) hipLaunchKernelGGL(k_latent_join<512>, jgrid, dim3(256), 0, s, a);
         else hipLaunchKernelGGL(k_latent_join<256>, jgrid, dim3(256), 0, s, a);
     }
