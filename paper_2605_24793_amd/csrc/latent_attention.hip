@@ -185,21 +185,38 @@ template <int DC> __device__ inline u32x4 query_piece(const char *queries, int r
     return *reinterpret_cast<const u32x4 *>(queries + row * QB + (piece ^ turned_rotated(row)) * 16);
 }
 
-// More rows: 64 of them a workgroup, with four waves for the scores and four for the sums, one of each on a SIMD.
-// While the latter add up one turn, the former work on the next, so that the matrix cores are fed by one wave while the
-// other is at its exponentials, conversions or waits.  (One wave for both leaves them idle then: a lone wave
-// issues a vector instruction every 7.5 cycles.  Two for both would need 144 registers of queries and 64 of sums
-// each, and room to work.)
+// A workgroup takes up to 64 rows of a sequence (or 32, where there are no more), and all its keys or a piece of them, with
+// four waves for the scores and four for the sums, one of each on a SIMD.  While the latter add up one turn, the
+// former work on the next, so that the matrix cores are fed by one wave while the other is at its exponentials,
+// conversions or waits.  (One wave for both leaves them idle then: a lone wave issues a vector instruction every 7.5
+// cycles.  Two for both would need 144 registers of queries and 64 of sums each, and room to work.)
 //
-// Scores: 32 rows and half of a turn's keys a wave, with products of 32 x 32 (turns of 64 keys) or 16 x 16 (32
-// keys, where 64 would not fit three times into LDS).  Sums: all rows and a quarter of the components a wave.
+// S^T = K Q^T and O^T = C^T P^T: the second product's operand C^T has positions where the rows lie; LDS turns
+// them while they are read (ds_read_b64_tr).  Scores: a part of a turn's keys and of the rows a wave, with products of
+// 32 x 32 (64 rows, turns of 64 keys) or 16 x 16.  Sums: all rows and a quarter of the components a wave.  The
+// rounded weights go from one to the other through LDS.
 //
 // After barrier i turn i is staged and turn i - 1 weighed: the scores' waves take turn i, the sums' waves turn
-// i - 1, and load ahead.  Rows' maxima as in k_latent_few.
+// i - 1, and load ahead.
+//
+// A row's weights are 2^(s - m) with m the maximum of the first turn in which it sees a key: that is as exact as with
+// the running one, as long as no later score is kFar above it.  Then the sums need not be scaled
+// down on the way, and all waves know m.  Where a score is, the piece is taken again: its maxima first, then the
+// sums (the rest of the pass that finds it is for nothing: nothing else may leave the loop, or the compiler
+// keeps the sums twice).
+//
+// 64 rows: the matrix cores bound them (2176 cycles of 3100 that a turn of 64 e4m3 keys takes; the sums' waves take 900 to
+// get its loads out, and between products they take as long and come later: 160 us instead of 149), then 20 000 cycles of
+// each workgroup's start and end.  64 x 17 queries of 32 heads after 1536 to 2048 e4m3 positions 149 us, 908 TFLOP/s; 16
+// trees of 60 nodes over bf16 136 us, 886.  Turns of 32 e4m3 keys took 178 us where those of 64 took 157; bf16 of 512
+// components has no room for three turns of 64.
+// 32 rows: memory bounds them, so turns are short and four are on their way: 64 x 1 query of 32 heads after up to
+// 4096 e4m3 positions 46.3 us, 3.3 TB/s with the join (turns of 64 keys, one on its way: 48.5; five of 32: 46.7).  With 64
+// rows half of them empty 52 us; 64 rows by two workgroups of 32 46.5 us for 37.8 (64 x 2 queries after 2048 positions).
 template <int DC, bool F8, int ROWS>
 __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
     constexpr int EB = F8 ? 1 : 2, RB = DC * EB;            // bytes of a latent
-    constexpr int KS = RB > 512 ? 32 : 64;                  // keys of a turn
+    constexpr int KS = RB > 512 || ROWS == 32 ? 32 : 64;    // keys of a turn
     constexpr bool WIDE = KS == 64 && ROWS == 64;           // scores by 32 x 32 products, or by 16 x 16
     constexpr int QW = WIDE ? 32 : 16, TK = QW;             // rows and keys of a tile of scores
     constexpr int KP = KS / TK, RP = 4 / KP;                // parts of the keys, and of the rows, among the scores' waves
@@ -209,7 +226,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
     constexpr int NS = WIDE ? 16 : 4;                       // scores of a lane and query tile
     constexpr int DT = DC / 4 / 32, RT = ROWS / 32;         // component tiles, and tiles of rows, of a sums' wave
     constexpr int kRotAt = KS * RB, kScaleAt = kRotAt + KS * kRotBytes, kStage = kScaleAt + (F8 ? KS * 4 : 0);
-    constexpr int NB = RB > 512 ? 4 : 3, AHEAD = NB - 2;    // turns in LDS, and on their way
+    constexpr int NB = RB > 512 ? 4 : ROWS == 32 ? 6 : 3, AHEAD = NB - 2;   // turns in LDS, and on their way
     constexpr int PPR = RB / 16;                            // pieces of a row
     constexpr int SR = KS / 4;                              // keys that a sums' wave loads
     constexpr int LPT = TurnLoads<DC, F8, SR>::COUNT;       // its loads of a turn
@@ -364,7 +381,9 @@ __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
                 for (int i = 0; i <= turns; ++i, buf = buf + 1 == NB ? 0 : buf + 1) {
                     const int k0 = seg + i * KS;
                     if constexpr (!SCORES) {                // turn i has come
-                        if (AHEAD > 1 && i + 1 < turns) wait_vm<LPT>();
+                        if (AHEAD > 3 && i + 3 < turns) wait_vm<3 * LPT>();
+                        else if (AHEAD > 2 && i + 2 < turns) wait_vm<2 * LPT>();
+                        else if (AHEAD > 1 && i + 1 < turns) wait_vm<LPT>();
                         else wait_vm<0>();
                     }
                     lds_barrier();
