@@ -211,8 +211,9 @@ template <int DC> __device__ inline u32x4 query_piece(const char *queries, int r
 // trees of 60 nodes over bf16 136 us, 886.  Turns of 32 e4m3 keys took 178 us where those of 64 took 157; bf16 of 512
 // components has no room for three turns of 64.
 // 32 rows: memory bounds them, so turns are short and four are on their way: 64 x 1 query of 32 heads after up to
-// 4096 e4m3 positions 46.3 us, 3.3 TB/s with the join (turns of 64 keys, one on its way: 48.5; five of 32: 46.7).  With 64
-// rows half of them empty 52 us; 64 rows by two workgroups of 32 46.5 us for 37.8 (64 x 2 queries after 2048 positions).
+// 4096 e4m3 positions 46.3 us, 3.3 TB/s with the join (turns of 64 keys, one on its way: 48.5; five of 32: 46.7).  The other
+// choice: these with 64 rows, half of them empty, 50.8 us; 64 x 17 queries by workgroups of 32 rows 201 us for 151, 64 x 2
+// after 2048 positions 42.8 for 36.4.
 template <int DC, bool F8, int ROWS>
 __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
     constexpr int EB = F8 ? 1 : 2, RB = DC * EB;            // bytes of a latent

@@ -14,8 +14,12 @@ namespace {
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kEntryThreads = 256;
+
+// A copy is bound by memory; a thread has four 16-byte loads out at a time, and eight workgroups of them share a CU.  64
+// pages of 2 MB (8 layers) that 8 sequences share: 45.1 us with pieces of 16 KB, 53.8 of 8, 49.2 of 32; 46.7 with
+// 1024 workgroups, 44.8 with 4096, where 449 MB of separate pages take 105 and 107.
 constexpr int kPieceBytes = 16384;    // of a page's plane, one workgroup's turn
-constexpr int kCopyWorkgroups = 2048; // eight a CU
+constexpr int kCopyWorkgroups = 2048;
 constexpr int kPoolWaves = kPoolThreads / 64;
 
 __device__ inline bool names_page(int32_t e, int64_t n_pages) { return e >= 0 && e < n_pages; }
@@ -222,7 +226,8 @@ __global__ __launch_bounds__(kEntryThreads) void k_pages_entries(CompactArgs a) 
                  static_cast<int64_t>(gridDim.x) * kEntryThreads);
 }
 
-// Pieces of 16 KB of a page's planes, dealt to the workgroups.
+// Pieces of a page's planes, dealt to the workgroups: 4.4 TB/s read and written where no page is read twice (32 sequences' pages,
+// 449 MB), 4.7 for a large copy.
 __global__ __launch_bounds__(kEntryThreads) void k_pages_copy(CopyArgs a) {
     const int tid = threadIdx.x;
     const int pairs = a.count ? min(max(*a.count, 0), a.n_pairs) : a.n_pairs;
@@ -259,7 +264,8 @@ __global__ __launch_bounds__(kEntryThreads) void k_pages_copy(CopyArgs a) {
     }
 }
 
-// Tables of more entries are rewritten by many workgroups, in a launch of their own.
+// Tables of more entries are rewritten by many workgroups, in a launch of their own, which costs 3 us of a small pool's
+// 21 (4 sequences of 700 positions, 300 pages to spare).
 constexpr int64_t kEntriesInPlace = 16384;
 
 unsigned entry_grid(int64_t n) { return static_cast<unsigned>((n + kEntryThreads - 1) / kEntryThreads); }
