@@ -147,8 +147,9 @@ template <int N> __device__ inline void load_lds_rows(const char *base, const ui
     else {
         static_assert(N % 4 == 0);
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\t"
-                     "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:3072"
-                     : : "s"(lds), "s"(base), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]) : "memory", "m0");
+                     "global_load_lds_dwordx4 %4, %1 offset:%6\n\tglobal_load_lds_dwordx4 %5, %1 offset:%7"
+                     : : "s"(lds), "s"(base), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "i"(2 * 1024), "i"(3 * 1024)
+                     : "memory", "m0");
         if constexpr (N > 4) load_lds_rows<N - 4>(base + 4096, off + 4, lds + 4096);
     }
 }
