@@ -208,7 +208,7 @@ template <int DC> __device__ inline u32x4 query_piece(const char *queries, int r
 // 64 rows: the matrix cores bound them (2176 cycles of 3100 that a turn of 64 e4m3 keys takes; the sums' waves take 900 to
 // get its loads out, and between products they take as long and come later: 160 us instead of 149), then 20 000 cycles of
 // each workgroup's start and end.  64 x 17 queries of 32 heads after 1536 to 2048 e4m3 positions 149 us, 908 TFLOP/s; 16
-// trees of 60 nodes over bf16 136 us, 886.  Turns of 32 e4m3 keys took 178 us where those of 64 took 157; bf16 of 512
+// trees of 60 nodes over bf16 135 us, 893.  Turns of 32 e4m3 keys took 178 us where those of 64 took 157; bf16 of 512
 // components has no room for three turns of 64.
 // 32 rows: memory bounds them, so turns are short and four are on their way: 64 x 1 query of 32 heads after up to
 // 4096 e4m3 positions 46.3 us, 3.3 TB/s with the join (turns of 64 keys, one on its way: 48.5; five of 32: 46.7).  The other
