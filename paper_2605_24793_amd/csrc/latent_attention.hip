@@ -11,6 +11,7 @@
 
 #include "attend.h"
 #include "latent.h"
+#include "turn_flags.h"
 
 namespace cospec {
 namespace {
@@ -239,7 +240,8 @@ __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
     __shared__ float s_max[KP][ROWS];
     __shared__ float s_sum[KP][ROWS];
     __shared__ uint32_t s_bad[2];                           // of a turn's keys: latent or scale not finite
-    __shared__ int s_new, s_far, s_none;
+    __shared__ TurnFlags s_new;                             // a row's first keys, or a score far above its m
+    __shared__ int s_far, s_none;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int gh = lane >> 5, l32 = lane & 31;
@@ -266,7 +268,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
         if (tid < ROWS * 8) s_seen[tid / 8][tid % 8] = anc[quot(a.by_grp, min(q0 + tid / 8, q1 - 1))][tid % 8];
         __syncthreads();
     }
-    if (tid == 0) s_new = s_far = 0;
+    if (tid == 0) s_new.lower_all(), s_far = 0;
     wait_vm<0>();
     __syncthreads();                                        // the queries are there
 
@@ -408,7 +410,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
                             }
                         }
                     };
-                    if (__builtin_expect(uniform(s_new), 0)) {
+                    if (__builtin_expect(uniform(s_new.raised(i - 1)), 0)) {
                         // the same maximum in all waves, then the weights of turn i - 1 again
                         if constexpr (SCORES) {
                             if (kg == 0) {
@@ -418,7 +420,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
                         }
                         lds_barrier();
                         if constexpr (SCORES) {
-                            if (tid == 0) s_new = 0;
+                            if (tid == 0) s_new.lower(i - 1);
                             bool above = false;
 #pragma unroll
                             for (int t = 0; t < QT; ++t) {
@@ -548,7 +550,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
 #pragma unroll
                             for (int t = 0; t < QT; ++t) m[t] = fmaxf(m[t], bm[t]);
                         } else if (__ballot(fresh) != 0 && lane == 0) {
-                            s_new = 1;
+                            s_new.raise(i);
                         }
                     } else {
                         const int to = buf + AHEAD >= NB ? buf + AHEAD - NB : buf + AHEAD;
