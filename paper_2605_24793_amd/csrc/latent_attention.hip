@@ -692,7 +692,8 @@ __global__ __launch_bounds__(256) void k_latent_join(LatentArgs a) {
 #pragma unroll
             for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
             w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
-            l = ml.x == -INFINITY ? 0.f : w * ml.y;
+            // (a piece without a maximum has a weight sum of 0, or of NaN where the row saw only scores that are NaN)
+            l = ml.x == -INFINITY ? ml.y : w * ml.y;
 #pragma unroll
             for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off);
         }

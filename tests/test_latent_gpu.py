@@ -229,6 +229,66 @@ def test_a_query_that_is_not_finite_stays_alone():
     assert torch.equal(good, out)
 
 
+def _cut(q, cache, table, ctx, q_start, scale=0.07):
+    """cs.latent_attention, of calls whose keys are cut into pieces that are joined."""
+    call = cs.prepare_latent_attention(q.to(DEV), cache, table.to(DEV), _int(ctx), _int(q_start), 0, scale)
+    assert call.workspace is not None
+    call.launch()
+    return call.outputs["out"]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F8])
+@pytest.mark.parametrize("dc,n,Hq,ctx", [(256, 1, 8, 300), (512, 1, 32, 2000), (512, 6, 8, 700), (256, 6, 8, 140)])
+def test_a_query_that_is_not_finite_stays_alone_over_pieces(dtype, dc, n, Hq, ctx):
+    P = 16
+    table, n_pages = _table(2, -(-ctx // P), 9)
+    cache = _filled(table, n_pages, dc, P, dtype, [ctx, ctx - 9], 9)
+    q = (torch.randn(2, n, Hq, dc + 64, generator=_gen(9)) * 0.6).to(BF16)
+    bad = q.clone()
+    bad[0, n // 2, 3, 7] = math.nan
+    args = (cache, table, [ctx, ctx - 9], [ctx - n, ctx - 9 - n])
+    good, out = _cut(q, *args), _cut(bad, *args)
+    assert bool(torch.isfinite(good).all())
+    assert bool(torch.isnan(out[0, n // 2, 3]).all())
+    out[0, n // 2, 3] = good[0, n // 2, 3]
+    assert torch.equal(good, out)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F8])
+@pytest.mark.parametrize("where", ["latent", "key", "scale"])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("n,Hq,ctx", [(1, 8, 129), (1, 40, 257), (14, 3, 140), (14, 20, 268)])
+def test_what_is_not_finite_alone_in_a_piece(dtype, where, value, n, Hq, ctx):
+    """The first position of the last piece: a query there sees nothing else in it."""
+    if where == "scale" and dtype == BF16:
+        pytest.skip("bf16 latents have no scales")
+    P, dc = 16, 256
+    bad = (ctx - 1) // 128 * 128
+    table, n_pages = _table(1, -(-ctx // P), 9)
+    cache = _filled(table, n_pages, dc, P, dtype, [ctx], 9)
+    page, slot = int(table[0, bad // P]), bad % P
+    q = (torch.randn(1, n, Hq, dc + 64, generator=_gen(9)) * 0.6).to(BF16).to(DEV)
+    if where == "latent":
+        cache.c[page, slot, 17] = torch.tensor(math.nan if dtype == F8 else value).to(dtype)
+    elif where == "key":
+        cache.r[page, slot, 5] = value
+    else:
+        cache.scale[page, slot] = value
+    first = ctx - n
+    out = _cut(q, cache, table, [ctx], [first])
+    # queries before it: as if it held nothing
+    _check(out, cache, table, q, lambda b, room: ref.hybrid_sees(ctx, first, 0, n, room) & (torch.arange(room) != bad), 0.07,
+           rows=range(bad - first))
+    seen = out[0, bad - first:].float()
+    if where == "key" and value == value:
+        # plus infinity (NaN) or minus infinity (weight zero) of a score, by the query's sign
+        up = (q[0, bad - first:, :, dc + 5].float() * value) > 0
+        assert bool(torch.isnan(seen).all(-1)[up].all())
+        assert bool(torch.isfinite(seen[~up]).all())
+    else:
+        assert bool(torch.isnan(seen).any(-1).all())
+
+
 def _parents(B, N, seed, kind="random"):
     g = _gen(seed)
     p = torch.full((B, N), -1, dtype=torch.int32)
