@@ -341,6 +341,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
 
         // Once, unless a score lies far above its row's m: then once more for the maxima alone, and again for the sums.
         bool finding = false;
+        [[maybe_unused]] bool met = false;                  // a turn without a mask: every live row sees all of its keys
         for (;;) {
             [[maybe_unused]] floatx16 o[RT][DT];
             [[maybe_unused]] float l[QT];                   // of this lane's keys alone
@@ -450,6 +451,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
                             for (int t = 0; t < QT; ++t) l[t] += sum[t];
                         }
                         if (i == turns) break;
+                        met |= !masked;
                         // S^T.  Operands are read from LDS a group ahead of the products that take them.
                         constexpr int LP = WIDE ? 2 : 4, PER = 16 / LP;  // pieces of a key that a load's lanes take side by side
                         constexpr int LOADS = CS / (F8 ? 2 : 1), G = F8 ? 2 : 4, NG = LOADS / G;
@@ -605,8 +607,9 @@ __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
                     l[t] += __shfl_xor(l[t], 32);
                     const int row = rw * (QT * QW) + t * QW + ql;
                     if (kg == 0) {
-                        // (unmasked turns give padding rows some weights)
-                        s_sum[kp][row] = node[t] >= 0 ? l[t] : 0.f;
+                        // (unmasked turns give padding rows some weights; a row that met only scores of minus infinity, as
+                        // infinite latents make them, has none, and sums that are not finite)
+                        s_sum[kp][row] = node[t] < 0 ? 0.f : met && m[t] == -INFINITY ? NAN : l[t];
                         s_max[kp][row] = node[t] >= 0 || finding ? m[t] : -INFINITY;
                     }
                 }

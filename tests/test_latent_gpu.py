@@ -289,6 +289,25 @@ def test_what_is_not_finite_alone_in_a_piece(dtype, where, value, n, Hq, ctx):
         assert bool(torch.isnan(seen).any(-1).all())
 
 
+@pytest.mark.parametrize("dtype", [BF16, F8])
+@pytest.mark.parametrize("n,Hq,ctx", [(1, 8, 64), (1, 40, 128), (1, 8, 256), (3, 20, 640), (1, 8, 300)])
+def test_infinite_latents_where_no_score_is_above_minus_infinity(dtype, n, Hq, ctx):
+    """Every latent that a query sees is infinite, and every score minus infinity: in one piece and in several."""
+    P, dc = 16, 256
+    table, n_pages = _table(2, -(-ctx // P), 9)
+    cache = _filled(table, n_pages, dc, P, dtype, [ctx, ctx], 9)
+    pages = table[0].long().to(DEV)
+    if dtype == BF16:
+        cache.c[pages, :, 17] = math.inf
+    else:
+        cache.c[pages] = torch.ones(1, device=DEV).to(F8)
+        cache.scale[pages] = math.inf
+    q = (torch.rand(2, n, Hq, dc + 64, generator=_gen(9)) * -0.6 - 0.1).to(BF16).to(DEV)
+    out = cs.latent_attention(q, cache, table.to(DEV), _int([ctx, ctx]), _int([ctx - n, ctx - n]), 0, 0.07)
+    assert bool((~torch.isfinite(out[0])).any(-1).all())
+    assert bool(torch.isfinite(out[1]).all())                # (the other sequence)
+
+
 def _parents(B, N, seed, kind="random"):
     g = _gen(seed)
     p = torch.full((B, N), -1, dtype=torch.int32)
