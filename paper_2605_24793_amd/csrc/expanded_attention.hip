@@ -280,8 +280,9 @@ __global__ __launch_bounds__(64 * kWavesExpanded, 2) void k_expanded_attention(E
     l += __shfl_xor(l, 32);
     if (!valid) return;
     // O^T tile t, elements 4e .. 4e + 3: components 32 t + 8 e + 4 gh + 0..3 of this lane's row
-    if (!live) l = 0.f;                                     // (unmasked turns gave it some weights)
-    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;   // NaN stays
+    // A row that sees nothing gets zeros (unmasked turns gave it some weights).  NaN stays, also in sums without a weight, as
+    // scores of minus infinity alone leave them where a value is not finite.
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
     char *dst = a.out + (R * D + 4 * gh) * 2;
 #pragma unroll
     for (int t = 0; t < DT; ++t)
@@ -289,7 +290,7 @@ __global__ __launch_bounds__(64 * kWavesExpanded, 2) void k_expanded_attention(E
         for (int e = 0; e < 4; ++e) {
             floatx4 x;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = l == 0.f ? 0.f : o[t][4 * e + i] * inv;
+            for (int i = 0; i < 4; ++i) x[i] = live ? o[t][4 * e + i] * inv : 0.f;
             *reinterpret_cast<u32x2 *>(dst + (32 * t + 8 * e) * 2) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
         }
 }

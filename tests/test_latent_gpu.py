@@ -584,6 +584,22 @@ def test_expanded_values_that_are_not_finite(n):
 
 
 @pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("ctx,n", [(64, 1), (64, 9), (256, 130)])
+def test_expanded_values_that_are_not_finite_where_no_score_is_above_minus_infinity(d, ctx, n):
+    g = _gen(5)
+    q = -torch.rand(1, n, 2, d + 64, generator=g).to(BF16).to(DEV) - 0.1
+    kv = torch.randn(1, ctx, 2, 2 * d, generator=g).to(BF16).to(DEV)
+    k_r = torch.randn(1, ctx, 64, generator=g).to(BF16).to(DEV)
+    args = (k_r, _int([ctx]), _int([ctx - n]), 0, 0.08)
+    good = cs.expanded_attention(q, kv[..., :d], kv[..., d:], *args)
+    kv[0, :, 1, 4] = math.inf                               # a component of every key
+    kv[0, 3, 1, d + 10] = math.nan                          # one of a value that all queries see
+    out = cs.expanded_attention(q, kv[..., :d], kv[..., d:], *args)
+    assert bool(torch.isnan(out[0, :, 1, 10]).all())
+    assert torch.equal(out[0, :, 0], good[0, :, 0])
+
+
+@pytest.mark.parametrize("d", [128, 64])
 @pytest.mark.parametrize("layout", ["heads first", "one key for all", "wide"])
 def test_expanded_strides(d, layout):
     """Heads before positions, one position's key and value for every position, and rows of 2^24 bytes and more."""
