@@ -1035,6 +1035,8 @@ def prepare_latent_append(cache: LatentCache, table, start, c, k_r, weight: Opti
         if tuple(q_out.shape) != (B, n, Hq, _ROT):
             raise ValueError("q_out must have q's shape")
         ld_out, head_out = _head_rows(q_out, B, n, _ROT, "q_out")
+        if Hq == 1:
+            head_out = ld_out                               # one head: the distance of its tokens
         if B * n > 1 and ld_out != Hq * head_out:
             raise ValueError("q_out's tokens must lie one after the other")
         outputs["q"] = q_out

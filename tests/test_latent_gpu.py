@@ -469,6 +469,22 @@ def test_append_forms(dtype, kw):
     _run_append(dtype, 512, 32, 5, [0, 30, 64], seed=3, **kw)
 
 
+@pytest.mark.parametrize("B,n", [(1, 1), (1, 7), (3, 1), (2, 5)])
+def test_one_heads_queries_into_the_attentions(B, n):
+    dc, P, g = 256, 16, _gen(B * n)
+    table, n_pages = _table(B, 2, 3)
+    cache = cs.LatentCache.empty(n_pages, dc, P)
+    x = torch.randn(B, n, dc + 64, generator=g).to(BF16).to(DEV)
+    q = torch.randn(B, n, 1, 64, generator=g).to(BF16).to(DEV)
+    inv_freq = (10000.0 ** (-torch.arange(32) / 32)).to(DEV)
+    args = (cache, table.to(DEV), _int([4] * B), x[..., :dc], x[..., dc:])
+    want = cs.latent_append(*args, inv_freq=inv_freq, q=q)["q"]
+    whole = torch.full((B, n, 1, dc + 64), 7.0, dtype=BF16, device=DEV)
+    out = cs.latent_append(*args, inv_freq=inv_freq, q=q, q_out=whole[..., dc:])["q"]
+    assert torch.equal(out, want) and torch.equal(whole[..., dc:], want)
+    assert bool((whole[..., :dc] == 7).all())
+
+
 @pytest.mark.parametrize("dtype", [BF16, F8])
 def test_append_where_there_is_no_place(dtype):
     # before the first position, behind the last one, on no page
