@@ -719,7 +719,10 @@ cospec_status cospec_pages_fork(const cospec_page_pool *pool, const int32_t *tab
  * An entry that names no page gets one, and an entry whose page others hold too gets another one instead; pages
  * are the free ones of lowest number, in the order of the sequences and their positions.
  *  copies  [B][2] out: {from, to} where the sequence's first new position lies inside a page that was shared, whose
- *          earlier positions it needs a copy of (cospec_pages_copy), else {-1, -1}.
+ *          earlier positions it needs a copy of (cospec_pages_copy), else {-1, -1}.  Where all that shared a page
+ *          leave it in one call, `from` is free afterwards: the copies must be enqueued before the next reserve or
+ *          compact of the pool, which may hand it out or move another page there, and before the
+ *          new positions are written.
  *  lacking [1] out: 0, or how many pages are missing; then nothing is changed, and copies are -1.
  *  workspace 256-byte aligned, cospec_pages_reserve_workspace_size(pool, B, n) bytes.
  */
@@ -738,7 +741,8 @@ cospec_status cospec_pages_release(const cospec_page_pool *pool, int32_t *table,
  * Moves the pages in use to the front: with U of them, those numbered U and above take, in order, the free numbers
  * below U.  table must hold every entry that names a page of the pool.
  *  moves    [max(n_pages / 2, 1)][2] out: {from, to}, then {-1, -1};  n_moves [1] out.  (cospec_pages_copy moves
- *           what the pages hold.)
+ *           what the pages hold: to be enqueued before anything else reads or writes them, and before the pool's next
+ *           reserve or compact.)
  *  workspace 256-byte aligned, cospec_pages_compact_workspace_size(pool) bytes.
  */
 size_t cospec_pages_compact_workspace_size(const cospec_page_pool *pool);

@@ -1258,7 +1258,9 @@ def prepare_pages_reserve(pool: PagePool, table, start, n: int, count: Optional[
                           caches=()) -> PoolCall:
     """Pre-marshalled cospec_pages_reserve: positions start[b] .. start[b] + count[b] - 1 (int32 [B]; count
     None: n) get pages of their sequence's own in table, and the caches' pages are copied where a sequence leaves a
-    page that others share inside it.  outputs: copies [B, 2], lacking [1] (0: done; else nothing was)."""
+    page that others share inside it.  outputs: copies [B, 2], lacking [1] (0: done; else nothing was).
+    Caches that are left out have to take the copies by pages_copy before the pool's next reserve or compact and before
+    new positions are written: a page that all its holders left is free."""
     B, T = pool._table(table)
     start = _i32_kept(start, B, "start")
     if count is not None:
@@ -1300,7 +1302,8 @@ def pages_release(pool: PagePool, table, keep) -> None:
 
 def prepare_pages_compact(pool: PagePool, table, caches=()) -> PoolCall:
     """Pre-marshalled cospec_pages_compact: the pages in use move to the pool's front, in table (which must hold
-    every entry that names one) and in the caches.  outputs: moves [n_pages // 2, 2] and n_moves [1]."""
+    every entry that names one) and in the caches.  outputs: moves [n_pages // 2, 2] and n_moves [1].  Caches that are
+    left out have to take the moves by pages_copy (with n_moves) before they are used again."""
     B, T = pool._table(table)
     caches = list(caches)
     dev = pool.refs.device

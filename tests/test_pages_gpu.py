@@ -219,6 +219,31 @@ def test_branches_of_a_prompt():
     assert all(torch.equal(a, b) for a, b in zip(alone, reads(both[:2].contiguous(), lens, slice(0, 2))))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F8])
+def test_all_holders_of_a_page_leave_it_at_once(dtype):
+    """The page that they share is free then, and still holds what their copies take; the next reserve hands it out."""
+    g = torch.Generator().manual_seed(4)
+    P, n_pages, dc = 16, 8, 256
+    pool, cache = cs.PagePool.empty(n_pages, P), cs.LatentCache.empty(n_pages, dc, P, dtype)
+    prompt = torch.full((1, 3), -1, dtype=torch.int32, device=DEV)
+    cs.pages_reserve(pool, prompt, _int([0]), 20)
+    x = torch.randn(1, 20, dc + 64, generator=g).to(BF16).to(DEV)
+    cs.latent_append(cache, prompt, _int([0]), x[..., :dc], x[..., dc:])
+    fork = cs.pages_fork(pool, prompt, _int([0, 0, 0]), _int([20, 20, 20]))
+    cs.pages_release(pool, prompt, _int([0]))
+    assert pool.refs.tolist() == [3, 3] + [0] * 6
+    before = [t[1].view(torch.uint8).clone() for t in cache._planes()]
+    out = cs.pages_reserve(pool, fork, _int([20, 20, 20]), 4, caches=[cache])
+    assert int(out["lacking"]) == 0 and out["copies"].tolist() == [[1, 2], [1, 3], [1, 4]]
+    assert fork.tolist() == [[0, 2, -1], [0, 3, -1], [0, 4, -1]]
+    assert pool.refs.tolist() == [3, 0, 1, 1, 1, 0, 0, 0]
+    for t, old in zip(cache._planes(), before):
+        assert all(torch.equal(t[p].view(torch.uint8), old) for p in (1, 2, 3, 4))
+    other = torch.full((1, 3), -1, dtype=torch.int32, device=DEV)
+    cs.pages_reserve(pool, other, _int([0]), 1)
+    assert other.tolist() == [[1, -1, -1]]
+
+
 def test_captured_turns_of_a_pool():
     """Fork, reserve with copies, release and compact in one graph, replayed."""
     P, n_pages, T = 16, 64, 6
