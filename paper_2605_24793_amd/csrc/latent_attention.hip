@@ -750,7 +750,6 @@ hipError_t launch_latent_attention(LatentArgs a, const LatentPlan &p, hipStream_
     a.row_tiles = p.rows;
     a.splits = p.splits;
     a.min_piece = kMinPieceLatent;
-    a.units = static_cast<int32_t>(p.units);
     a.whole = static_cast<int32_t>(p.whole);
     a.by_grp = fast_div(a.Hq);
     a.by_blocks = fast_div(p.blocks);
