@@ -341,7 +341,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
 
         // Once, unless a score lies far above its row's m: then once more for the maxima alone, and again for the sums.
         bool finding = false;
-        [[maybe_unused]] bool met = false;                  // a turn without a mask: every live row sees all of its keys
+        [[maybe_unused]] bool met = false;                  // a turn without a mask: live rows see all of its keys
         for (;;) {
             [[maybe_unused]] floatx16 o[RT][DT];
             [[maybe_unused]] float l[QT];                   // of this lane's keys alone
@@ -371,6 +371,7 @@ __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
                 }
                 __syncthreads();
                 any_none = uniform(s_none) != 0;
+                met |= !any_none && seg + KS <= all_see;
                 [[maybe_unused]] uint32_t next = 0;         // the page that is loaded from next
                 if constexpr (!SCORES) {
 #pragma unroll
@@ -451,7 +452,6 @@ __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
                             for (int t = 0; t < QT; ++t) l[t] += sum[t];
                         }
                         if (i == turns) break;
-                        met |= !masked;
                         // S^T.  Operands are read from LDS a group ahead of the products that take them.
                         constexpr int LP = WIDE ? 2 : 4, PER = 16 / LP;  // pieces of a key that a load's lanes take side by side
                         constexpr int LOADS = CS / (F8 ? 2 : 1), G = F8 ? 2 : 4, NG = LOADS / G;
