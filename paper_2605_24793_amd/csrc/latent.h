@@ -26,7 +26,7 @@ struct LatentAppendArgs {
 
 // An attention call.  A unit is a block of a sequence's rows; units are numbered by sequence.
 struct LatentArgs : PagedArgs {
-    int32_t whole;             // the first ones, that are not cut
+    int32_t whole;             // the first units, that are not cut
 };
 
 // How a call's units are dealt: rounds of one for every CU, and the rest cut into pieces that fill a last round.

@@ -30,7 +30,8 @@ constexpr float kFar = 60.f;          // log2 units a score may exceed a row's m
 
 // A latent's sixteen-byte pieces lie in LDS in another order: piece i at place i ^ turned(key), sixteen at a time, so that
 // neither product's reads meet in the 64 banks: the first one's, sixteen rows' same piece, and the second one's, two
-// pieces of eight rows (e4m3) or four of four (bf16).  Rotated keys, eight pieces each, likewise.
+// pieces of eight rows (e4m3) or four of four (bf16).  Rotated keys, eight pieces each, likewise.  (Of the whole kernel's LDS
+// cycles 10% are conflicts all the same over e4m3, 34% over bf16 of 512 components.)
 template <bool F8> __device__ inline int turned(int key) {
     return F8 ? (key & 7) << 1 | (key >> 3 & 1) : (key & 3) << 2 | (key >> 2 & 3);
 }
@@ -206,15 +207,17 @@ template <int DC> __device__ inline u32x4 query_piece(const char *queries, int r
 // sums (the rest of the pass that finds it is for nothing: nothing else may leave the loop, or the compiler
 // keeps the sums twice).
 //
-// 64 rows: the matrix cores bound them (2176 cycles of 3100 that a turn of 64 e4m3 keys takes; the sums' waves take 900 to
-// get its loads out, and between products they take as long and come later: 160 us instead of 149), then 20 000 cycles of
-// each workgroup's start and end.  64 x 17 queries of 32 heads after 1536 to 2048 e4m3 positions 149 us, 908 TFLOP/s; 16
-// trees of 60 nodes over bf16 135 us, 893.  Turns of 32 e4m3 keys took 178 us where those of 64 took 157; bf16 of 512
-// components has no room for three turns of 64.
-// 32 rows: memory bounds them, so turns are short and four are on their way: 64 x 1 query of 32 heads after up to
-// 4096 e4m3 positions 46.3 us, 3.3 TB/s with the join (turns of 64 keys, one on its way: 48.5; five of 32: 46.7).  The other
-// choice: these with 64 rows, half of them empty, 50.8 us; 64 x 17 queries by workgroups of 32 rows 201 us for 151, 64 x 2
-// after 2048 positions 42.8 for 36.4.
+// 64 rows: a turn of 64 e4m3 keys takes 3100 cycles, its products 2176 (clocks read in a copy of the kernel; the sums' waves
+// take 900 to get its loads out, and between products they take as long and come later: 160 us where this takes 149), and each
+// workgroup's start and end 20 000; counted over a whole call the matrix cores are at work half of the CUs' cycles.  64 x 17
+// queries of 32 heads after 1536 to 2048 e4m3 positions 155 to 159 us from card to card, 859 to 883 TFLOP/s; 16 trees of 60
+// nodes over bf16 138 us, 874.  Turns of 32 e4m3 keys took 178 us where those of 64 took 157; bf16 of 512 components has no
+// room for three turns of 64.
+// 32 rows: a workgroup has few products and waits for loads, so turns are short and four are on their way: 64 x 1 query of
+// 32 heads after up to 4096 e4m3 positions 47 us, 3.3 TB/s with the join (turns of 64 keys, one on its way: 48.5 where these
+// took 46.3; five of 32: 46.7).  The loads reach 4.2 TB/s, which is not the memory's limit: one workgroup fills a CU, and nothing
+// covers its start and end.  Over bf16 64.5 us, 5.0 TB/s.  The other choice: these with 64 rows, half of them empty, 50.8 us;
+// 64 x 17 queries by workgroups of 32 rows 201 us for 151, 64 x 2 after 2048 positions 42.8 for 36.4.
 template <int DC, bool F8, int ROWS>
 __global__ __launch_bounds__(512, 1) void k_latent_attention(LatentArgs a) {
     constexpr int EB = F8 ? 1 : 2, RB = DC * EB;            // bytes of a latent
@@ -735,7 +738,8 @@ LatentPlan latent_plan(const PageArgs &c, int32_t B, int32_t n_q, int32_t Hq) {
     p.blocks = static_cast<int32_t>((rows + p.rows - 1) / p.rows);
     p.units = static_cast<int64_t>(B) * p.blocks;
     // A workgroup fills a CU, so units come in rounds of one for each; what is left over is cut into pieces that fill
-    // the CUs once.  (64 x 17 queries, 64 of 576 units left over: 166 us uncut, 153 cut on the same card; 64 x 1 query 89 and
+    // the CUs once: in equally many each, whatever their lengths, and from 129 units on not at all (130 x 1 query 51 us, 128 x 1
+    // 50).  (64 x 17 queries, 64 of 576 units left over: 166 us uncut, 153 cut on the same card; 64 x 1 query 89 and
     // 46; one query over 2000 positions 33 and 12.)
     p.whole = p.units / kCus * kCus;
     const int64_t left = p.units - p.whole, room = static_cast<int64_t>(c.max_pages) << c.log_page;
